@@ -45,7 +45,8 @@ typedef enum {
 typedef enum { H3_F32 = 0, H3_F16 = 1, H3_BF16 = 2 } h3_dtype;
 
 /* Operation codes for h3_workspace_size. */
-enum { H3_OP_FFTCONV = 1, H3_OP_STATEPASS = 2, H3_OP_LAYER = 3, H3_OP_FFTCONV_BWD = 4, H3_OP_LAYER_HEADS = 5 };
+enum { H3_OP_FFTCONV = 1, H3_OP_STATEPASS = 2, H3_OP_LAYER = 3, H3_OP_FFTCONV_BWD = 4, H3_OP_LAYER_HEADS = 5,
+       H3_OP_LAYERNORM_BWD = 6, H3_OP_DELTA = 7, H3_OP_DELTA_SAVED = 8, H3_OP_DELTA_BWD = 9 };
 
 /* Limits of this build. */
 #define H3_MAX_MODES 64     /* m: complex modes per channel of a diagonal SSM      */
@@ -54,6 +55,8 @@ enum { H3_OP_FFTCONV = 1, H3_OP_STATEPASS = 2, H3_OP_LAYER = 3, H3_OP_FFTCONV_BW
 #define H3_FUSED_LIMIT_F32 8192  /* the same for float32 I/O, the spectral entry points and
                                     the kernel gradient of h3_fftconv_bwd                    */
 #define H3_MAX_SHIFT 64     /* longest shift-SSM filter in h3_layer_fwd            */
+#define H3_DELTA_MAX_DK 128 /* largest key size of the delta rule's state          */
+#define H3_DELTA_MAX_DV 256 /* largest value size of the delta rule's state        */
 
 /*
  * h3_ssm_discretize — zero-order-hold discretisation of H diagonal SSMs of m
@@ -263,8 +266,60 @@ int h3_layer_fwd_heads(const void *x, const void *Wq, const void *Wk, const void
                        void *workspace, size_t ws_bytes, void *stream);
 
 /*
+ * h3_layernorm — layer norm over the last dimension, as in front of the mixers
+ * of a pre-norm block:
+ *   mean = sum_j x_j / d,  rstd = (sum_j (x_j - mean)^2 / d + eps)^-1/2,
+ *   y_j = (x_j - mean) rstd w_j + b_j          per row.
+ *   x, y        (rows, d) of `dtype`, aligned to their element; y may be x,
+ *               and otherwise does not overlap it.
+ *   w, b        (d) float32, or NULL for 1 and 0.
+ *   eps         >= 0.
+ *   mean, rstd  (rows) float32, written, or NULL.  They overlap nothing.
+ * Arithmetic in float32.  Any d >= 1; rows and row sizes that are multiples of
+ * 16 bytes are read 16 bytes at a time.
+ * Errors: EINVAL, EUNSUPPORTED (dtype), EDEVICE.
+ */
+int h3_layernorm(const void *x, const float *w, const float *b, int rows, int d, float eps, int dtype, void *y,
+                 float *mean, float *rstd, void *stream);
+
+/*
+ * h3_layernorm_bwd — backward pass of h3_layernorm for an output gradient dy,
+ * from the mean and rstd that it wrote: with xh = (x - mean) rstd, t = dy w,
+ *   dx = rstd (t - mean_j(t) - xh mean_j(t xh)),
+ *   dw_j = sum over rows of dy_j xh_j,   db_j = sum over rows of dy_j.
+ *   dy, x, dx   (rows, d) of `dtype`, dx not overlapping dy or x, except that dx may be dy or x itself
+ *               where neither dw nor db is asked.
+ *   w           (d) float32 or NULL.   mean, rstd (rows) float32.
+ *   dw, db      (d) float32.  Each of dx, dw, db may be NULL, not all three.
+ *   workspace   >= h3_workspace_size(H3_OP_LAYERNORM_BWD, rows, d, 1, 0, 0, dtype)
+ *               (partial sums of dw and db, added in a fixed order).
+ * Errors: EINVAL, EUNSUPPORTED (dtype), EWORKSPACE, EDEVICE.
+ */
+int h3_layernorm_bwd(const void *dy, const void *x, const float *w, const float *mean, const float *rstd, int rows,
+                     int d, int dtype, void *dx, float *dw, float *db, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * h3_delta_step — the gated delta rule in its recurrent form, for generation:
+ * for each sequence b and head h, with a state S of Dk x Dv, over T tokens
+ *   S <- exp(g_t) S;   e_t = v_t - S^T k_t;   S <- S + k_t (beta_t e_t)^T;
+ *   o_t = scale S^T q_t.
+ * A state written by h3_delta_rule continues that sequence.
+ *   q, k        (B, T, Hk, Dk) of `dtype`; value head h reads head h / (H / Hk).
+ *   v, o        (B, T, H, Dv) of `dtype`.
+ *   g, beta     (B, T, H) float32: log decay (0: none, -inf: the state is
+ *               dropped) and write strength.
+ *   S           (B, H, Dk, Dv) float32, 16-byte aligned, read and overwritten.
+ *   Dk a multiple of 8 up to H3_DELTA_MAX_DK, Dv one up to H3_DELTA_MAX_DV;
+ *   Hk divides H.  Outputs overlap nothing.  Arithmetic in float32.
+ * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype), EDEVICE.
+ */
+int h3_delta_step(const void *q, const void *k, const void *v, const float *g, const float *beta, float scale, int B,
+                  int T, int H, int Hk, int Dk, int Dv, int dtype, float *S, void *o, void *stream);
+
+/*
  * h3_workspace_size — bytes of workspace an operation needs (0 if the
- * arguments are invalid).  H_or_d is H for the convolutions, d for the layer;
+ * arguments are invalid).  H_or_d is H for the convolutions, d for the layer
+ * and the norm, whose B is its number of rows;
  * m is the mode count (state passing) or the shift length (layer); chunk is
  * the chunk length (state passing) or the head dimension (H3_OP_LAYER_HEADS).
  */

@@ -21,7 +21,8 @@ import torch
 __all__ = [
     "H3Error", "lib", "ssm_discretize", "ssm_kernel", "fftconv", "statepass_conv",
     "statepass_conv_noalloc", "layer_fwd", "layer_fwd_heads", "ssm_step", "fftconv_bwd", "kernel_spectrum", "fftconv_spectral", "workspace_size", "status_string", "F32", "F16", "BF16",
-    "OP_FFTCONV", "OP_STATEPASS", "OP_LAYER", "OP_FFTCONV_BWD", "OP_LAYER_HEADS", "FUSED_LIMIT", "FUSED_LIMIT_F32", "MAX_MODES",
+    "layernorm", "layernorm_bwd", "delta_step",
+    "OP_FFTCONV", "OP_STATEPASS", "OP_LAYER", "OP_FFTCONV_BWD", "OP_LAYER_HEADS", "OP_LAYERNORM_BWD", "FUSED_LIMIT", "FUSED_LIMIT_F32", "MAX_MODES",
 ]
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -29,6 +30,7 @@ LIB_PATH = os.path.join(HERE, "libh3flash.so")
 
 F32, F16, BF16 = 0, 1, 2
 OP_FFTCONV, OP_STATEPASS, OP_LAYER, OP_FFTCONV_BWD, OP_LAYER_HEADS = 1, 2, 3, 4, 5
+OP_LAYERNORM_BWD, OP_DELTA, OP_DELTA_SAVED, OP_DELTA_BWD = 6, 7, 8, 9
 FUSED_LIMIT = 16384       # 16-bit I/O
 FUSED_LIMIT_F32 = 8192    # float32 I/O, spectral entry points, kernel gradient
 MAX_MODES = 64
@@ -65,13 +67,17 @@ def lib() -> ctypes.CDLL:
         L.h3_ssm_step.argtypes = [vp, vp, vp, vp, vp, i, i, i, i, i, vp, vp, vp]
         L.h3_fftconv_bwd.argtypes = [vp, vp, vp, vp, i, i, i, i, vp, vp, vp, vp, sz, vp]
         L.h3_layer_fwd_heads.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, i, vp, vp, sz, vp]
+        fl = ctypes.c_float
+        L.h3_layernorm.argtypes = [vp, vp, vp, i, i, fl, i, vp, vp, vp, vp]
+        L.h3_layernorm_bwd.argtypes = [vp, vp, vp, vp, vp, i, i, i, vp, vp, vp, vp, sz, vp]
+        L.h3_delta_step.argtypes = [vp, vp, vp, vp, vp, fl, i, i, i, i, i, i, i, vp, vp, vp]
         L.h3_workspace_size.argtypes = [i, i, i, i, i, i, i]
         L.h3_workspace_size.restype = sz
         L.h3_status_string.argtypes = [i]
         L.h3_status_string.restype = ctypes.c_char_p
         for fn in ("h3_ssm_discretize", "h3_ssm_kernel", "h3_fftconv", "h3_statepass_conv", "h3_statepass_conv_noalloc",
                    "h3_layer_fwd", "h3_kernel_spectrum", "h3_fftconv_spectral", "h3_ssm_step", "h3_fftconv_bwd",
-                   "h3_layer_fwd_heads"):
+                   "h3_layer_fwd_heads", "h3_layernorm", "h3_layernorm_bwd", "h3_delta_step"):
             getattr(L, fn).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -192,6 +198,23 @@ def _out(name: str, t: Optional[torch.Tensor], shape, dtype, dev):
         raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+
+
+class _Here:
+    def __enter__(self):
+        return None
+
+    def __exit__(self, *a):
+        return False
+
+
+_HERE = _Here()
+
+
+def _device(dev: torch.device):
+    """A context in which `dev` is current: kernels are launched on the current
+    device, whatever device their stream belongs to."""
+    return _HERE if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
 
 
 # ----------------------------------------------------------------- ops -----
@@ -454,4 +477,90 @@ def layer_fwd(x: torch.Tensor, Wq: torch.Tensor, Wk: torch.Tensor, Wv: torch.Ten
         _ptr(x), *[_ptr(w) for w in Ws], _ptr(shift_C), _ptr(shift_D), _ptr(diag_k),
         _ptr(diag_D), Bn, L, d, m_s, dt, _ptr(o), _ptr(ws), ws.numel() * ws.element_size(),
         _stream(x.device)))
+    return o
+
+
+def layernorm(x: torch.Tensor, w: Optional[torch.Tensor] = None, b: Optional[torch.Tensor] = None, eps: float = 1e-5,
+              out: Optional[torch.Tensor] = None):
+    """Layer norm over the last dimension of ``x`` (..., d), with weight ``w``
+    and bias ``b`` (d).  Returns (y, mean, rstd), mean and rstd float32 of x's
+    leading shape, which layernorm_bwd takes."""
+    dev = _gpu("x", x)
+    x = x.contiguous()
+    if x.dim() < 1:
+        raise ValueError("x must be (..., d)")
+    d = x.shape[-1]
+    w, b = _f32(w), _f32(b)
+    dt = _dtype(x)
+    _on(dev, w=w, b=b)
+    _shape("w", w, (d,)); _shape("b", b, (d,))
+    _out("out", out, x.shape, x.dtype, dev)
+    y = out if out is not None else torch.empty_like(x)
+    stats = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=dev)
+    mean, rstd = stats[0], stats[1]
+    with _device(dev):
+        _check("h3_layernorm", lib().h3_layernorm(
+            _ptr(x), _ptr(w), _ptr(b), x.numel() // d if d else 0, d, eps, dt, _ptr(y), _ptr(mean), _ptr(rstd),
+            _stream(dev)))
+    return y, mean, rstd
+
+
+def layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, w: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
+                  want_dx: bool = True, want_dw: bool = True, want_db: bool = True,
+                  workspace: Optional[torch.Tensor] = None):
+    """Backward pass of layernorm for the output gradient ``dy``, given the mean
+    and rstd that it returned.  Returns (dx, dw, db); one not asked for is None."""
+    dev = _gpu("dy", dy)
+    _on(dev, x=x, w=w, mean=mean, rstd=rstd)
+    dy, x = dy.contiguous(), x.contiguous()
+    if dy.dim() < 1:
+        raise ValueError("dy must be (..., d)")
+    if x.shape != dy.shape or x.dtype != dy.dtype:
+        raise ValueError("x must match dy in shape and dtype")
+    d = dy.shape[-1]
+    rows = dy.numel() // d if d else 0
+    dt = _dtype(dy)
+    w, mean, rstd = _f32(w), _f32(mean), _f32(rstd)
+    _shape("w", w, (d,)); _shape("mean", mean, dy.shape[:-1]); _shape("rstd", rstd, dy.shape[:-1])
+    dx = torch.empty_like(dy) if want_dx else None
+    dw = torch.empty((d,), dtype=torch.float32, device=dev) if want_dw else None
+    db = torch.empty((d,), dtype=torch.float32, device=dev) if want_db else None
+    ws = _workspace(_ws_size(OP_LAYERNORM_BWD, rows, d, 1, 0, 0, dt), dev, workspace)
+    with _device(dev):
+        _check("h3_layernorm_bwd", lib().h3_layernorm_bwd(
+            _ptr(dy), _ptr(x), _ptr(w), _ptr(mean), _ptr(rstd), rows, d, dt, _ptr(dx), _ptr(dw), _ptr(db), _ptr(ws),
+            ws.numel() * ws.element_size(), _stream(dev)))
+    return dx, dw, db
+
+
+def _delta_args(q, k, v, g, beta):
+    """Checked (q, k, v, g, beta), contiguous, gates in float32, and their sizes."""
+    dev = _gpu("q", q)
+    _on(dev, k=k, v=v, g=g, beta=beta)
+    if q.dim() != 4 or v.dim() != 4:
+        raise ValueError("q must be (B, L, Hk, Dk) and v (B, L, H, Dv)")
+    Bn, L, Hk, Dk = q.shape
+    H, Dv = v.shape[2], v.shape[3]
+    dt = _dtype(q)
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("q, k and v must have the same dtype")
+    _shape("k", k, (Bn, L, Hk, Dk)); _shape("v", v, (Bn, L, H, Dv))
+    _shape("g", g, (Bn, L, H)); _shape("beta", beta, (Bn, L, H))
+    return dev, q.contiguous(), k.contiguous(), v.contiguous(), _f32(g), _f32(beta), (Bn, L, H, Hk, Dk, Dv, dt)
+
+
+def delta_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, g: torch.Tensor, beta: torch.Tensor, S: torch.Tensor,
+               scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gated delta rule, recurrent: advance the state ``S`` (B, H, Dk, Dv)
+    float32, in place, over the tokens q, k (B, T, Hk, Dk), v (B, T, H, Dv),
+    log decays g and write strengths beta (B, T, H); returns o shaped like v.
+    ``scale`` is Dk^-1/2 unless given."""
+    dev, q, k, v, g, beta, (Bn, T, H, Hk, Dk, Dv, dt) = _delta_args(q, k, v, g, beta)
+    _out("S", S, (Bn, H, Dk, Dv), torch.float32, dev)
+    _out("out", out, v.shape, v.dtype, dev)
+    o = out if out is not None else torch.empty_like(v)
+    with _device(dev):
+        _check("h3_delta_step", lib().h3_delta_step(
+            _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), Dk ** -0.5 if scale is None else scale, Bn, T, H, Hk, Dk, Dv,
+            dt, _ptr(S), _ptr(o), _stream(dev)))
     return o

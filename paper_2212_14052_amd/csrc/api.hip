@@ -32,6 +32,22 @@ bool overlap(const void *p, size_t n, const void *q, size_t m) {
 
 int launched(hipError_t e) { return e == hipSuccess ? H3_OK : H3_EDEVICE; }
 
+// key and value sizes of the delta rule
+bool delta_sizes_ok(int Dk, int Dv) {
+    return Dk >= 8 && Dk % 8 == 0 && Dk <= H3_DELTA_MAX_DK && Dv >= 8 && Dv % 8 == 0 && Dv <= H3_DELTA_MAX_DV;
+}
+// bytes of its tensors: q or k, v or o, g or beta, a state for each head
+struct DeltaBytes {
+    size_t qk, v, gate, state;
+    DeltaBytes(int B, int L, int H, int Hk, int Dk, int Dv, int dtype) {
+        const size_t tok = (size_t)B * L, es = esize(dtype);
+        qk = tok * Hk * Dk * es;
+        v = tok * H * Dv * es;
+        gate = tok * H * 4;
+        state = (size_t)B * H * Dk * Dv * 4;
+    }
+};
+
 // fused length / chunk: a power of two in [H3_MIN_LEN, H3_FUSED_LIMIT]; above
 // H3_FUSED_LIMIT_F32 only where the matrix-core kernels take it (16-bit I/O)
 bool fused_len_ok(int L, int dtype) {
@@ -237,6 +253,8 @@ size_t h3_workspace_size(int op, int B, int H, int L, int m, int chunk, int dtyp
             if (chunk == 1) return layer_ws(B, H, L).total;
             if (chunk != 2 && chunk != 4 && chunk != 8) return 0;
             return heads_ws(B, H, L, chunk).total;
+        case H3_OP_LAYERNORM_BWD:   // B = rows, H = d
+            return align_up(layernorm_bwd_workspace(B, H));
         case H3_OP_FFTCONV_BWD: {
             // the spectrum of the du pass; at L = 2048 (16-bit) also room for
             // kernel-gradient partial sums per eight rows, which no kernel
@@ -535,6 +553,70 @@ int h3_layer_fwd_heads(const void *x, const void *Wq, const void *Wk, const void
     // O_t[j] = sum_i Q_t[i] S_t[i][j], token-major; out = O Wo
     if ((e = launch_heads_contract(d_head, q, g, o_tm, B, d, L, dtype, s)) != hipSuccess) return H3_EDEVICE;
     return launched(layer_out(o_tm, Wo, out, B, L, d, dtype, wt, s));
+}
+
+int h3_layernorm(const void *x, const float *w, const float *b, int rows, int d, float eps, int dtype, void *y,
+                 float *mean, float *rstd, void *stream) {
+    if (!x || !y || rows < 1 || d < 1 || !(eps >= 0.f)) return H3_EINVAL;
+    if (!dtype_ok(dtype)) return H3_EUNSUPPORTED;
+    const size_t io = (size_t)rows * d * esize(dtype), ps = (size_t)d * 4, rs = (size_t)rows * 4;
+    const uintptr_t ea = esize(dtype) - 1;
+    if (((uintptr_t)x & ea) || ((uintptr_t)y & ea) || ((uintptr_t)w & 3) || ((uintptr_t)b & 3) || ((uintptr_t)mean & 3) ||
+        ((uintptr_t)rstd & 3))
+        return H3_EINVAL;
+    if ((y != x && overlap(y, io, x, io)) || overlap(mean, rs, rstd, rs)) return H3_EINVAL;
+    const void *outs[3] = {y, mean, rstd};
+    const size_t osz[3] = {io, rs, rs};
+    for (int i = 0; i < 3; ++i)
+        if (overlap(outs[i], osz[i], w, ps) || overlap(outs[i], osz[i], b, ps) ||
+            (i && (overlap(outs[i], osz[i], x, io) || overlap(outs[i], osz[i], y, io))))
+            return H3_EINVAL;
+    return launched(launch_layernorm(x, w, b, rows, d, eps, dtype, y, mean, rstd, (hipStream_t)stream));
+}
+
+int h3_layernorm_bwd(const void *dy, const void *x, const float *w, const float *mean, const float *rstd, int rows,
+                     int d, int dtype, void *dx, float *dw, float *db, void *workspace, size_t ws_bytes, void *stream) {
+    if (!dy || !x || !mean || !rstd || rows < 1 || d < 1 || (!dx && !dw && !db)) return H3_EINVAL;
+    if (!dtype_ok(dtype)) return H3_EUNSUPPORTED;
+    const size_t need = h3_workspace_size(H3_OP_LAYERNORM_BWD, rows, d, 1, 0, 0, dtype);
+    if (!workspace || ws_bytes < need) return H3_EWORKSPACE;
+    const size_t io = (size_t)rows * d * esize(dtype), ps = (size_t)d * 4, rs = (size_t)rows * 4;
+    const uintptr_t ea = esize(dtype) - 1;
+    if (((uintptr_t)dy & ea) || ((uintptr_t)x & ea) || ((uintptr_t)dx & ea) || ((uintptr_t)w & 3) ||
+        ((uintptr_t)mean & 3) || ((uintptr_t)rstd & 3) || ((uintptr_t)dw & 3) || ((uintptr_t)db & 3) ||
+        !aligned16(workspace))
+        return H3_EINVAL;
+    const void *ins[5] = {dy, x, w, mean, rstd};
+    const size_t isz[5] = {io, io, ps, rs, rs};
+    const void *outs[4] = {dx, dw, db, workspace};
+    const size_t osz[4] = {io, ps, ps, need};
+    const bool in_place = dx && !dw && !db && (dx == dy || dx == x);
+    for (int i = 0; i < 4; ++i) {
+        for (int j = 0; j < 5; ++j)
+            if (overlap(outs[i], osz[i], ins[j], isz[j]) && !(i == 0 && in_place && ins[j] == dx)) return H3_EINVAL;
+        for (int j = i + 1; j < 4; ++j)
+            if (overlap(outs[i], osz[i], outs[j], osz[j])) return H3_EINVAL;
+    }
+    return launched(launch_layernorm_bwd(dy, x, w, mean, rstd, rows, d, dtype, dx, dw, db, (float *)workspace,
+                                         (hipStream_t)stream));
+}
+
+int h3_delta_step(const void *q, const void *k, const void *v, const float *g, const float *beta, float scale, int B,
+                  int T, int H, int Hk, int Dk, int Dv, int dtype, float *S, void *o, void *stream) {
+    if (!q || !k || !v || !g || !beta || !S || !o || B < 1 || T < 1 || H < 1 || Hk < 1 || Dk < 1 || Dv < 1 || H % Hk)
+        return H3_EINVAL;
+    if (!dtype_ok(dtype) || !delta_sizes_ok(Dk, Dv)) return H3_EUNSUPPORTED;
+    const DeltaBytes n(B, T, H, Hk, Dk, Dv, dtype);
+    const uintptr_t ea = esize(dtype) - 1;
+    if (((uintptr_t)q & ea) || ((uintptr_t)k & ea) || ((uintptr_t)v & ea) || ((uintptr_t)o & ea) || ((uintptr_t)g & 3) ||
+        ((uintptr_t)beta & 3) || !aligned16(S))
+        return H3_EINVAL;
+    const void *ins[5] = {q, k, v, g, beta};
+    const size_t isz[5] = {n.qk, n.qk, n.v, n.gate, n.gate};
+    for (int j = 0; j < 5; ++j)
+        if (overlap(S, n.state, ins[j], isz[j]) || overlap(o, n.v, ins[j], isz[j])) return H3_EINVAL;
+    if (overlap(S, n.state, o, n.v)) return H3_EINVAL;
+    return launched(launch_delta_step(q, k, v, g, beta, scale, B, T, H, Hk, Dk, Dv, dtype, S, o, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -158,4 +158,17 @@ hipError_t launch_layer_mid(const void *q, const void *k, const void *v, const f
                             const float *diag_D, int B, int d, int L, int dtype, void *o,
                             hipStream_t s);
 
+// Layer norm over rows of d; the backward pass's workspace holds partial sums
+// of dw and db.  w, b, mean, rstd, dx, dw, db as in the C ABI (null allowed there).
+hipError_t launch_layernorm(const void *x, const float *w, const float *b, int rows, int d, float eps, int dtype, void *y,
+                            float *mean, float *rstd, hipStream_t s);
+size_t layernorm_bwd_workspace(int rows, int d);
+hipError_t launch_layernorm_bwd(const void *dy, const void *x, const float *w, const float *mean, const float *rstd,
+                                int rows, int d, int dtype, void *dx, float *dw, float *db, float *ws, hipStream_t s);
+
+// The gated delta rule for T tokens of each (b, h) from the state S (B, H, Dk,
+// Dv), updated in place.
+hipError_t launch_delta_step(const void *q, const void *k, const void *v, const float *g, const float *beta, float scale,
+                             int B, int T, int H, int Hk, int Dk, int Dv, int dtype, float *S, void *o, hipStream_t s);
+
 }  // namespace h3

@@ -1,0 +1,92 @@
+"""Refusals of the layer norm and the delta rule: C ABI and binding, before
+anything is launched (no GPU needed)."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2212_14052_amd as h3
+
+OK, EINVAL, EUNSUP, EWS = 0, -1, -2, -3
+P = lambda v: ctypes.c_void_p(v)
+Q, K, V, G, BE, S, O, W, X, Y = (0x10000000 * i for i in range(1, 11))   # fake, aligned, far apart
+
+
+def norm(x=X, w=K, b=K + 65536, rows=4, d=64, eps=1e-5, dt=2, y=Y, mean=G, rstd=BE):
+    return h3.lib().h3_layernorm(P(x), P(w), P(b), rows, d, eps, dt, P(y), P(mean), P(rstd), None)
+
+
+def test_layernorm_refusals():
+    assert norm(x=0) == EINVAL
+    assert norm(y=0) == EINVAL
+    assert norm(rows=0) == EINVAL
+    assert norm(d=0) == EINVAL
+    assert norm(eps=-1.0) == EINVAL
+    assert norm(eps=float("nan")) == EINVAL
+    assert norm(dt=3) == EUNSUP
+    assert norm(x=X + 1) == EINVAL                  # not aligned to its element
+    assert norm(dt=0, y=Y + 2) == EINVAL
+    assert norm(w=K + 2) == EINVAL
+    assert norm(y=X + 64) == EINVAL                 # partly over x
+    assert norm(mean=X + 16) == EINVAL              # inside x
+    assert norm(rstd=Y) == EINVAL                   # inside y
+    assert norm(rstd=G) == EINVAL                   # mean's buffer
+    assert norm(w=Y + 128) == EINVAL                # y over the weight
+
+
+def norm_bwd(dy=V, x=X, w=K, mean=G, rstd=BE, rows=4, d=64, dt=2, dx=Y, dw=S, db=S + 65536, ws=W, wsb=1 << 20):
+    return h3.lib().h3_layernorm_bwd(P(dy), P(x), P(w), P(mean), P(rstd), rows, d, dt, P(dx), P(dw), P(db), P(ws), wsb, None)
+
+
+def test_layernorm_bwd_refusals():
+    for name in ("dy", "x", "mean", "rstd"):
+        assert norm_bwd(**{name: 0}) == EINVAL
+    assert norm_bwd(rows=0) == EINVAL
+    assert norm_bwd(dx=0, dw=0, db=0) == EINVAL     # nothing asked
+    assert norm_bwd(dt=9) == EUNSUP
+    assert norm_bwd(ws=0) == EWS
+    assert norm_bwd(wsb=h3.workspace_size(h3.OP_LAYERNORM_BWD, 4, 64, 1, 0, 0, 2) - 1) == EWS
+    assert norm_bwd(ws=W + 8) == EINVAL
+    assert norm_bwd(dx=V) == EINVAL                 # in place, but dw and db are still summed from dy
+    assert norm_bwd(dw=K) == EINVAL                 # dw over w
+    assert norm_bwd(db=S) == EINVAL                 # db over dw
+    assert norm_bwd(ws=X) == EINVAL
+    assert norm_bwd(dw=S + 1) == EINVAL
+    assert h3.workspace_size(h3.OP_LAYERNORM_BWD, 16384, 768, 1, 0, 0, h3.F16) >= 256 * 2 * 768 * 4
+    assert h3.workspace_size(h3.OP_LAYERNORM_BWD, 0, 768, 1, 0, 0, h3.F16) == 0
+
+
+def step(q=Q, k=K, v=V, g=G, beta=BE, scale=0.1, B=2, T=1, H=4, Hk=2, Dk=64, Dv=64, dt=2, S=S, o=O):
+    return h3.lib().h3_delta_step(P(q), P(k), P(v), P(g), P(beta), scale, B, T, H, Hk, Dk, Dv, dt, P(S), P(o), None)
+
+
+def test_delta_step_refusals():
+    for name in ("q", "k", "v", "g", "beta", "S", "o"):
+        assert step(**{name: 0}) == EINVAL
+    for name in ("B", "T", "H", "Hk", "Dk", "Dv"):
+        assert step(**{name: 0}) == EINVAL
+    assert step(Hk=3) == EINVAL                     # heads not shared evenly
+    assert step(Dk=12) == EUNSUP
+    assert step(Dk=136) == EUNSUP
+    assert step(Dv=20) == EUNSUP
+    assert step(Dv=264) == EUNSUP
+    assert step(dt=5) == EUNSUP
+    assert step(S=S + 8) == EINVAL                  # state not 16-byte aligned
+    assert step(q=Q + 1) == EINVAL
+    assert step(g=G + 2) == EINVAL
+    assert step(o=V) == EINVAL                      # output over v
+    assert step(o=S + 256) == EINVAL                # output inside the state
+    assert step(S=K) == EINVAL
+
+
+def test_binding_refusals():
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError):
+        h3.layernorm(x)
+    with pytest.raises(TypeError):
+        h3.layernorm([1.0])
+    with pytest.raises(ValueError):
+        h3.layernorm_bwd(x, x, None, x[:, 0], x[:, 0])
+    q, v, g = torch.zeros(1, 1, 2, 8), torch.zeros(1, 1, 2, 8), torch.zeros(1, 1, 2)
+    with pytest.raises(ValueError):
+        h3.delta_step(q, q, v, g, g, torch.zeros(1, 2, 8, 8))
