@@ -317,11 +317,37 @@ int h3_delta_step(const void *q, const void *k, const void *v, const float *g, c
                   int T, int H, int Hk, int Dk, int Dv, int dtype, float *S, void *o, void *stream);
 
 /*
+ * h3_delta_rule — the gated delta rule (see h3_delta_step) over whole
+ * sequences, chunk by chunk on the matrix cores: the same outputs and final
+ * state as the recurrence.
+ *   q, k        (B, L, Hk, Dk), v, o (B, L, H, Dv) of `dtype`, 16-byte aligned.
+ *   g, beta     (B, L, H) float32.
+ *   S0          (B, H, Dk, Dv) float32, or NULL for the zero state.
+ *   lengths     (B) int32 on the device, or NULL: tokens from lengths[b] on are
+ *               not read, their outputs are 0 and the final state is the one before
+ *               them (values outside 0 .. L are taken as 0 or L).
+ *   S_final     (B, H, Dk, Dv) float32, or NULL; may be the buffer of S0.
+ *   saved       NULL, or >= h3_workspace_size(H3_OP_DELTA_SAVED, B, H, L, Dk,
+ *               Dv, dtype) bytes in which h3_delta_rule_bwd finds the chunks'
+ *               states and solved matrices.
+ *   workspace   >= h3_workspace_size(H3_OP_DELTA, B, H, L, Dk, Dv, dtype).
+ *   Dk, Dv, Hk as for h3_delta_step; any L >= 1.  Other than S_final and S0
+ *   nothing that is written overlaps anything.
+ * States, gates and sums are float32, differences of summed log decays
+ * float64; a NaN or Inf may reach every token of its chunk of 64.
+ * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, 2^31 chunks), EWORKSPACE, EDEVICE.
+ */
+int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, const float *beta, const float *S0,
+                  const int *lengths, float scale, int B, int L, int H, int Hk, int Dk, int Dv, int dtype, void *o,
+                  float *S_final, void *saved, size_t saved_bytes, void *workspace, size_t ws_bytes, void *stream);
+
+/*
  * h3_workspace_size — bytes of workspace an operation needs (0 if the
  * arguments are invalid).  H_or_d is H for the convolutions, d for the layer
  * and the norm, whose B is its number of rows;
  * m is the mode count (state passing) or the shift length (layer); chunk is
  * the chunk length (state passing) or the head dimension (H3_OP_LAYER_HEADS).
+ * The delta rule's operations take Dk as m and Dv as chunk.
  */
 size_t h3_workspace_size(int op, int B, int H_or_d, int L, int m, int chunk, int dtype);
 

@@ -21,8 +21,8 @@ import torch
 __all__ = [
     "H3Error", "lib", "ssm_discretize", "ssm_kernel", "fftconv", "statepass_conv",
     "statepass_conv_noalloc", "layer_fwd", "layer_fwd_heads", "ssm_step", "fftconv_bwd", "kernel_spectrum", "fftconv_spectral", "workspace_size", "status_string", "F32", "F16", "BF16",
-    "layernorm", "layernorm_bwd", "delta_step",
-    "OP_FFTCONV", "OP_STATEPASS", "OP_LAYER", "OP_FFTCONV_BWD", "OP_LAYER_HEADS", "OP_LAYERNORM_BWD", "FUSED_LIMIT", "FUSED_LIMIT_F32", "MAX_MODES",
+    "layernorm", "layernorm_bwd", "delta_rule", "delta_step",
+    "OP_FFTCONV", "OP_STATEPASS", "OP_LAYER", "OP_FFTCONV_BWD", "OP_LAYER_HEADS", "OP_LAYERNORM_BWD", "OP_DELTA", "OP_DELTA_SAVED", "FUSED_LIMIT", "FUSED_LIMIT_F32", "MAX_MODES",
 ]
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -71,13 +71,15 @@ def lib() -> ctypes.CDLL:
         L.h3_layernorm.argtypes = [vp, vp, vp, i, i, fl, i, vp, vp, vp, vp]
         L.h3_layernorm_bwd.argtypes = [vp, vp, vp, vp, vp, i, i, i, vp, vp, vp, vp, sz, vp]
         L.h3_delta_step.argtypes = [vp, vp, vp, vp, vp, fl, i, i, i, i, i, i, i, vp, vp, vp]
+        L.h3_delta_rule.argtypes = [vp] * 7 + [fl] + [i] * 7 + [vp, vp, vp, sz, vp, sz, vp]
         L.h3_workspace_size.argtypes = [i, i, i, i, i, i, i]
         L.h3_workspace_size.restype = sz
         L.h3_status_string.argtypes = [i]
         L.h3_status_string.restype = ctypes.c_char_p
         for fn in ("h3_ssm_discretize", "h3_ssm_kernel", "h3_fftconv", "h3_statepass_conv", "h3_statepass_conv_noalloc",
                    "h3_layer_fwd", "h3_kernel_spectrum", "h3_fftconv_spectral", "h3_ssm_step", "h3_fftconv_bwd",
-                   "h3_layer_fwd_heads", "h3_layernorm", "h3_layernorm_bwd", "h3_delta_step"):
+                   "h3_layer_fwd_heads", "h3_layernorm", "h3_layernorm_bwd", "h3_delta_step",
+                   "h3_delta_rule"):
             getattr(L, fn).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -564,3 +566,45 @@ def delta_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, g: torch.Tenso
             _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), Dk ** -0.5 if scale is None else scale, Bn, T, H, Hk, Dk, Dv,
             dt, _ptr(S), _ptr(o), _stream(dev)))
     return o
+
+
+def _lengths(lengths: Optional[torch.Tensor], Bn: int, dev: torch.device) -> Optional[torch.Tensor]:
+    if lengths is None:
+        return None
+    _on(dev, lengths=lengths)
+    _shape("lengths", lengths, (Bn,))
+    if lengths.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"lengths must be int32 or int64 (got {lengths.dtype})")
+    return lengths.to(torch.int32).contiguous()
+
+
+def _aligned(t: torch.Tensor) -> torch.Tensor:
+    """t, copied if it does not start on 16 bytes (a view into another tensor)."""
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
+def delta_rule(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, g: torch.Tensor, beta: torch.Tensor,
+               S0: Optional[torch.Tensor] = None, scale: Optional[float] = None, lengths: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None, save: bool = False, workspace: Optional[torch.Tensor] = None):
+    """The gated delta rule over whole sequences (the recurrence of delta_step,
+    chunk by chunk): q, k (B, L, Hk, Dk), v (B, L, H, Dv), g, beta (B, L, H), from
+    the state S0 (B, H, Dk, Dv) or zero; tokens from lengths[b] on are left out.
+    Returns (o, S_final), and with ``save`` also the buffer for delta_rule_bwd."""
+    dev, q, k, v, g, beta, (Bn, L, H, Hk, Dk, Dv, dt) = _delta_args(q, k, v, g, beta)
+    _on(dev, S0=S0)
+    S0 = _f32(S0)
+    _shape("S0", S0, (Bn, H, Dk, Dv))
+    lengths = _lengths(lengths, Bn, dev)
+    _out("out", out, v.shape, v.dtype, dev)
+    q, k, v = _aligned(q), _aligned(k), _aligned(v)
+    o = out if out is not None else torch.empty_like(v)
+    S = torch.empty((Bn, H, Dk, Dv), dtype=torch.float32, device=dev)
+    ws = _workspace(_ws_size(OP_DELTA, Bn, H, L, Dk, Dv, dt), dev, workspace)
+    n = _ws_size(OP_DELTA_SAVED, Bn, H, L, Dk, Dv, dt) if save else 0
+    saved = torch.empty(max(n, 256), dtype=torch.uint8, device=dev) if save else None
+    with _device(dev):
+        _check("h3_delta_rule", lib().h3_delta_rule(
+            _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(S0), _ptr(lengths), Dk ** -0.5 if scale is None else scale,
+            Bn, L, H, Hk, Dk, Dv, dt, _ptr(o), _ptr(S), _ptr(saved), n, _ptr(ws), ws.numel() * ws.element_size(),
+            _stream(dev)))
+    return (o, S, saved) if save else (o, S)

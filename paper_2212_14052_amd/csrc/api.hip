@@ -36,6 +36,10 @@ int launched(hipError_t e) { return e == hipSuccess ? H3_OK : H3_EDEVICE; }
 bool delta_sizes_ok(int Dk, int Dv) {
     return Dk >= 8 && Dk % 8 == 0 && Dk <= H3_DELTA_MAX_DK && Dv >= 8 && Dv % 8 == 0 && Dv <= H3_DELTA_MAX_DV;
 }
+// its launches hold one workgroup a chunk: at most 2^31 - 1
+bool delta_chunks_ok(int B, int L, int H, int Dv) {
+    return (double)B * H * ((L + kDeltaChunk - 1) / kDeltaChunk) < 2147483647.0 && (double)B * H * ((Dv + 15) / 16) < 2147483647.0;
+}
 // bytes of its tensors: q or k, v or o, g or beta, a state for each head
 struct DeltaBytes {
     size_t qk, v, gate, state;
@@ -45,6 +49,28 @@ struct DeltaBytes {
         v = tok * H * Dv * es;
         gate = tok * H * 4;
         state = (size_t)B * H * Dk * Dv * 4;
+    }
+};
+
+// Buffers of the delta rule's chunks (each region 256-byte aligned): what the
+// forward pass needs by itself (X, P, the gates where nothing is kept), what
+// it leaves for the backward pass (the gates, both transposes, the errors and the
+// chunks' first states).
+struct DeltaWs {
+    size_t x, p, gates, xt, pt, es, states, fwd, saved;
+    DeltaWs(int B, int H, int L, int Dk, int Dv, int dtype) {
+        const size_t ch = (size_t)B * H * ((L + kDeltaChunk - 1) / kDeltaChunk);
+        const size_t mat = align_up(ch * (dtype == H3_F32 ? 3 : 2) * kDeltaChunk * kDeltaChunk * 2);
+        const size_t gb = align_up(ch * sizeof(ChunkGates));
+        x = 0;
+        p = mat;
+        gates = 2 * mat;   // of the workspace, and at 0 of what is kept
+        fwd = gates + gb;
+        xt = gb;
+        pt = xt + mat;
+        es = pt + mat;
+        states = es + align_up(ch * kDeltaChunk * Dv * 4);
+        saved = states + align_up(ch * Dk * Dv * 4);
     }
 };
 
@@ -253,6 +279,10 @@ size_t h3_workspace_size(int op, int B, int H, int L, int m, int chunk, int dtyp
             if (chunk == 1) return layer_ws(B, H, L).total;
             if (chunk != 2 && chunk != 4 && chunk != 8) return 0;
             return heads_ws(B, H, L, chunk).total;
+        case H3_OP_DELTA:   // m = Dk, chunk = Dv
+            return delta_sizes_ok(m, chunk) ? DeltaWs(B, H, L, m, chunk, dtype).fwd : 0;
+        case H3_OP_DELTA_SAVED:
+            return delta_sizes_ok(m, chunk) ? DeltaWs(B, H, L, m, chunk, dtype).saved : 0;
         case H3_OP_LAYERNORM_BWD:   // B = rows, H = d
             return align_up(layernorm_bwd_workspace(B, H));
         case H3_OP_FFTCONV_BWD: {
@@ -617,6 +647,44 @@ int h3_delta_step(const void *q, const void *k, const void *v, const float *g, c
         if (overlap(S, n.state, ins[j], isz[j]) || overlap(o, n.v, ins[j], isz[j])) return H3_EINVAL;
     if (overlap(S, n.state, o, n.v)) return H3_EINVAL;
     return launched(launch_delta_step(q, k, v, g, beta, scale, B, T, H, Hk, Dk, Dv, dtype, S, o, (hipStream_t)stream));
+}
+
+int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, const float *beta, const float *S0,
+                  const int *lengths, float scale, int B, int L, int H, int Hk, int Dk, int Dv, int dtype, void *o,
+                  float *S_final, void *saved, size_t saved_bytes, void *workspace, size_t ws_bytes, void *stream) {
+    if (!q || !k || !v || !g || !beta || !o || B < 1 || L < 1 || H < 1 || Hk < 1 || Dk < 1 || Dv < 1 || H % Hk)
+        return H3_EINVAL;
+    if (!dtype_ok(dtype) || !delta_sizes_ok(Dk, Dv) || !delta_chunks_ok(B, L, H, Dv)) return H3_EUNSUPPORTED;
+    const DeltaWs w(B, H, L, Dk, Dv, dtype);
+    if (!workspace || ws_bytes < w.fwd || (saved && saved_bytes < w.saved)) return H3_EWORKSPACE;
+    const DeltaBytes n(B, L, H, Hk, Dk, Dv, dtype);
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || ((uintptr_t)g & 3) || ((uintptr_t)beta & 3) ||
+        ((uintptr_t)S0 & 3) || ((uintptr_t)S_final & 3) || ((uintptr_t)lengths & 3) || !aligned16(saved) ||
+        !aligned16(workspace))
+        return H3_EINVAL;
+    const void *ins[7] = {q, k, v, g, beta, S0, lengths};
+    const size_t isz[7] = {n.qk, n.qk, n.v, n.gate, n.gate, n.state, (size_t)B * 4};
+    const void *outs[4] = {o, S_final, saved, workspace};
+    const size_t osz[4] = {n.v, n.state, w.saved, w.fwd};
+    for (int i = 0; i < 4; ++i) {
+        for (int j = 0; j < 7; ++j)
+            if (overlap(outs[i], osz[i], ins[j], isz[j]) && !(i == 1 && j == 5 && S_final == S0)) return H3_EINVAL;
+        for (int j = i + 1; j < 4; ++j)
+            if (overlap(outs[i], osz[i], outs[j], osz[j])) return H3_EINVAL;
+    }
+    DeltaArgs a{q, k, v, g, beta, lengths, S0, scale, B, L, H, Hk, Dk, Dv, (L + kDeltaChunk - 1) / kDeltaChunk};
+    char *ws = (char *)workspace, *sv = (char *)saved;
+    DeltaBuffers d{};
+    d.X = (uint4 *)(ws + w.x);
+    d.P = (uint4 *)(ws + w.p);
+    d.gates = (ChunkGates *)(sv ? sv : ws + w.gates);
+    if (sv) {
+        d.XT = (uint4 *)(sv + w.xt);
+        d.PT = (uint4 *)(sv + w.pt);
+        d.es = (float *)(sv + w.es);
+        d.states = (float *)(sv + w.states);
+    }
+    return launched(launch_delta_rule(a, dtype, d, o, S_final, (hipStream_t)stream));
 }
 
 }  // extern "C"

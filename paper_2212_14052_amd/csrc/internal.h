@@ -171,4 +171,30 @@ hipError_t launch_layernorm_bwd(const void *dy, const void *x, const float *w, c
 hipError_t launch_delta_step(const void *q, const void *k, const void *v, const float *g, const float *beta, float scale,
                              int B, int T, int H, int Hk, int Dk, int Dv, int dtype, float *S, void *o, hipStream_t s);
 
+// The gated delta rule over whole sequences, chunks of 64 tokens.
+constexpr int kDeltaChunk = 64;
+struct DeltaArgs {
+    const void *q, *k, *v;
+    const float *g, *beta;
+    const int *lengths;   // (B) or null
+    const float *S0;      // or null
+    float scale;
+    int B, L, H, Hk, Dk, Dv, N;   // N: chunks of a sequence
+};
+// What a chunk keeps beside its matrices: exp(G_i) from the chunk's start,
+// exp(G_63 - G_i) to its end, beta_i (0 behind the sequence's end).
+struct ChunkGates {
+    float from0[kDeltaChunk], toend[kDeltaChunk], beta[kDeltaChunk];
+};
+// Buffers of the chunks of every (b, h): operand fragments of X and P (64 x 64,
+// mat_pieces bf16 pieces), of their transposes, the gates, the errors e (64,
+// Dv) and the first states (Dk, Dv).  The forward pass writes XT, PT, es and
+// states where they are given (all or none).
+struct DeltaBuffers {
+    uint4 *X, *P, *XT, *PT;
+    ChunkGates *gates;
+    float *es, *states;
+};
+hipError_t launch_delta_rule(const DeltaArgs &a, int dtype, const DeltaBuffers &w, void *o, float *S_final, hipStream_t s);
+
 }  // namespace h3

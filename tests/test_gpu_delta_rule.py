@@ -1,0 +1,189 @@
+"""The gated delta rule over whole sequences against the recurrence in 64 bits.
+
+Tolerances.  Keys of unit length, beta in (0, 1) and decays at most 1 make each
+token's map of the state a contraction: what a chunk of 64 rounds away adds up
+over the chunks at most.  With M the largest state column's length plus the
+largest error e, a chunk's float32 sums are off by (Dk + 64) 2^-24 M.  Matrices
+and vectors of 16-bit inputs enter the solved product X (beta R) and the
+output's P u in two bf16 pieces each (2^-15 of the terms' sizes at most), float32
+inputs in three (2^-22): the terms' sizes are the row sums of |X| and |P|."""
+import pytest
+import torch
+
+import paper_2212_14052_amd as h3
+
+pytestmark = pytest.mark.gpu
+E32 = 2.0 ** -24
+DTYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def inputs(B, L, H, Hk, Dk, Dv, dtype, seed=0, alike=0.0):
+    gen = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(*s, generator=gen)
+    q, k = r(B, L, Hk, Dk), r(B, L, Hk, Dk)
+    k = k + alike * r(B, 1, Hk, Dk)   # a common part of all keys
+    q, k = q / q.norm(dim=-1, keepdim=True), k / k.norm(dim=-1, keepdim=True)
+    g = -torch.empty(B, L, H).uniform_(-7, 0, generator=gen).exp()
+    ts = [t.to(DTYPES[dtype]).cuda() for t in (q, k, r(B, L, H, Dv))]
+    return ts + [g.cuda(), torch.sigmoid(r(B, L, H)).cuda(), r(B, H, Dk, Dv).cuda()]
+
+
+def reference(q, k, v, g, beta, S0, scale, lengths=None):
+    """o, S, M and the largest row sums of |X beta| and |P| of any chunk."""
+    q, k, v, g, beta = (t.double() for t in (q, k, v, g, beta))
+    B, L, H, Dv = v.shape
+    per = H // q.shape[2]
+    q, k = q.repeat_interleave(per, 2), k.repeat_interleave(per, 2)
+    S = torch.zeros(B, H, q.shape[-1], Dv, dtype=torch.float64, device=v.device) if S0 is None else S0.double()
+    o, size = torch.zeros_like(v), S.norm(dim=2).amax()
+    for t in range(L):
+        Sn = S * g[:, t].exp()[..., None, None]
+        e = v[:, t] - (Sn * k[:, t, :, :, None]).sum(2)
+        Sn = Sn + k[:, t, :, :, None] * (beta[:, t, :, None] * e)[:, :, None, :]
+        if lengths is not None:
+            on = (t < lengths)[:, None, None, None]
+            Sn, e = torch.where(on, Sn, S), e.masked_fill(~on[..., 0], 0.0)
+            o[:, t] = torch.where(on[..., 0], scale * (Sn * q[:, t, :, :, None]).sum(2), 0.0)
+        else:
+            o[:, t] = scale * (Sn * q[:, t, :, :, None]).sum(2)
+        S = Sn
+        size = torch.maximum(size, S.norm(dim=2).amax() + e.abs().amax())
+    xs = ps = 0.0
+    for a in range(0, L, 64):
+        at = slice(a, a + 64)
+        kc, qc = k[:, at].transpose(1, 2), q[:, at].transpose(1, 2)
+        G = g[:, at].transpose(1, 2).cumsum(-1)
+        D = (G[..., :, None] - G[..., None, :]).tril().exp().tril().nan_to_num(0.0)
+        b = beta[:, at].transpose(1, 2)[..., None, :]
+        kt = kc.transpose(-1, -2).contiguous()
+        A = (torch.matmul(kc, kt) * D).tril(-1)
+        X = torch.linalg.solve_triangular(A * b + torch.eye(D.shape[-1], device=A.device, dtype=A.dtype), A, upper=False)
+        xs = max(xs, (X * b).abs().sum(-1).max().item())
+        ps = max(ps, (torch.matmul(qc, kt) * D).abs().sum(-1).max().item())
+    return o, S, size.item(), xs, ps
+
+
+def off_by(Dk, L, dtype, M, xs):
+    pieces = 2.0 ** -22 if dtype == "f32" else 2.0 ** -15
+    return -(-L // 64) * M * (pieces * xs + (Dk + 64) * E32 * (1 + xs)) * 1.1   # rounded keys: lengths to 1 + 2^-8
+
+
+def run_and_check(dtype, q, k, v, g, beta, S0, scale=None, lengths=None):
+    B, L, H, Dv = v.shape
+    Dk = q.shape[-1]
+    sc = Dk ** -0.5 if scale is None else scale
+    ro, rS, M, xs, ps = reference(q, k, v, g, beta, S0, sc, lengths)
+    off = off_by(Dk, L, dtype, M, xs)
+    o, S = h3.delta_rule(q, k, v, g, beta, S0=S0, scale=scale, lengths=lengths)
+    assert o.shape == v.shape and o.dtype == v.dtype and S.dtype == torch.float32
+    print("off S %.2e of %.2e" % ((S.double() - rS).abs().max().item(), off), end=" ")
+    assert (S.double() - rS).abs().max() <= off
+    pieces = 2.0 ** -22 if dtype == "f32" else 2.0 ** -15
+    tol = ro.abs() * torch.finfo(v.dtype).eps / 2 + abs(sc) * (1 + ps) * (off + (pieces + (Dk + 64) * E32) * M) + 2.0 ** -25
+    assert ((o.double() - ro).abs() <= tol).all()
+    return o, S
+
+
+SIZES = [(1, 1, 1, 1, 8, 8), (2, 63, 2, 2, 16, 16), (1, 64, 3, 1, 128, 128), (2, 65, 2, 1, 64, 64), (3, 200, 4, 2, 96, 40),
+         (1, 333, 2, 2, 32, 256), (2, 130, 2, 2, 120, 24), (1, 1100, 2, 1, 128, 72)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,L,H,Hk,Dk,Dv", SIZES)
+def test_delta_rule(B, L, H, Hk, Dk, Dv, dtype):
+    run_and_check(dtype, *inputs(B, L, H, Hk, Dk, Dv, dtype))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_no_first_state_and_scale(dtype):
+    *args, S0 = inputs(2, 150, 3, 3, 64, 64, dtype, 1)
+    run_and_check(dtype, *args, None, 1.7)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_keys_that_are_alike(dtype):
+    """Keys of one direction: the chunks' triangular systems are far from the identity."""
+    run_and_check(dtype, *inputs(1, 256, 2, 2, 64, 64, dtype, 2, alike=3.0))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_lengths(dtype):
+    """Padded sequences, one empty, NaN behind their ends; lengths outside 0 .. L."""
+    q, k, v, g, beta, S0 = inputs(6, 200, 2, 1, 64, 64, dtype, 3)
+    lengths = torch.tensor([200, 0, 1, 64, 129, 65], device="cuda", dtype=torch.int32)
+    ref = run_and_check(dtype, q, k, v, g, beta, S0, None, lengths)
+    behind = torch.arange(200, device="cuda")[None] >= lengths[:, None]
+    for t in (q, k, v, g, beta):
+        t[behind] = float("nan")
+    o, S = h3.delta_rule(q, k, v, g, beta, S0=S0, lengths=lengths)
+    assert torch.equal(o, ref[0]) and torch.equal(S, ref[1])
+    assert (o[behind] == 0).all() and torch.equal(S[1], S0[1])
+    out = torch.tensor([999, -5, 1, 64, 129, 65], device="cuda")
+    o, S = h3.delta_rule(q, k, v, g, beta, S0=S0, lengths=out)
+    assert torch.equal(o, ref[0]) and torch.equal(S, ref[1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gates_at_their_ends(dtype):
+    q, k, v, g, beta, S0 = inputs(2, 100, 2, 2, 32, 32, dtype, 4)
+    g[:, 10], g[:, 70], g[:, 71] = -float("inf"), -1e30, 0.0
+    beta[:, 20], beta[:, 30] = 0.0, 1.0
+    run_and_check(dtype, q, k, v, g, beta, S0)
+    zero = torch.zeros_like(g)
+    o, S = h3.delta_rule(q, k, v, zero, zero, S0=S0)
+    assert torch.equal(S, S0)   # nothing decays, nothing is written
+
+
+def test_sizes_of_values():
+    """bf16 values of any size: results scale with them bit for bit."""
+    q, k, v, g, beta, S0 = inputs(1, 100, 2, 2, 64, 64, "bf16", 5)
+    o, S = h3.delta_rule(q, k, v, g, beta, S0=S0)
+    for f in (2.0 ** 60, 2.0 ** -60):
+        o2, S2 = h3.delta_rule(q, k, v * f, g, beta, S0=S0 * f)
+        assert torch.equal(o2, o * f) and torch.equal(S2, S * f)
+
+
+def test_continues_and_meets_the_step():
+    """Two halves, and the second one token by token, give the state of the whole."""
+    q, k, v, g, beta, S0 = inputs(2, 192, 2, 2, 64, 64, "f32", 6)
+    part = lambda a, b: [t[:, a:b] for t in (q, k, v, g, beta)]
+    o, S = h3.delta_rule(q, k, v, g, beta, S0=S0)
+    o1, S1 = h3.delta_rule(*part(0, 128), S0=S0)
+    o2, S2 = h3.delta_rule(*part(128, 192), S0=S1)
+    assert torch.equal(o1, o[:, :128]) and torch.equal(o2, o[:, 128:]) and torch.equal(S2, S)
+    M = reference(q, k, v, g, beta, S0, 0.125)[2]
+    o3 = h3.delta_step(*part(128, 192), S1)
+    off = 64 * 80 * E32 * M + off_by(64, 64, "f32", M, 4.0)   # both derived above; sums of |X beta| of random keys stay under 4
+    assert (S1 - S).abs().max() <= off and (o3 - o2).abs().max() <= 8 * off
+
+
+def test_views_stream_workspace_and_out():
+    q, k, v, g, beta, S0 = inputs(2, 130, 4, 4, 64, 64, "bf16", 7)
+    want = h3.delta_rule(q, k, v, g, beta, S0=S0)
+    qkv = torch.cat([q, k, v], -1)
+    ws = torch.full((h3.workspace_size(h3.OP_DELTA, 2, 4, 130, 64, 64, h3.BF16),), 255, dtype=torch.uint8, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        out = torch.empty_like(v)
+        got = h3.delta_rule(qkv[..., :64], qkv[..., 64:128], qkv[..., 128:], g, beta, S0=S0, out=out, workspace=ws)
+    torch.cuda.current_stream().wait_stream(s)
+    assert got[0] is out and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    off = torch.empty(q.numel() + 1, dtype=q.dtype, device="cuda")[1:].view(q.shape)
+    off.copy_(q)
+    got = h3.delta_rule(off, k, v, g, beta, S0=S0)   # queries that start 2 bytes off
+    assert torch.equal(got[0], want[0])
+
+
+def test_repeats_in_a_graph():
+    q, k, v, g, beta, S0 = inputs(2, 200, 3, 3, 64, 64, "f16", 8)
+    want = [t.clone() for t in h3.delta_rule(q, k, v, g, beta, S0=S0)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = h3.delta_rule(q, k, v, g, beta, S0=S0)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert all(torch.equal(a, b) for a, b in zip(h3.delta_rule(q, k, v, g, beta, S0=S0), want))
