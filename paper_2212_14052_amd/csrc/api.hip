@@ -60,7 +60,7 @@ struct DeltaWs {
     size_t x, p, gates, xt, pt, es, states, fwd, saved;
     DeltaWs(int B, int H, int L, int Dk, int Dv, int dtype) {
         const size_t ch = (size_t)B * H * ((L + kDeltaChunk - 1) / kDeltaChunk);
-        const size_t mat = align_up(ch * (dtype == H3_F32 ? 3 : 2) * kDeltaChunk * kDeltaChunk * 2);
+        const size_t mat = align_up(ch * (dtype == H3_F32 ? 3 : 2) * kDeltaMatBytes);
         const size_t gb = align_up(ch * sizeof(ChunkGates));
         x = 0;
         p = mat;

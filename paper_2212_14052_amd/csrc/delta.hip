@@ -124,16 +124,20 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
     const long at = ch * NM * MAT;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        const int row = 16 * w + c16, c0 = 32 * s + 4 * g4, f = (2 * w + s) * FRAG + lane;
-        const float *ar = A + row * AROW + c0, *pr = P + row * AROW + c0;
-        const Op<NM> x = split8<NM>(*(const dl_f4 *)ar, *(const dl_f4 *)(ar + 16));
-        const Op<NM> p = split8<NM>(*(const dl_f4 *)pr, *(const dl_f4 *)(pr + 16));
+        const int row = 16 * w + c16, c0 = 32 * s + 4 * g4;
+        if (s <= w / 2) {
+            const int f = lower_frag(w, s) * FRAG + lane;
+            const float *ar = A + row * AROW + c0, *pr = P + row * AROW + c0;
+            const Op<NM> x = split8<NM>(*(const dl_f4 *)ar, *(const dl_f4 *)(ar + 16));
+            const Op<NM> p = split8<NM>(*(const dl_f4 *)pr, *(const dl_f4 *)(pr + 16));
 #pragma unroll
-        for (int i = 0; i < NM; ++i) {
-            XF[at + i * MAT + f] = x.p[i];
-            PF[at + i * MAT + f] = p.p[i];
+            for (int i = 0; i < NM; ++i) {
+                XF[at + i * MAT + f] = x.p[i];
+                PF[at + i * MAT + f] = p.p[i];
+            }
         }
-        if (XTF) {   // the transposes, for the backward pass
+        if (XTF && s >= w / 2) {   // the transposes, for the backward pass
+            const int f = upper_frag(w, s) * FRAG + lane;
             float xt[8], pt[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -151,6 +155,16 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
     }
 }
 
+// LDS of a workgroup of NW waves: keys and queries in pieces, X and P as
+// fragments, its columns of V (rows padded by 16 bytes), the gates.
+template <int DT, int KS, int NW> struct ScanLds {
+    static constexpr int vrow = 16 * NW + 16 / (int)sizeof(typename IO<DT>::T);
+    static constexpr int kq = pieces<DT>() * DC * lds_row<KS>() * 2;
+    static constexpr int k = 0, q = kq, mats = 2 * kq, v = mats + 2 * mat_pieces<DT>() * MAT * 16,
+                         gates = v + DC * vrow * (int)sizeof(typename IO<DT>::T), total = gates + (int)sizeof(ChunkGates);
+    static_assert(total <= 160 * 1024, "LDS of a CU");
+};
+
 // NW waves of 16 columns.  es, states: the chunks' errors (64, Dv) and first
 // states (Dk, Dv), for the backward pass, or null.
 template <int DT, int KS, int NW>
@@ -161,10 +175,16 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
                                                                float *__restrict__ es, float *__restrict__ states) {
     typedef typename IO<DT>::T T;
     constexpr int NT = pieces<DT>(), NM = mat_pieces<DT>(), NO = DT == F32 ? 3 : 2;
-    constexpr int ITEMS = 4 * KS / NW;   // groups of eight channels a thread brings in, of keys and of queries
-    extern __shared__ __attribute__((aligned(16))) uint16_t lds[];
-    uint16_t *ks = lds, *qs = lds + NT * DC * lds_row<KS>();
-    ChunkGates *gt = (ChunkGates *)(qs + NT * DC * lds_row<KS>());
+    typedef ScanLds<DT, KS, NW> Lds;
+    // what a thread brings in: groups of eight channels of keys and of queries, 16-byte
+    // words of X and P, groups of eight values, words of the gates
+    constexpr int NTH = 64 * NW, ITEMS = 4 * KS / NW, MATS = 2 * NM * MAT / NTH, VALS = 2, GATES = (3 * DC + NTH - 1) / NTH;
+    static_assert(2 * NM * MAT % NTH == 0 && 4 * KS % NW == 0 && DC * 2 * NW == VALS * NTH, "whole shares");
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    uint16_t *ks = (uint16_t *)(lds + Lds::k), *qs = (uint16_t *)(lds + Lds::q);
+    uint4 *ms = (uint4 *)(lds + Lds::mats);
+    T *vs = (T *)(lds + Lds::v);
+    ChunkGates *gt = (ChunkGates *)(lds + Lds::gates);
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g4 = lane >> 4, c16 = lane & 15;
     const int tiles = (a.Dv + 16 * NW - 1) / (16 * NW);
     const long bh = blockIdx.x / tiles;
@@ -176,8 +196,10 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
     const int len = tokens_of(a, b), nb = (len + DC - 1) / DC;
     const T *kp = (const T *)a.k, *qp = (const T *)a.q, *vp = (const T *)a.v;
 
-    Raw8<DT> pk[ITEMS], pq[ITEMS];
-    float pg[(3 * DC + 64 * NW - 1) / (64 * NW)];
+    Raw8<DT> pk[ITEMS], pq[ITEMS], pv[VALS];
+    uint4 pm[MATS];
+    float pg[GATES];
+    const int cb = c0 - 16 * w;   // the workgroup's first column
     auto fetch = [&](int n) {
         const long tok0 = (long)b * a.L + n * DC;
         const int nt = len - n * DC;
@@ -188,10 +210,22 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
             pk[i] = ld8_raw<DT>(kp + at, t < nt && c < a.Dk);
             pq[i] = ld8_raw<DT>(qp + at, t < nt && c < a.Dk);
         }
-        const float *gp = (const float *)(gates + bh * a.N + n);
 #pragma unroll
-        for (int i = 0; i < (3 * DC + 64 * NW - 1) / (64 * NW); ++i)
-            if (i * 64 * NW + tid < 3 * DC) pg[i] = gp[i * 64 * NW + tid];
+        for (int i = 0; i < VALS; ++i) {
+            const int it = i * NTH + tid, t = it / (2 * NW), c = cb + 8 * (it % (2 * NW));
+            pv[i] = ld8_raw<DT>(vp + ((tok0 + t) * a.H + h) * a.Dv + c, t < nt && c < a.Dv);
+        }
+        const long ch = bh * a.N + n;
+        const uint4 *xp = XF + ch * NM * MAT, *pp = PF + ch * NM * MAT;
+#pragma unroll
+        for (int i = 0; i < MATS; ++i) {
+            const int it = i * NTH + tid;
+            pm[i] = it < NM * MAT ? xp[it] : pp[it - NM * MAT];
+        }
+        const float *gp = (const float *)(gates + ch);
+#pragma unroll
+        for (int i = 0; i < GATES; ++i)
+            if (i * NTH + tid < 3 * DC) pg[i] = gp[i * NTH + tid];
     };
 
     dl_f4 S[2 * KS];
@@ -218,19 +252,20 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
             }
         }
 #pragma unroll
-        for (int i = 0; i < (3 * DC + 64 * NW - 1) / (64 * NW); ++i)
-            if (i * 64 * NW + tid < 3 * DC) ((float *)gt)[i * 64 * NW + tid] = pg[i];
+        for (int i = 0; i < VALS; ++i) {
+            const int it = i * NTH + tid;
+            T *p = vs + it / (2 * NW) * Lds::vrow + 8 * (it % (2 * NW));
+#pragma unroll
+            for (int j = 0; j < (DT == F32 ? 2 : 1); ++j) ((uint4 *)p)[j] = pv[i].a[j];
+        }
+#pragma unroll
+        for (int i = 0; i < MATS; ++i) ms[i * NTH + tid] = pm[i];
+#pragma unroll
+        for (int i = 0; i < GATES; ++i)
+            if (i * NTH + tid < 3 * DC) ((float *)gt)[i * NTH + tid] = pg[i];
         __syncthreads();
         if (n + 1 < nb) fetch(n + 1);
         if (!here) continue;
-        float v[4][4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int tt = 16 * t + 4 * g4 + r;
-                v[t][r] = on && tt < nt ? IO<DT>::ld(vp, ((tok0 + tt) * a.H + h) * a.Dv + col) : 0.f;
-            }
         if (states && on) {
 #pragma unroll
             for (int t = 0; t < 2 * KS; ++t)
@@ -256,9 +291,23 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
         for (int t = 0; t < 4; ++t) {
             const dl_f4 f = *(const dl_f4 *)(gt->from0 + 16 * t + 4 * g4);
             be[t] = *(const dl_f4 *)(gt->beta + 16 * t + 4 * g4);
+            float v[4];   // tokens 16 t + 4 g .. + 3 of this lane's column
+            if constexpr (DT == F32) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = vs[(16 * t + 4 * g4 + r) * Lds::vrow + 16 * w + c16];
+            } else {
+                const T *p = vs + (16 * t + 4 * g4 + (c16 >> 2)) * Lds::vrow + 16 * w + 4 * (lane & 3);
+                const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((dl_lds_s4 *)p));
+                const uint32_t y[2] = {x.x, x.y};
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint16_t z = (uint16_t)(r & 1 ? y[r / 2] >> 16 : y[r / 2] & 0xffffu);
+                    v[r] = DT == BF16 ? bf16_to_f32(z) : f16_to_f32(z);
+                }
+            }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                R[t][r] = v[t][r] - f[r] * R[t][r];
+                R[t][r] = v[r] - f[r] * R[t][r];
                 u[t][r] = be[t][r] * R[t][r];
             }
         }
@@ -271,7 +320,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
             for (int t = 0; t < 4; ++t) {
                 dl_f4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int s = 0; s <= t / 2; ++s) x = mm(ld_frag<NM>(XF + ch * NM * MAT, t, s, lane), br[s], x);
+                for (int s = 0; s <= t / 2; ++s) x = mm(ld_frag<NM>(ms, lower_frag(t, s), lane), br[s], x);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     R[t][r] -= x[r];
@@ -303,7 +352,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
 #pragma unroll
                 for (int r = 0; r < 4; ++r) x[r] *= f;
 #pragma unroll
-                for (int s = 0; s <= t / 2; ++s) x = mm(uo[s], ld_frag<NM>(PF + ch * NM * MAT, t, s, lane), x);
+                for (int s = 0; s <= t / 2; ++s) x = mm(uo[s], ld_frag<NM>(ms + NM * MAT, lower_frag(t, s), lane), x);
                 const int tt = 16 * t + c16;
                 if (on4 && n * DC + tt < a.L) {
                     const bool real = tt < nt;
@@ -363,10 +412,10 @@ hipError_t fwd_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_f
     delta_chunk_kernel<DT, KS><<<(unsigned)(bh * a.N), 256, 0, st>>>(a, w.X, w.P, w.XT, w.PT, w.gates);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const size_t lds = (size_t)2 * pieces<DT>() * DC * lds_row<KS>() * 2 + sizeof(ChunkGates);
+    constexpr int lds = ScanLds<DT, KS, NW>::total;
     const int tiles = (a.Dv + 16 * NW - 1) / (16 * NW);
     if (lds > 65536)
-        (void)hipFuncSetAttribute((const void *)delta_scan_kernel<DT, KS, NW>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        (void)hipFuncSetAttribute((const void *)delta_scan_kernel<DT, KS, NW>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     delta_scan_kernel<DT, KS, NW><<<(unsigned)(bh * tiles), 64 * NW, lds, st>>>(a, w.X, w.P, w.gates, (T *)o, S_final, w.es,
                                                                                w.states);
     return hipGetLastError();

@@ -124,11 +124,13 @@ template <int DT> __device__ __forceinline__ Op<pieces<DT>()> op_of(const Raw8<D
 // contiguous bytes of a key or query: tile 2 s + h, row r is channel
 //     32 s + 8 (r / 4) + 4 h + r % 4.
 //
-// A 64 x 64 matrix of a chunk (X, P and their transposes) is kept in global
-// memory as the left operand's registers: fragments (row tile, s), 64 lanes of
-// 16 bytes, each piece for itself.
+// A triangular 64 x 64 matrix of a chunk (X, P and their transposes) is kept in
+// global memory as the left operand's registers: six fragments (row tile, s) of
+// 64 lanes of 16 bytes, the two that hold only zeros left out, each piece for itself.
 constexpr int FRAG = 64;                 // uint4 a fragment
-constexpr int MAT = 8 * FRAG;            // uint4 a piece of a 64 x 64 matrix
+constexpr int MAT = 6 * FRAG;            // uint4 a piece of a matrix
+constexpr int lower_frag(int t, int s) { return t < 2 ? t : 2 * t - 2 + s; }       // s <= t / 2
+constexpr int upper_frag(int t, int s) { return t < 2 ? 2 * t + s : 2 + t; }       // s >= t / 2
 
 // keys and queries of a chunk in LDS: [piece][token][channel], rows padded by
 // 16 bytes, which spreads a tile's 16 rows over the banks
@@ -161,11 +163,11 @@ __device__ __forceinline__ Op<NT> lds_cols(const uint16_t *m, int T, int s, int 
     }
     return o;
 }
-// fragment (t, s) of a chunk's matrix in N pieces
-template <int N> __device__ __forceinline__ Op<N> ld_frag(const uint4 *m, int t, int s, int lane) {
+// fragment f of a matrix in N pieces
+template <int N> __device__ __forceinline__ Op<N> ld_frag(const uint4 *m, int f, int lane) {
     Op<N> o;
 #pragma unroll
-    for (int n = 0; n < N; ++n) o.p[n] = m[n * MAT + (2 * t + s) * FRAG + lane];
+    for (int n = 0; n < N; ++n) o.p[n] = m[n * MAT + f * FRAG + lane];
     return o;
 }
 

@@ -173,6 +173,7 @@ hipError_t launch_delta_step(const void *q, const void *k, const void *v, const 
 
 // The gated delta rule over whole sequences, chunks of 64 tokens.
 constexpr int kDeltaChunk = 64;
+constexpr size_t kDeltaMatBytes = 6 * 1024;   // a bf16 piece of a triangular 64 x 64 matrix, 16 x 32 blocks of zeros left out
 struct DeltaArgs {
     const void *q, *k, *v;
     const float *g, *beta;
