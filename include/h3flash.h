@@ -342,6 +342,27 @@ int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, c
                   float *S_final, void *saved, size_t saved_bytes, void *workspace, size_t ws_bytes, void *stream);
 
 /*
+ * h3_delta_rule_bwd — backward pass of h3_delta_rule for gradients do of its
+ * output and dS of its final state, from what it left in `saved`.
+ *   q, k, v, g, beta, lengths, scale, sizes: as in that call, unchanged.
+ *   dout        the output's gradient, of o's shape and type (tokens from lengths[b] on are not read).
+ *   dS          (B, H, Dk, Dv) float32, or NULL for zero.
+ *   saved       that call's buffer, read only.
+ *   dq, dk (B, L, Hk, Dk), dv (B, L, H, Dv) of `dtype`: heads that share a key
+ *               and query add up their gradients in float32, rounded once.
+ *   dg, dbeta   (B, L, H) float32.
+ *   dS0         (B, H, Dk, Dv) float32, the gradient of the first state, or NULL; may be dS's buffer.
+ *               Gradients of tokens from lengths[b] on are 0.
+ *   workspace   >= h3_workspace_size(H3_OP_DELTA_BWD, B, H, L, Dk, Dv, dtype).
+ * Nothing else that is written overlaps anything.  Results do not depend on timing.
+ * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, 2^31 chunks), EWORKSPACE, EDEVICE.
+ */
+int h3_delta_rule_bwd(const void *q, const void *k, const void *v, const float *g, const float *beta, const void *dout,
+                      const float *dS, const void *saved, size_t saved_bytes, const int *lengths, float scale, int B, int L,
+                      int H, int Hk, int Dk, int Dv, int dtype, void *dq, void *dk, void *dv, float *dg, float *dbeta,
+                      float *dS0, void *workspace, size_t ws_bytes, void *stream);
+
+/*
  * h3_workspace_size — bytes of workspace an operation needs (0 if the
  * arguments are invalid).  H_or_d is H for the convolutions, d for the layer
  * and the norm, whose B is its number of rows;

@@ -21,8 +21,8 @@ import torch
 __all__ = [
     "H3Error", "lib", "ssm_discretize", "ssm_kernel", "fftconv", "statepass_conv",
     "statepass_conv_noalloc", "layer_fwd", "layer_fwd_heads", "ssm_step", "fftconv_bwd", "kernel_spectrum", "fftconv_spectral", "workspace_size", "status_string", "F32", "F16", "BF16",
-    "layernorm", "layernorm_bwd", "delta_rule", "delta_step",
-    "OP_FFTCONV", "OP_STATEPASS", "OP_LAYER", "OP_FFTCONV_BWD", "OP_LAYER_HEADS", "OP_LAYERNORM_BWD", "OP_DELTA", "OP_DELTA_SAVED", "FUSED_LIMIT", "FUSED_LIMIT_F32", "MAX_MODES",
+    "layernorm", "layernorm_bwd", "delta_rule", "delta_rule_bwd", "delta_step",
+    "OP_FFTCONV", "OP_STATEPASS", "OP_LAYER", "OP_FFTCONV_BWD", "OP_LAYER_HEADS", "OP_LAYERNORM_BWD", "OP_DELTA", "OP_DELTA_SAVED", "OP_DELTA_BWD", "FUSED_LIMIT", "FUSED_LIMIT_F32", "MAX_MODES",
 ]
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -72,6 +72,7 @@ def lib() -> ctypes.CDLL:
         L.h3_layernorm_bwd.argtypes = [vp, vp, vp, vp, vp, i, i, i, vp, vp, vp, vp, sz, vp]
         L.h3_delta_step.argtypes = [vp, vp, vp, vp, vp, fl, i, i, i, i, i, i, i, vp, vp, vp]
         L.h3_delta_rule.argtypes = [vp] * 7 + [fl] + [i] * 7 + [vp, vp, vp, sz, vp, sz, vp]
+        L.h3_delta_rule_bwd.argtypes = [vp] * 8 + [sz, vp, fl] + [i] * 7 + [vp] * 7 + [sz, vp]
         L.h3_workspace_size.argtypes = [i, i, i, i, i, i, i]
         L.h3_workspace_size.restype = sz
         L.h3_status_string.argtypes = [i]
@@ -79,7 +80,7 @@ def lib() -> ctypes.CDLL:
         for fn in ("h3_ssm_discretize", "h3_ssm_kernel", "h3_fftconv", "h3_statepass_conv", "h3_statepass_conv_noalloc",
                    "h3_layer_fwd", "h3_kernel_spectrum", "h3_fftconv_spectral", "h3_ssm_step", "h3_fftconv_bwd",
                    "h3_layer_fwd_heads", "h3_layernorm", "h3_layernorm_bwd", "h3_delta_step",
-                   "h3_delta_rule"):
+                   "h3_delta_rule", "h3_delta_rule_bwd"):
             getattr(L, fn).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -608,3 +609,34 @@ def delta_rule(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, g: torch.Tenso
             Bn, L, H, Hk, Dk, Dv, dt, _ptr(o), _ptr(S), _ptr(saved), n, _ptr(ws), ws.numel() * ws.element_size(),
             _stream(dev)))
     return (o, S, saved) if save else (o, S)
+
+
+def delta_rule_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, g: torch.Tensor, beta: torch.Tensor,
+                   do: torch.Tensor, saved: torch.Tensor, dS: Optional[torch.Tensor] = None,
+                   scale: Optional[float] = None, lengths: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None):
+    """Backward pass of delta_rule for the gradients ``do`` of its output and
+    ``dS`` (or None) of its final state, from the buffer that its call with
+    ``save`` and the same arguments returned.  Returns (dq, dk, dv, dg, dbeta, dS0)."""
+    dev, q, k, v, g, beta, (Bn, L, H, Hk, Dk, Dv, dt) = _delta_args(q, k, v, g, beta)
+    _on(dev, do=do, dS=dS, saved=saved)
+    _shape("do", do, v.shape)
+    if do.dtype != v.dtype:
+        raise ValueError("do must have v's dtype")
+    dS = _f32(dS)
+    _shape("dS", dS, (Bn, H, Dk, Dv))
+    lengths = _lengths(lengths, Bn, dev)
+    if not saved.is_contiguous():
+        raise ValueError("saved must be contiguous")
+    q, k, v, do = _aligned(q), _aligned(k), _aligned(v), _aligned(do.contiguous())
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    dg, dbeta = torch.empty_like(g), torch.empty_like(beta)
+    dS0 = torch.empty((Bn, H, Dk, Dv), dtype=torch.float32, device=dev)
+    ws = _workspace(_ws_size(OP_DELTA_BWD, Bn, H, L, Dk, Dv, dt), dev, workspace)
+    with _device(dev):
+        _check("h3_delta_rule_bwd", lib().h3_delta_rule_bwd(
+            _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(do), _ptr(dS), _ptr(saved),
+            saved.numel() * saved.element_size(), _ptr(lengths), Dk ** -0.5 if scale is None else scale, Bn, L, H, Hk, Dk, Dv,
+            dt, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dg), _ptr(dbeta), _ptr(dS0), _ptr(ws), ws.numel() * ws.element_size(),
+            _stream(dev)))
+    return dq, dk, dv, dg, dbeta, dS0

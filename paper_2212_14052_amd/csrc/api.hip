@@ -57,20 +57,24 @@ struct DeltaBytes {
 // it leaves for the backward pass (the gates, both transposes, the errors and the
 // chunks' first states).
 struct DeltaWs {
-    size_t x, p, gates, xt, pt, es, states, fwd, saved;
+    size_t x, p, gates, xt, pt, es, states, dends, fwd, saved, bwd;
     DeltaWs(int B, int H, int L, int Dk, int Dv, int dtype) {
         const size_t ch = (size_t)B * H * ((L + kDeltaChunk - 1) / kDeltaChunk);
         const size_t mat = align_up(ch * (dtype == H3_F32 ? 3 : 2) * kDeltaMatBytes);
+        const size_t back = align_up(ch * 3 * kDeltaMatBytes);   // X and the transposes: three pieces for every type
         const size_t gb = align_up(ch * sizeof(ChunkGates));
         x = 0;
-        p = mat;
-        gates = 2 * mat;   // of the workspace, and at 0 of what is kept
+        p = back;
+        gates = p + mat;   // of the workspace, and at 0 of what is kept
         fwd = gates + gb;
         xt = gb;
-        pt = xt + mat;
-        es = pt + mat;
+        pt = xt + back;
+        es = pt + back;
         states = es + align_up(ch * kDeltaChunk * Dv * 4);
         saved = states + align_up(ch * Dk * Dv * 4);
+        // the backward pass's workspace: z of every token, the gradient of every chunk's last state
+        dends = align_up(ch * kDeltaChunk * Dv * 4);
+        bwd = dends + align_up(ch * Dk * Dv * 4);
     }
 };
 
@@ -283,6 +287,8 @@ size_t h3_workspace_size(int op, int B, int H, int L, int m, int chunk, int dtyp
             return delta_sizes_ok(m, chunk) ? DeltaWs(B, H, L, m, chunk, dtype).fwd : 0;
         case H3_OP_DELTA_SAVED:
             return delta_sizes_ok(m, chunk) ? DeltaWs(B, H, L, m, chunk, dtype).saved : 0;
+        case H3_OP_DELTA_BWD:
+            return delta_sizes_ok(m, chunk) ? DeltaWs(B, H, L, m, chunk, dtype).bwd : 0;
         case H3_OP_LAYERNORM_BWD:   // B = rows, H = d
             return align_up(layernorm_bwd_workspace(B, H));
         case H3_OP_FFTCONV_BWD: {
@@ -685,6 +691,44 @@ int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, c
         d.states = (float *)(sv + w.states);
     }
     return launched(launch_delta_rule(a, dtype, d, o, S_final, (hipStream_t)stream));
+}
+
+int h3_delta_rule_bwd(const void *q, const void *k, const void *v, const float *g, const float *beta, const void *dout,
+                      const float *dS, const void *saved, size_t saved_bytes, const int *lengths, float scale, int B, int L,
+                      int H, int Hk, int Dk, int Dv, int dtype, void *dq, void *dk, void *dv, float *dg, float *dbeta,
+                      float *dS0, void *workspace, size_t ws_bytes, void *stream) {
+    if (!q || !k || !v || !g || !beta || !dout || !saved || !dq || !dk || !dv || !dg || !dbeta || B < 1 || L < 1 || H < 1 ||
+        Hk < 1 || Dk < 1 || Dv < 1 || H % Hk)
+        return H3_EINVAL;
+    if (!dtype_ok(dtype) || !delta_sizes_ok(Dk, Dv) || !delta_chunks_ok(B, L, H, Dv)) return H3_EUNSUPPORTED;
+    const DeltaWs w(B, H, L, Dk, Dv, dtype);
+    if (!workspace || ws_bytes < w.bwd || saved_bytes < w.saved) return H3_EWORKSPACE;
+    const DeltaBytes n(B, L, H, Hk, Dk, Dv, dtype);
+    for (const void *p : {q, k, v, dout, saved, (const void *)dq, (const void *)dk, (const void *)dv, (const void *)workspace})
+        if (!aligned16(p)) return H3_EINVAL;
+    for (const void *p : {(const void *)g, (const void *)beta, (const void *)dS, (const void *)lengths, (const void *)dg,
+                          (const void *)dbeta, (const void *)dS0})
+        if ((uintptr_t)p & 3) return H3_EINVAL;
+    const void *ins[9] = {q, k, v, g, beta, dout, dS, saved, lengths};
+    const size_t isz[9] = {n.qk, n.qk, n.v, n.gate, n.gate, n.v, n.state, w.saved, (size_t)B * 4};
+    const void *outs[7] = {dq, dk, dv, dg, dbeta, dS0, workspace};
+    const size_t osz[7] = {n.qk, n.qk, n.v, n.gate, n.gate, n.state, w.bwd};
+    for (int i = 0; i < 7; ++i) {
+        for (int j = 0; j < 9; ++j)
+            if (overlap(outs[i], osz[i], ins[j], isz[j]) && !(i == 5 && j == 6 && dS0 == dS)) return H3_EINVAL;
+        for (int j = i + 1; j < 7; ++j)
+            if (overlap(outs[i], osz[i], outs[j], osz[j])) return H3_EINVAL;
+    }
+    DeltaArgs a{q, k, v, g, beta, lengths, nullptr, scale, B, L, H, Hk, Dk, Dv, (L + kDeltaChunk - 1) / kDeltaChunk};
+    char *ws = (char *)workspace, *sv = (char *)saved;
+    DeltaBuffers d{};
+    d.gates = (ChunkGates *)sv;
+    d.XT = (uint4 *)(sv + w.xt);
+    d.PT = (uint4 *)(sv + w.pt);
+    d.es = (float *)(sv + w.es);
+    d.states = (float *)(sv + w.states);
+    DeltaGrads r{dout, dS, dq, dk, dv, dg, dbeta, dS0, (float *)ws, (float *)(ws + w.dends)};
+    return launched(launch_delta_rule_bwd(a, dtype, d, r, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -21,11 +21,6 @@
 namespace h3 {
 namespace {
 
-constexpr double kLog2e = 1.4426950408889634073599246810018921;
-// a log decay below this is an exact zero in float32 whatever it is (also -inf,
-// whose differences would not be numbers)
-constexpr double kLowest = -1e6;
-
 constexpr int AROW = DC + 4;   // floats a row of a 64 x 64 matrix in LDS
 
 template <int DT, int KS>
@@ -33,7 +28,7 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
                                                           uint4 *__restrict__ XTF, uint4 *__restrict__ PTF,
                                                           ChunkGates *__restrict__ gates) {
     typedef typename IO<DT>::T T;
-    constexpr int NT = pieces<DT>(), NM = mat_pieces<DT>();
+    constexpr int NT = pieces<DT>(), NM = mat_pieces<DT>(), NX = kFullPieces;
     __shared__ __attribute__((aligned(16))) uint16_t ks[NT * DC * lds_row<KS>()];
     __shared__ __attribute__((aligned(16))) float A[DC * AROW], P[DC * AROW];
     __shared__ double gd[DC];
@@ -47,14 +42,7 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
     const int hk = h / (a.H / a.Hk);
     if (w == 0) {
         const bool on = lane < nt;
-        double x = on ? (double)a.g[(tok0 + lane) * a.H + h] : 0.0;
-        x = x < kLowest ? kLowest : x;
-#pragma unroll
-        for (int m = 1; m < 64; m *= 2) {
-            const double y = __shfl_up(x, m);
-            if (lane >= m) x += y;
-        }
-        x *= kLog2e;
+        const double x = decay_sum(on ? a.g[(tok0 + lane) * a.H + h] : 0.f, on, lane);
         const float bt = on ? a.beta[(tok0 + lane) * a.H + h] : 0.f;
         gd[lane] = x;
         be[lane] = bt;
@@ -85,8 +73,8 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 const Op<NT> kj = lds_rows<NT, KS>(ks, j, s, lane);
-                ka = mm(lds_rows<NT, KS>(ks, w, s, lane), kj, ka);
-                pa = mm(qo[s], kj, pa);
+                ka = mm<NT, NT, input_products<DT>()>(lds_rows<NT, KS>(ks, w, s, lane), kj, ka);
+                pa = mm<NT, NT, input_products<DT>()>(qo[s], kj, pa);
             }
         }
         const int col = 16 * j + c16;
@@ -121,20 +109,19 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
         }
     }
     __syncthreads();
-    const long at = ch * NM * MAT;
+    const long at = ch * NM * MAT, xat = ch * NX * MAT;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         const int row = 16 * w + c16, c0 = 32 * s + 4 * g4;
         if (s <= w / 2) {
             const int f = lower_frag(w, s) * FRAG + lane;
             const float *ar = A + row * AROW + c0, *pr = P + row * AROW + c0;
-            const Op<NM> x = split8<NM>(*(const dl_f4 *)ar, *(const dl_f4 *)(ar + 16));
+            const Op<NX> x = split8<NX>(*(const dl_f4 *)ar, *(const dl_f4 *)(ar + 16));
             const Op<NM> p = split8<NM>(*(const dl_f4 *)pr, *(const dl_f4 *)(pr + 16));
 #pragma unroll
-            for (int i = 0; i < NM; ++i) {
-                XF[at + i * MAT + f] = x.p[i];
-                PF[at + i * MAT + f] = p.p[i];
-            }
+            for (int i = 0; i < NX; ++i) XF[xat + i * MAT + f] = x.p[i];
+#pragma unroll
+            for (int i = 0; i < NM; ++i) PF[at + i * MAT + f] = p.p[i];
         }
         if (XTF && s >= w / 2) {   // the transposes, for the backward pass
             const int f = upper_frag(w, s) * FRAG + lane;
@@ -145,25 +132,15 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
                 xt[j] = A[r * AROW + row];
                 pt[j] = P[r * AROW + row];
             }
-            const Op<NM> xo = split8<NM>(xt), po = split8<NM>(pt);
+            const Op<NX> xo = split8<NX>(xt), po = split8<NX>(pt);
 #pragma unroll
-            for (int i = 0; i < NM; ++i) {
-                XTF[at + i * MAT + f] = xo.p[i];
-                PTF[at + i * MAT + f] = po.p[i];
+            for (int i = 0; i < NX; ++i) {
+                XTF[xat + i * MAT + f] = xo.p[i];
+                PTF[xat + i * MAT + f] = po.p[i];
             }
         }
     }
 }
-
-// LDS of a workgroup of NW waves: keys and queries in pieces, X and P as
-// fragments, its columns of V (rows padded by 16 bytes), the gates.
-template <int DT, int KS, int NW> struct ScanLds {
-    static constexpr int vrow = 16 * NW + 16 / (int)sizeof(typename IO<DT>::T);
-    static constexpr int kq = pieces<DT>() * DC * lds_row<KS>() * 2;
-    static constexpr int k = 0, q = kq, mats = 2 * kq, v = mats + 2 * mat_pieces<DT>() * MAT * 16,
-                         gates = v + DC * vrow * (int)sizeof(typename IO<DT>::T), total = gates + (int)sizeof(ChunkGates);
-    static_assert(total <= 160 * 1024, "LDS of a CU");
-};
 
 // NW waves of 16 columns.  es, states: the chunks' errors (64, Dv) and first
 // states (Dk, Dv), for the backward pass, or null.
@@ -174,12 +151,12 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
                                                                typename IO<DT>::T *__restrict__ o, float *S_final,
                                                                float *__restrict__ es, float *__restrict__ states) {
     typedef typename IO<DT>::T T;
-    constexpr int NT = pieces<DT>(), NM = mat_pieces<DT>(), NO = DT == F32 ? 3 : 2;
-    typedef ScanLds<DT, KS, NW> Lds;
+    constexpr int NT = pieces<DT>(), NX = kFullPieces, NM = mat_pieces<DT>(), NO = DT == F32 ? 3 : 2;
+    typedef ScanLds<DT, KS, NW, kFullPieces + mat_pieces<DT>()> Lds;
     // what a thread brings in: groups of eight channels of keys and of queries, 16-byte
     // words of X and P, groups of eight values, words of the gates
-    constexpr int NTH = 64 * NW, ITEMS = 4 * KS / NW, MATS = 2 * NM * MAT / NTH, VALS = 2, GATES = (3 * DC + NTH - 1) / NTH;
-    static_assert(2 * NM * MAT % NTH == 0 && 4 * KS % NW == 0 && DC * 2 * NW == VALS * NTH, "whole shares");
+    constexpr int NTH = 64 * NW, ITEMS = 4 * KS / NW, WORDS = (NX + NM) * MAT, MATS = (WORDS + NTH - 1) / NTH, VALS = 2, GATES = (3 * DC + NTH - 1) / NTH;
+    static_assert(4 * KS % NW == 0 && DC * 2 * NW == VALS * NTH, "whole shares");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     uint16_t *ks = (uint16_t *)(lds + Lds::k), *qs = (uint16_t *)(lds + Lds::q);
     uint4 *ms = (uint4 *)(lds + Lds::mats);
@@ -216,11 +193,11 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
             pv[i] = ld8_raw<DT>(vp + ((tok0 + t) * a.H + h) * a.Dv + c, t < nt && c < a.Dv);
         }
         const long ch = bh * a.N + n;
-        const uint4 *xp = XF + ch * NM * MAT, *pp = PF + ch * NM * MAT;
+        const uint4 *xp = XF + ch * NX * MAT, *pp = PF + ch * NM * MAT;
 #pragma unroll
         for (int i = 0; i < MATS; ++i) {
             const int it = i * NTH + tid;
-            pm[i] = it < NM * MAT ? xp[it] : pp[it - NM * MAT];
+            if (it < WORDS) pm[i] = it < NX * MAT ? xp[it] : pp[it - NX * MAT];
         }
         const float *gp = (const float *)(gates + ch);
 #pragma unroll
@@ -259,7 +236,8 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
             for (int j = 0; j < (DT == F32 ? 2 : 1); ++j) ((uint4 *)p)[j] = pv[i].a[j];
         }
 #pragma unroll
-        for (int i = 0; i < MATS; ++i) ms[i * NTH + tid] = pm[i];
+        for (int i = 0; i < MATS; ++i)
+            if (i * NTH + tid < WORDS) ms[i * NTH + tid] = pm[i];
 #pragma unroll
         for (int i = 0; i < GATES; ++i)
             if (i * NTH + tid < 3 * DC) ((float *)gt)[i * NTH + tid] = pg[i];
@@ -291,20 +269,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
         for (int t = 0; t < 4; ++t) {
             const dl_f4 f = *(const dl_f4 *)(gt->from0 + 16 * t + 4 * g4);
             be[t] = *(const dl_f4 *)(gt->beta + 16 * t + 4 * g4);
-            float v[4];   // tokens 16 t + 4 g .. + 3 of this lane's column
-            if constexpr (DT == F32) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = vs[(16 * t + 4 * g4 + r) * Lds::vrow + 16 * w + c16];
-            } else {
-                const T *p = vs + (16 * t + 4 * g4 + (c16 >> 2)) * Lds::vrow + 16 * w + 4 * (lane & 3);
-                const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((dl_lds_s4 *)p));
-                const uint32_t y[2] = {x.x, x.y};
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint16_t z = (uint16_t)(r & 1 ? y[r / 2] >> 16 : y[r / 2] & 0xffffu);
-                    v[r] = DT == BF16 ? bf16_to_f32(z) : f16_to_f32(z);
-                }
-            }
+            const dl_f4 v = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * w, lane);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 R[t][r] = v[r] - f[r] * R[t][r];
@@ -313,14 +278,14 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
         }
         // e = R - X (beta R), u = beta e
         {
-            Op<NM> br[2];
+            Op<NX> br[2];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) br[s] = split8<NM>(u[2 * s], u[2 * s + 1]);
+            for (int s = 0; s < 2; ++s) br[s] = split8<NX>(u[2 * s], u[2 * s + 1]);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 dl_f4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int s = 0; s <= t / 2; ++s) x = mm(ld_frag<NM>(ms, lower_frag(t, s), lane), br[s], x);
+                for (int s = 0; s <= t / 2; ++s) x = mm(ld_frag<NX>(ms, lower_frag(t, s), lane), br[s], x);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     R[t][r] -= x[r];
@@ -352,7 +317,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
 #pragma unroll
                 for (int r = 0; r < 4; ++r) x[r] *= f;
 #pragma unroll
-                for (int s = 0; s <= t / 2; ++s) x = mm(uo[s], ld_frag<NM>(ms + NM * MAT, lower_frag(t, s), lane), x);
+                for (int s = 0; s <= t / 2; ++s) x = mm(uo[s], ld_frag<NM>(ms + NX * MAT, lower_frag(t, s), lane), x);
                 const int tt = 16 * t + c16;
                 if (on4 && n * DC + tt < a.L) {
                     const bool real = tt < nt;
@@ -412,7 +377,7 @@ hipError_t fwd_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_f
     delta_chunk_kernel<DT, KS><<<(unsigned)(bh * a.N), 256, 0, st>>>(a, w.X, w.P, w.XT, w.PT, w.gates);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    constexpr int lds = ScanLds<DT, KS, NW>::total;
+    constexpr int lds = ScanLds<DT, KS, NW, kFullPieces + mat_pieces<DT>()>::total;
     const int tiles = (a.Dv + 16 * NW - 1) / (16 * NW);
     if (lds > 65536)
         (void)hipFuncSetAttribute((const void *)delta_scan_kernel<DT, KS, NW>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);

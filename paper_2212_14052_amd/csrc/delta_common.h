@@ -22,8 +22,10 @@ typedef float dl_f4 __attribute__((ext_vector_type(4)));
 typedef short dl_s4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) dl_s4 dl_lds_s4;
 
-// pieces of the inputs by type
+// pieces of the inputs by type, and how far the products of two inputs are
+// taken (both pieces of fp16 are exact: all four)
 template <int DT> constexpr int pieces() { return DT == BF16 ? 1 : DT == F16 ? 2 : 3; }
+template <int DT> constexpr int input_products() { return DT == BF16 ? 1 : 3; }
 
 // an operand of eight values a lane in N pieces
 template <int N> struct Op {
@@ -33,9 +35,9 @@ template <int N> struct Op {
 __device__ __forceinline__ dl_f4 dl_mfma(uint4 a, uint4 b, dl_f4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(dl_b8, a), __builtin_bit_cast(dl_b8, b), c, 0, 0, 0);
 }
-// c + a b, the smallest products first
-template <int NA, int NB> __device__ __forceinline__ dl_f4 mm(const Op<NA> &a, const Op<NB> &b, dl_f4 c) {
-    constexpr int N = NA > NB ? NA : NB;
+// c + a b, the smallest products first; N: how far products of pieces are taken
+template <int NA, int NB, int N = (NA > NB ? NA : NB)>
+__device__ __forceinline__ dl_f4 mm(const Op<NA> &a, const Op<NB> &b, dl_f4 c) {
 #pragma unroll
     for (int s = N - 1; s >= 0; --s)
 #pragma unroll
@@ -171,6 +173,45 @@ template <int N> __device__ __forceinline__ Op<N> ld_frag(const uint4 *m, int f,
     return o;
 }
 
+// rows r0 .. r0 + 3 of this lane's column (c0 + lane % 16) of 16-bit or float32 values in LDS, r0 = a + 4 (lane / 16)
+template <int DT>
+__device__ __forceinline__ dl_f4 lds_column4(const typename IO<DT>::T *m, int row, int a, int c0, int lane) {
+    const int g4 = lane >> 4, c16 = lane & 15;
+    dl_f4 v;
+    if constexpr (DT == F32) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = m[(a + 4 * g4 + r) * row + c0 + c16];
+    } else {
+        const typename IO<DT>::T *p = m + (a + 4 * g4 + (c16 >> 2)) * row + c0 + 4 * (lane & 3);
+        const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((dl_lds_s4 *)p));
+        const uint32_t y[2] = {x.x, x.y};
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const uint16_t z = (uint16_t)(r & 1 ? y[r / 2] >> 16 : y[r / 2] & 0xffffu);
+            v[r] = DT == BF16 ? bf16_to_f32(z) : f16_to_f32(z);
+        }
+    }
+    return v;
+}
+
+// ------------------------------------------------------- a chunk's decays ---
+constexpr double kLog2e = 1.4426950408889634073599246810018921;
+// a log decay below this is an exact zero in float32 whatever it is (also -inf,
+// whose differences would not be numbers)
+constexpr double kLowest = -1e6;
+
+// The running sum over the wave's lanes, in units of log 2.
+__device__ __forceinline__ double decay_sum(float g, bool on, int lane) {
+    double x = on ? (double)g : 0.0;
+    x = x < kLowest ? kLowest : x;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const double y = __shfl_up(x, m);
+        if (lane >= m) x += y;
+    }
+    return x * kLog2e;
+}
+
 // ----------------------------------------------------------- arguments -----
 // tokens of sequence b
 __device__ __forceinline__ int tokens_of(const DeltaArgs &a, int b) {
@@ -179,7 +220,20 @@ __device__ __forceinline__ int tokens_of(const DeltaArgs &a, int b) {
     return n < 0 ? 0 : n > a.L ? a.L : n;
 }
 
-// pieces of X and P: 16-bit results need 16 bits of them
+// Pieces of X and of the transposes that the backward pass reads: the states and the
+// gates' gradients are float32 (with X in two pieces beta's gradient was 1.3e-6 off).
+constexpr int kFullPieces = 3;
+// pieces of P, which only o is made of: 16-bit results need 16 bits of it
 template <int DT> constexpr int mat_pieces() { return DT == F32 ? 3 : 2; }
+
+// LDS of a workgroup of NW waves: keys and queries in pieces, two
+// triangular matrices of MP pieces together as fragments, its columns of V (or do) (rows padded by 16 bytes), the gates.
+template <int DT, int KS, int NW, int MP> struct ScanLds {
+    static constexpr int vrow = 16 * NW + 16 / (int)sizeof(typename IO<DT>::T);
+    static constexpr int kq = pieces<DT>() * DC * lds_row<KS>() * 2;
+    static constexpr int k = 0, q = kq, mats = 2 * kq, v = mats + MP * MAT * 16,
+                         gates = v + DC * vrow * (int)sizeof(typename IO<DT>::T), total = gates + (int)sizeof(ChunkGates);
+    static_assert(total <= 160 * 1024, "LDS of a CU");
+};
 
 }  // namespace h3

@@ -188,7 +188,7 @@ struct ChunkGates {
     float from0[kDeltaChunk], toend[kDeltaChunk], beta[kDeltaChunk];
 };
 // Buffers of the chunks of every (b, h): operand fragments of X and P (64 x 64,
-// mat_pieces bf16 pieces), of their transposes, the gates, the errors e (64,
+// three bf16 pieces, P two for 16-bit types), of their transposes, the gates, the errors e (64,
 // Dv) and the first states (Dk, Dv).  The forward pass writes XT, PT, es and
 // states where they are given (all or none).
 struct DeltaBuffers {
@@ -196,6 +196,16 @@ struct DeltaBuffers {
     ChunkGates *gates;
     float *es, *states;
 };
+// Its backward pass: zs (64, Dv) and dends (Dk, Dv) of every chunk are scratch.
+// dS, dS0 may be null.
+struct DeltaGrads {
+    const void *dout;
+    const float *dS;
+    void *dq, *dk, *dv;
+    float *dg, *dbeta, *dS0;
+    float *zs, *dends;
+};
+hipError_t launch_delta_rule_bwd(const DeltaArgs &a, int dtype, const DeltaBuffers &w, const DeltaGrads &d, hipStream_t s);
 hipError_t launch_delta_rule(const DeltaArgs &a, int dtype, const DeltaBuffers &w, void *o, float *S_final, hipStream_t s);
 
 }  // namespace h3

@@ -90,3 +90,81 @@ def test_binding_refusals():
     q, v, g = torch.zeros(1, 1, 2, 8), torch.zeros(1, 1, 2, 8), torch.zeros(1, 1, 2)
     with pytest.raises(ValueError):
         h3.delta_step(q, q, v, g, g, torch.zeros(1, 2, 8, 8))
+
+
+def rule(q=Q, k=K, v=V, g=G, beta=BE, S0=None, lengths=None, scale=0.1, B=2, L=70, H=4, Hk=2, Dk=64, Dv=64, dt=2, o=O, Sf=S,
+         saved=None, savedb=0, ws=W, wsb=1 << 26):
+    return h3.lib().h3_delta_rule(P(q), P(k), P(v), P(g), P(beta), P(S0), P(lengths), scale, B, L, H, Hk, Dk, Dv, dt, P(o),
+                                  P(Sf), P(saved), savedb, P(ws), wsb, None)
+
+
+def size(op, B=2, L=70, H=4, Dk=64, Dv=64, dt=2):
+    return h3.workspace_size(op, B, H, L, Dk, Dv, dt)
+
+
+def test_delta_rule_refusals():
+    for name in ("q", "k", "v", "g", "beta", "o"):
+        assert rule(**{name: 0}) == EINVAL
+    for name in ("B", "L", "H", "Hk", "Dk", "Dv"):
+        assert rule(**{name: 0}) == EINVAL
+    assert rule(Hk=3) == EINVAL
+    for name, bad in (("Dk", 12), ("Dk", 136), ("Dv", 20), ("Dv", 264), ("dt", 4)):
+        assert rule(**{name: bad}) == EUNSUP
+    assert rule(B=1 << 20, L=1 << 24, H=2, Hk=2, Dk=8, Dv=8) == EUNSUP     # 2^31 chunks and more
+    assert rule(ws=0) == EWS
+    assert rule(wsb=size(h3.OP_DELTA) - 1) == EWS
+    assert rule(saved=X, savedb=size(h3.OP_DELTA_SAVED) - 1) == EWS
+    for name, at in (("q", Q), ("k", K), ("v", V), ("o", O)):
+        assert rule(**{name: at + 8}) == EINVAL                            # 16-byte alignment
+    assert rule(S0=X + 2) == EINVAL
+    assert rule(lengths=X + 2) == EINVAL
+    assert rule(o=V) == EINVAL
+    assert rule(Sf=O + 256) == EINVAL
+    assert rule(S0=X, Sf=X + 4) == EINVAL                                  # partly over the first state
+    assert rule(ws=Q - 4096) == EINVAL
+    assert rule(saved=W + 4096, savedb=1 << 26) == EINVAL                  # inside the workspace
+    assert rule(lengths=W + 64) == EINVAL
+
+
+def bwd(q=Q, k=K, v=V, g=G, beta=BE, do=X, dS=None, saved=Y, savedb=1 << 27, lengths=None, scale=0.1, B=2, L=70, H=4, Hk=2,
+        Dk=64, Dv=64, dt=2, dq=O, dk=O + (1 << 22), dv=O + (1 << 23), dg=S, dbeta=S + (1 << 20), dS0=None, ws=W, wsb=1 << 26):
+    return h3.lib().h3_delta_rule_bwd(P(q), P(k), P(v), P(g), P(beta), P(do), P(dS), P(saved), savedb, P(lengths), scale, B,
+                                      L, H, Hk, Dk, Dv, dt, P(dq), P(dk), P(dv), P(dg), P(dbeta), P(dS0), P(ws), wsb, None)
+
+
+def test_delta_rule_bwd_refusals():
+    for name in ("q", "k", "v", "g", "beta", "do", "saved", "dq", "dk", "dv", "dg", "dbeta"):
+        assert bwd(**{name: 0}) == EINVAL
+    for name in ("B", "L", "H", "Hk", "Dk", "Dv"):
+        assert bwd(**{name: 0}) == EINVAL
+    assert bwd(Hk=3) == EINVAL
+    for name, bad in (("Dk", 4), ("Dk", 160), ("Dv", 12), ("Dv", 512), ("dt", -1)):
+        assert bwd(**{name: bad}) == (EUNSUP if bad != -1 or name == "dt" else EINVAL)
+    assert bwd(savedb=size(h3.OP_DELTA_SAVED) - 1) == EWS
+    assert bwd(ws=0) == EWS
+    assert bwd(wsb=size(h3.OP_DELTA_BWD) - 1) == EWS
+    assert bwd(do=X + 2) == EINVAL
+    assert bwd(saved=Y + 4) == EINVAL
+    assert bwd(dg=S + 2) == EINVAL
+    assert bwd(dq=Q) == EINVAL                                             # over an input
+    assert bwd(dk=O) == EINVAL                                             # over dq
+    assert bwd(dbeta=G) == EINVAL
+    assert bwd(ws=Y + 4096) == EINVAL                                      # inside what was kept
+    assert bwd(dS=V + (1 << 24), dS0=V + (1 << 24) + 64) == EINVAL         # partly over dS
+
+
+def test_delta_sizes():
+    assert size(h3.OP_DELTA, Dk=12) == 0 and size(h3.OP_DELTA_SAVED, Dv=0) == 0 and size(h3.OP_DELTA_BWD, L=0) == 0
+    # a chunk's state and errors in float32 for every 64 tokens
+    assert size(h3.OP_DELTA_SAVED) >= 2 * 4 * 2 * (64 * 64 * 4 + 64 * 64 * 4)
+    assert size(h3.OP_DELTA_BWD) >= 2 * 4 * 2 * (64 * 64 * 4 + 64 * 64 * 4)
+
+
+def test_delta_binding_refusals():
+    q, g = torch.zeros(1, 5, 2, 8), torch.zeros(1, 5, 2)
+    with pytest.raises(ValueError):
+        h3.delta_rule(q, q, q, g, g)
+    with pytest.raises(ValueError):
+        h3.delta_rule_bwd(q, q, q, g, g, q, torch.zeros(64, dtype=torch.uint8))
+    with pytest.raises(TypeError):
+        h3.delta_rule(None, q, q, g, g)
