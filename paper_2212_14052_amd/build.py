@@ -35,6 +35,7 @@ EXTRA = {
     "fftconv_wave16k.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "conv_direct.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "layer_direct.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "delta.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "ssm_scan.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     # these files' compile-time twiddle tables need more constexpr evaluation steps
     # than clang's default allows

@@ -52,29 +52,27 @@ struct DeltaBytes {
     }
 };
 
-// Buffers of the delta rule's chunks (each region 256-byte aligned): what the
-// forward pass needs by itself (X, P, the gates where nothing is kept), what
-// it leaves for the backward pass (the gates, both transposes, the errors and the
-// chunks' first states).
+// Buffers of the delta rule's chunks (each region 256-byte aligned): the forward
+// pass's records, keys and queries; what it leaves for the backward pass (records of the
+// transposes, errors, the chunks' first states, scales, keys and queries); the backward pass's scratch (z of every
+// token, the gradient of every chunk's last state, scales).
 struct DeltaWs {
-    size_t x, p, gates, xt, pt, es, states, dends, fwd, saved, bwd;
+    size_t kq, es, states, exps, kept_kq, dends, bexps, fwd, saved, bwd;
     DeltaWs(int B, int H, int L, int Dk, int Dv, int dtype) {
         const size_t ch = (size_t)B * H * ((L + kDeltaChunk - 1) / kDeltaChunk);
-        const size_t mat = align_up(ch * (dtype == H3_F32 ? 3 : 2) * kDeltaMatBytes);
-        const size_t back = align_up(ch * 3 * kDeltaMatBytes);   // X and the transposes: three pieces for every type
-        const size_t gb = align_up(ch * sizeof(ChunkGates));
-        x = 0;
-        p = back;
-        gates = p + mat;   // of the workspace, and at 0 of what is kept
-        fwd = gates + gb;
-        xt = gb;
-        pt = xt + back;
-        es = pt + back;
-        states = es + align_up(ch * kDeltaChunk * Dv * 4);
-        saved = states + align_up(ch * Dk * Dv * 4);
-        // the backward pass's workspace: z of every token, the gradient of every chunk's last state
-        dends = align_up(ch * kDeltaChunk * Dv * 4);
-        bwd = dends + align_up(ch * Dk * Dv * 4);
+        const size_t dkp = (Dk + 31) / 32 * 32, dvp = (Dv + 15) / 16 * 16;
+        const size_t rows = align_up(ch * kDeltaChunk * dvp * 4), state = align_up(ch * dkp * dvp * 4);
+        const size_t keys = align_up(ch * 2 * (dtype == H3_F32 ? 2 : 1) * kDeltaChunk * dkp * 2);
+        kq = align_up(ch * delta_rec_bytes(dtype == H3_BF16 ? 3 : 4));
+        fwd = kq + keys;
+        es = align_up(ch * delta_rec_bytes(4));
+        states = es + rows;
+        exps = states + state;
+        kept_kq = exps + align_up(ch * kDeltaTiles * sizeof(int2));
+        saved = kept_kq + keys;
+        dends = rows;
+        bexps = dends + state;
+        bwd = bexps + align_up(ch * kDeltaTiles * sizeof(int4));
     }
 };
 
@@ -681,14 +679,13 @@ int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, c
     DeltaArgs a{q, k, v, g, beta, lengths, S0, scale, B, L, H, Hk, Dk, Dv, (L + kDeltaChunk - 1) / kDeltaChunk};
     char *ws = (char *)workspace, *sv = (char *)saved;
     DeltaBuffers d{};
-    d.X = (uint4 *)(ws + w.x);
-    d.P = (uint4 *)(ws + w.p);
-    d.gates = (ChunkGates *)(sv ? sv : ws + w.gates);
+    d.rec = (uint4 *)ws;
+    d.kq = (uint4 *)(sv ? sv + w.kept_kq : ws + w.kq);
     if (sv) {
-        d.XT = (uint4 *)(sv + w.xt);
-        d.PT = (uint4 *)(sv + w.pt);
+        d.back = (uint4 *)sv;
         d.es = (float *)(sv + w.es);
         d.states = (float *)(sv + w.states);
+        d.exps = (int2 *)(sv + w.exps);
     }
     return launched(launch_delta_rule(a, dtype, d, o, S_final, (hipStream_t)stream));
 }
@@ -722,12 +719,12 @@ int h3_delta_rule_bwd(const void *q, const void *k, const void *v, const float *
     DeltaArgs a{q, k, v, g, beta, lengths, nullptr, scale, B, L, H, Hk, Dk, Dv, (L + kDeltaChunk - 1) / kDeltaChunk};
     char *ws = (char *)workspace, *sv = (char *)saved;
     DeltaBuffers d{};
-    d.gates = (ChunkGates *)sv;
-    d.XT = (uint4 *)(sv + w.xt);
-    d.PT = (uint4 *)(sv + w.pt);
+    d.back = (uint4 *)sv;
+    d.kq = (uint4 *)(sv + w.kept_kq);
     d.es = (float *)(sv + w.es);
     d.states = (float *)(sv + w.states);
-    DeltaGrads r{dout, dS, dq, dk, dv, dg, dbeta, dS0, (float *)ws, (float *)(ws + w.dends)};
+    d.exps = (int2 *)(sv + w.exps);
+    DeltaGrads r{dout, dS, dq, dk, dv, dg, dbeta, dS0, (float *)ws, (float *)(ws + w.dends), (int4 *)(ws + w.bexps)};
     return launched(launch_delta_rule_bwd(a, dtype, d, r, (hipStream_t)stream));
 }
 

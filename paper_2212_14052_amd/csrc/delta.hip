@@ -24,15 +24,16 @@ namespace {
 constexpr int AROW = DC + 4;   // floats a row of a 64 x 64 matrix in LDS
 
 template <int DT, int KS>
-__global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__restrict__ XF, uint4 *__restrict__ PF,
-                                                          uint4 *__restrict__ XTF, uint4 *__restrict__ PTF,
-                                                          ChunkGates *__restrict__ gates) {
+__global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__restrict__ rec, uint4 *__restrict__ back,
+                                                          uint4 *__restrict__ kq) {
     typedef typename IO<DT>::T T;
-    constexpr int NT = pieces<DT>(), NM = mat_pieces<DT>(), NX = kFullPieces;
-    __shared__ __attribute__((aligned(16))) uint16_t ks[NT * DC * lds_row<KS>()];
+    constexpr int NT = pieces<DT>(), NM = out_pieces<DT>(), NX = 2;
+    constexpr int KQ = kq_words<KS>(NT);
+    __shared__ uint4 ks[KQ];
     __shared__ __attribute__((aligned(16))) float A[DC * AROW], P[DC * AROW];
     __shared__ double gd[DC];
     __shared__ float be[DC];
+    __shared__ uint32_t red[2][4];
     const long ch = blockIdx.x;
     const int n = (int)(ch % a.N), h = (int)(ch / a.N % a.H), b = (int)(ch / a.N / a.H);
     const int nt = min(DC, tokens_of(a, b) - n * DC);   // tokens of this chunk
@@ -40,29 +41,91 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g4 = lane >> 4, c16 = lane & 15;
     const long tok0 = (long)b * a.L + n * DC;
     const int hk = h / (a.H / a.Hk);
+    uint4 *xf = rec + ch * ((NX + NM) * MAT + GATES), *pf = xf + NX * MAT;
+    uint4 *xt = back + ch * (2 * NX * MAT + GATES), *pt = xt + NX * MAT;
+    ChunkGates *gf = (ChunkGates *)(pf + NM * MAT), *gb = (ChunkGates *)(pt + NX * MAT);
+    const T *kp = (const T *)a.k + (tok0 * a.Hk + hk) * a.Dk, *qp = (const T *)a.q + (tok0 * a.Hk + hk) * a.Dk;
+    Raw8<DT> kr[KS], qr[KS];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+        const int it = i * 256 + tid, t = it / (4 * KS), c = 8 * (it % (4 * KS));
+        kr[i] = ld8_raw<DT>(kp + (long)min(t, nt - 1) * a.Hk * a.Dk + (c < a.Dk ? c : 0));
+        kr[i] = or_zero<DT>(kr[i], t < nt && c < a.Dk);
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {   // the left operand of row tile w
+        const int t = 16 * w + c16, c = 32 * s + 8 * g4;
+        qr[s] = ld8_raw<DT>(qp + (long)min(t, nt - 1) * a.Hk * a.Dk + (c < a.Dk ? c : 0));
+        qr[s] = or_zero<DT>(qr[s], t < nt && c < a.Dk);
+    }
     if (w == 0) {
         const bool on = lane < nt;
         const double x = decay_sum(on ? a.g[(tok0 + lane) * a.H + h] : 0.f, on, lane);
         const float bt = on ? a.beta[(tok0 + lane) * a.H + h] : 0.f;
         gd[lane] = x;
         be[lane] = bt;
-        gates[ch].from0[lane] = __builtin_amdgcn_exp2f((float)x);
-        gates[ch].toend[lane] = __builtin_amdgcn_exp2f((float)(__shfl(x, 63) - x));
-        gates[ch].beta[lane] = bt;
+        const float f = __builtin_amdgcn_exp2f((float)x), e = __builtin_amdgcn_exp2f((float)(__shfl(x, 63) - x));
+        gf->from0[lane] = f;
+        gf->toend[lane] = e;
+        gf->beta[lane] = bt;
+        // 2^et and 2^ef take every exp(G_63 - G_i) and exp(G_i) to at most 2
+        const int et = scale_exp(group_max<64>(__float_as_uint(e))) + 13, ef = scale_exp(group_max<64>(__float_as_uint(f))) + 13;
+        if (lane == 0) {
+            gf->et = et;
+            gf->ef = ef;
+        }
+        if (back) {
+            if (lane == 0) {
+                gb->et = et;
+                gb->ef = ef;
+            }
+            gb->from0[lane] = f;
+            gb->toend[lane] = e;
+            gb->beta[lane] = bt;
+        }
     }
-    const T *kp = (const T *)a.k, *qp = (const T *)a.q;
+    // the largest of two magnitudes over the workgroup
+    auto largest = [&](uint32_t x, uint32_t y) {
+        x = group_max<64>(x);
+        y = group_max<64>(y);
+        __syncthreads();
+        if (lane == 0) {
+            red[0][w] = x;
+            red[1][w] = y;
+        }
+        __syncthreads();
+        return make_int2(scale_exp(umax(umax(red[0][0], red[0][1]), umax(red[0][2], red[0][3]))),
+                         scale_exp(umax(umax(red[1][0], red[1][1]), umax(red[1][2], red[1][3]))));
+    };
+    int ek = 0, eq = 0;
+    if constexpr (DT != F16) {
+        uint32_t mk = 0, mq = 0;
 #pragma unroll
-    for (int i = 0; i < KS; ++i) {
-        const int it = i * 256 + tid, t = it / (4 * KS), c = 8 * (it % (4 * KS));
-        const Op<NT> o = op_of<DT>(ld8_raw<DT>(kp + ((tok0 + t) * a.Hk + hk) * a.Dk + c, t < nt && c < a.Dk));
-#pragma unroll
-        for (int p = 0; p < NT; ++p) *(uint4 *)(ks + (p * DC + t) * lds_row<KS>() + c) = o.p[p];
+        for (int i = 0; i < KS; ++i) {
+            mk = umax(mk, raw_mag<DT>(kr[i]));
+            mq = umax(mq, raw_mag<DT>(qr[i]));
+        }
+        const int2 e = largest(mk, mq);
+        ek = e.x;
+        eq = e.y;
     }
+    // the first value head of a key head leaves its keys and queries for the scans
+    uint4 *ki = h % (a.H / a.Hk) == 0 ? kq + (((long)b * a.Hk + hk) * a.N + n) * 2 * KQ : nullptr;
     Op<NT> qo[KS];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        const int t = 16 * w + c16, c = 32 * s + 8 * g4;
-        qo[s] = op_of<DT>(ld8_raw<DT>(qp + ((tok0 + t) * a.Hk + hk) * a.Dk + c, t < nt && c < a.Dk));
+    for (int i = 0; i < KS; ++i) {
+        const int it = i * 256 + tid, t = it / (4 * KS), c = it % (4 * KS);
+        const Op<NT> o = op_of<DT>(kr[i], pow2(-ek));
+        qo[i] = op_of<DT>(qr[i], pow2(-eq));
+#pragma unroll
+        for (int p = 0; p < NT; ++p) {
+            const int at = kq_block<KS>(p, t >> 4, c >> 2) * 64 + kq_place(t & 15, c & 3);
+            ks[at] = o.p[p];
+            if (ki) {
+                ki[at] = o.p[p];
+                ki[KQ + kq_block<KS>(p, w, i) * 64 + kq_place(c16, g4)] = qo[i].p[p];
+            }
+        }
     }
     __syncthreads();
     // row tile w of A and P
@@ -73,8 +136,8 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 const Op<NT> kj = lds_rows<NT, KS>(ks, j, s, lane);
-                ka = mm<NT, NT, input_products<DT>()>(lds_rows<NT, KS>(ks, w, s, lane), kj, ka);
-                pa = mm<NT, NT, input_products<DT>()>(qo[s], kj, pa);
+                ka = mm(lds_rows<NT, KS>(ks, w, s, lane), kj, ka);
+                pa = mm(qo[s], kj, pa);
             }
         }
         const int col = 16 * j + c16;
@@ -84,8 +147,8 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
             const int row = 16 * w + 4 * g4 + r;
             float f = 0.f;
             if (row >= col) f = __builtin_amdgcn_exp2f((float)(gd[row] - gj));
-            A[row * AROW + col] = row > col ? ka[r] * f : 0.f;
-            P[row * AROW + col] = row >= col ? pa[r] * f : 0.f;
+            A[row * AROW + col] = row > col ? __builtin_amdgcn_ldexpf(ka[r], 2 * ek) * f : 0.f;
+            P[row * AROW + col] = row >= col ? __builtin_amdgcn_ldexpf(pa[r], ek + eq) * f : 0.f;
         }
     }
     __syncthreads();
@@ -109,103 +172,97 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
         }
     }
     __syncthreads();
-    const long at = ch * NM * MAT, xat = ch * NX * MAT;
+    // the lower halves' fragments; the transposes for the backward pass
+    float xv[2][8], pv[2][8];
+    uint32_t mx = 0, mp = 0;
+    const int row = 16 * w + c16;
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int at = row * AROW + 32 * s + 4 * g4 + (j & 3) + 16 * (j >> 2);
+            xv[s][j] = A[at];
+            pv[s][j] = P[at];
+            mx = umax(mx, mag(xv[s][j]));
+            mp = umax(mp, mag(pv[s][j]));
+        }
+    const int2 em = largest(mx, mp);
+    const float sx = pow2(-em.x), sp = pow2(-em.y);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        const int row = 16 * w + c16, c0 = 32 * s + 4 * g4;
         if (s <= w / 2) {
             const int f = lower_frag(w, s) * FRAG + lane;
-            const float *ar = A + row * AROW + c0, *pr = P + row * AROW + c0;
-            const Op<NX> x = split8<NX>(*(const dl_f4 *)ar, *(const dl_f4 *)(ar + 16));
-            const Op<NM> p = split8<NM>(*(const dl_f4 *)pr, *(const dl_f4 *)(pr + 16));
+            const Op<NX> x = split8<NX>(xv[s], sx);
+            const Op<NM> p = split8<NM>(pv[s], sp);
 #pragma unroll
-            for (int i = 0; i < NX; ++i) XF[xat + i * MAT + f] = x.p[i];
+            for (int i = 0; i < NX; ++i) xf[i * MAT + f] = x.p[i];
 #pragma unroll
-            for (int i = 0; i < NM; ++i) PF[at + i * MAT + f] = p.p[i];
+            for (int i = 0; i < NM; ++i) pf[i * MAT + f] = p.p[i];
         }
-        if (XTF && s >= w / 2) {   // the transposes, for the backward pass
+        if (back && s >= w / 2) {
             const int f = upper_frag(w, s) * FRAG + lane;
-            float xt[8], pt[8];
+            float x[8], p[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int r = c0 + (j & 3) + 16 * (j >> 2);
-                xt[j] = A[r * AROW + row];
-                pt[j] = P[r * AROW + row];
+                const int at = (32 * s + 4 * g4 + (j & 3) + 16 * (j >> 2)) * AROW + row;
+                x[j] = A[at];
+                p[j] = P[at];
             }
-            const Op<NX> xo = split8<NX>(xt), po = split8<NX>(pt);
+            const Op<NX> xo = split8<NX>(x, sx), po = split8<NX>(p, sp);
 #pragma unroll
             for (int i = 0; i < NX; ++i) {
-                XTF[xat + i * MAT + f] = xo.p[i];
-                PTF[xat + i * MAT + f] = po.p[i];
+                xt[i * MAT + f] = xo.p[i];
+                pt[i * MAT + f] = po.p[i];
             }
+        }
+    }
+    if (tid == 0) {
+        gf->ek = ek;
+        gf->eq = eq;
+        gf->ex = em.x;
+        gf->ep = em.y;
+        if (back) {
+            gb->ek = ek;
+            gb->eq = eq;
+            gb->ex = em.x;
+            gb->ep = em.y;
         }
     }
 }
 
-// NW waves of 16 columns.  es, states: the chunks' errors (64, Dv) and first
-// states (Dk, Dv), for the backward pass, or null.
+// NW waves of 16 columns.  es, states, exps: for the backward pass, or null.
+//
+// A wave's vector instructions take longer than its matrix instructions here,
+// so scales cost nothing of their own: they ride on the rounding to pieces, on the
+// decays, or on a sum's multiplication.  The registers hold S 2^-E with one exponent
+// E for the wave, that of the last chunk's keys times errors, so that a chunk is
+// added in the same instruction that decays them.
 template <int DT, int KS, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, const uint4 *__restrict__ XF,
-                                                               const uint4 *__restrict__ PF,
-                                                               const ChunkGates *__restrict__ gates,
+__global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, const uint4 *__restrict__ rec,
+                                                               const uint4 *__restrict__ kq,
                                                                typename IO<DT>::T *__restrict__ o, float *S_final,
-                                                               float *__restrict__ es, float *__restrict__ states) {
+                                                               float *__restrict__ es, float *__restrict__ states,
+                                                               int2 *__restrict__ exps) {
     typedef typename IO<DT>::T T;
-    constexpr int NT = pieces<DT>(), NX = kFullPieces, NM = mat_pieces<DT>(), NO = DT == F32 ? 3 : 2;
-    typedef ScanLds<DT, KS, NW, kFullPieces + mat_pieces<DT>()> Lds;
-    // what a thread brings in: groups of eight channels of keys and of queries, 16-byte
-    // words of X and P, groups of eight values, words of the gates
-    constexpr int NTH = 64 * NW, ITEMS = 4 * KS / NW, WORDS = (NX + NM) * MAT, MATS = (WORDS + NTH - 1) / NTH, VALS = 2, GATES = (3 * DC + NTH - 1) / NTH;
-    static_assert(4 * KS % NW == 0 && DC * 2 * NW == VALS * NTH, "whole shares");
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    uint16_t *ks = (uint16_t *)(lds + Lds::k), *qs = (uint16_t *)(lds + Lds::q);
-    uint4 *ms = (uint4 *)(lds + Lds::mats);
-    T *vs = (T *)(lds + Lds::v);
-    ChunkGates *gt = (ChunkGates *)(lds + Lds::gates);
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g4 = lane >> 4, c16 = lane & 15;
-    const int tiles = (a.Dv + 16 * NW - 1) / (16 * NW);
+    constexpr int NT = pieces<DT>(), NX = 2, NO = out_pieces<DT>();
+    typedef ChunkCopy<DT, KS, NW, NX + NO> Copy;
+    typedef typename Copy::Lds Lds;
+    extern __shared__ uint4 lds[];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
+    const int tiles = (a.Dv + 16 * NW - 1) / (16 * NW), dvp = (a.Dv + 15) & ~15;
     const long bh = blockIdx.x / tiles;
     const int h = (int)(bh % a.H), b = (int)(bh / a.H), hk = h / (a.H / a.Hk);
-    const int c0 = ((int)(blockIdx.x % tiles) * NW + w) * 16;
-    const bool here = c0 < a.Dv;            // a wave without columns only helps to fetch
+    const int cb = (int)(blockIdx.x % tiles) * NW * 16, c0 = cb + 16 * w;   // first column of the workgroup, of the wave
+    const bool here = c0 < a.Dv;            // a wave without columns only helps to copy
     const int col = c0 + c16;
     const bool on = col < a.Dv, on4 = c0 + 4 * g4 < a.Dv;
     const int len = tokens_of(a, b), nb = (len + DC - 1) / DC;
-    const T *kp = (const T *)a.k, *qp = (const T *)a.q, *vp = (const T *)a.v;
-
-    Raw8<DT> pk[ITEMS], pq[ITEMS], pv[VALS];
-    uint4 pm[MATS];
-    float pg[GATES];
-    const int cb = c0 - 16 * w;   // the workgroup's first column
-    auto fetch = [&](int n) {
-        const long tok0 = (long)b * a.L + n * DC;
-        const int nt = len - n * DC;
-#pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const int it = i * 64 * NW + tid, t = it / (4 * KS), c = 8 * (it % (4 * KS));
-            const long at = ((tok0 + t) * a.Hk + hk) * a.Dk + c;
-            pk[i] = ld8_raw<DT>(kp + at, t < nt && c < a.Dk);
-            pq[i] = ld8_raw<DT>(qp + at, t < nt && c < a.Dk);
-        }
-#pragma unroll
-        for (int i = 0; i < VALS; ++i) {
-            const int it = i * NTH + tid, t = it / (2 * NW), c = cb + 8 * (it % (2 * NW));
-            pv[i] = ld8_raw<DT>(vp + ((tok0 + t) * a.H + h) * a.Dv + c, t < nt && c < a.Dv);
-        }
-        const long ch = bh * a.N + n;
-        const uint4 *xp = XF + ch * NX * MAT, *pp = PF + ch * NM * MAT;
-#pragma unroll
-        for (int i = 0; i < MATS; ++i) {
-            const int it = i * NTH + tid;
-            if (it < WORDS) pm[i] = it < NX * MAT ? xp[it] : pp[it - NX * MAT];
-        }
-        const float *gp = (const float *)(gates + ch);
-#pragma unroll
-        for (int i = 0; i < GATES; ++i)
-            if (i * NTH + tid < 3 * DC) pg[i] = gp[i * NTH + tid];
-    };
+    const Copy in{kq + ((long)b * a.Hk + hk) * a.N * 2 * Lds::kq, rec + bh * a.N * Lds::words,
+                  (const T *)a.v + ((long)b * a.L * a.H + h) * a.Dv + cb, (long)a.H * a.Dv, a.Dv - cb, len,
+                  (uint32_t)(uintptr_t)(dl_lds_void *)lds};
 
     dl_f4 S[2 * KS];
+    int E = 0;
 #pragma unroll
     for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
@@ -213,142 +270,186 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
             const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
             S[t][r] = a.S0 && on && dk < a.Dk ? a.S0[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
         }
-    if (nb > 0) fetch(0);
+    if (Lds::two && nb > 0) in.issue(0, w, lane);
     for (int n = 0; n < nb; ++n) {
         const int nt = min(DC, len - n * DC);
-        const long ch = bh * a.N + n, tok0 = (long)b * a.L + n * DC;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const int it = i * 64 * NW + tid, t = it / (4 * KS), c = 8 * (it % (4 * KS));
-            const Op<NT> ko = op_of<DT>(pk[i]), qo = op_of<DT>(pq[i]);
-#pragma unroll
-            for (int p = 0; p < NT; ++p) {
-                *(uint4 *)(ks + (p * DC + t) * lds_row<KS>() + c) = ko.p[p];
-                *(uint4 *)(qs + (p * DC + t) * lds_row<KS>() + c) = qo.p[p];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < VALS; ++i) {
-            const int it = i * NTH + tid;
-            T *p = vs + it / (2 * NW) * Lds::vrow + 8 * (it % (2 * NW));
-#pragma unroll
-            for (int j = 0; j < (DT == F32 ? 2 : 1); ++j) ((uint4 *)p)[j] = pv[i].a[j];
-        }
-#pragma unroll
-        for (int i = 0; i < MATS; ++i)
-            if (i * NTH + tid < WORDS) ms[i * NTH + tid] = pm[i];
-#pragma unroll
-        for (int i = 0; i < GATES; ++i)
-            if (i * NTH + tid < 3 * DC) ((float *)gt)[i * NTH + tid] = pg[i];
-        __syncthreads();
-        if (n + 1 < nb) fetch(n + 1);
+        const long ch = bh * a.N + n;
+        const uint4 *at = in.arrive(lds, n, n + 1, n + 1 < nb, w, lane);
         if (!here) continue;
-        if (states && on) {
+        const uint4 *ks = at + Lds::k, *qs = at + Lds::q, *xs = at + Lds::rec, *ps = xs + NX * MAT;
+        const T *vs = (const T *)(at + Lds::v);
+        const ChunkGates *gt = (const ChunkGates *)(ps + NO * MAT);
+        if (states) {
+            float *p = states + (ch * 32 * KS + 8 * g4) * dvp + col;
 #pragma unroll
             for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
-                    if (dk < a.Dk) states[(ch * a.Dk + dk) * a.Dv + col] = S[t][r];
+                for (int r = 0; r < 4; ++r) p[(32 * (t >> 1) + 4 * (t & 1) + r) * dvp] = __builtin_amdgcn_ldexpf(S[t][r], E);
+        }
+        const int ek = __builtin_amdgcn_readfirstlane(gt->ek), eq = __builtin_amdgcn_readfirstlane(gt->eq),
+                  ex = __builtin_amdgcn_readfirstlane(gt->ex), ep = __builtin_amdgcn_readfirstlane(gt->ep),
+                  et = __builtin_amdgcn_readfirstlane(gt->et);
+        // K S and, transposed (rows are columns of S, so that a lane will hold four
+        // consecutive values of one token), Q S
+        dl_f4 R[4], u[4], x[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) R[t] = x[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+        Op<NT> kf[2][4], qf[2][4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) kf[0][t] = lds_rows<NT, KS>(ks, t, 0, lane);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) qf[0][t] = lds_rows<NT, KS>(qs, t, 0, lane);
+        const int em = wave_exp(S), eS = em + E;   // of the registers, of S
+        const float sc = pow2(-em);
+        Op<NX> xo[6];
+        dl_f4 be[4], v[4], f0[4];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            if (s + 1 < KS) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) kf[(s + 1) & 1][t] = lds_rows<NT, KS>(ks, t, s + 1, lane);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) qf[(s + 1) & 1][t] = lds_rows<NT, KS>(qs, t, s + 1, lane);
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    f0[t] = *(const dl_f4 *)(gt->from0 + 16 * t + 4 * g4);
+                    be[t] = *(const dl_f4 *)(gt->beta + 16 * t + 4 * g4);
+                    v[t] = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * w, lane);
                 }
+#pragma unroll
+                for (int f = 0; f < 6; ++f) xo[f] = ld_frag<NX>(xs, f, lane);
+            }
+            in_order();
+            const Op<2> so = split8<2>(S[2 * s], S[2 * s + 1], sc);
+            Op<NO> sh;
+#pragma unroll
+            for (int p = 0; p < NO; ++p) sh.p[p] = so.p[p];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) R[t] = mm(kf[s & 1][t], so, R[t]);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) x[t] = mm(sh, qf[s & 1][t], x[t]);
+            in_order();
         }
         // R = V - exp(G) K S
-        Op<3> so[KS];
 #pragma unroll
-        for (int s = 0; s < KS; ++s) so[s] = split8<3>(S[2 * s], S[2 * s + 1]);
-        dl_f4 R[4], u[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) R[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-#pragma unroll
-            for (int t = 0; t < 4; ++t) R[t] = mm(lds_rows<NT, KS>(ks, t, s, lane), so[s], R[t]);
-        dl_f4 be[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const dl_f4 f = *(const dl_f4 *)(gt->from0 + 16 * t + 4 * g4);
-            be[t] = *(const dl_f4 *)(gt->beta + 16 * t + 4 * g4);
-            const dl_f4 v = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * w, lane);
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                R[t][r] = v[r] - f[r] * R[t][r];
+                R[t][r] = v[t][r] - __builtin_amdgcn_ldexpf(f0[t][r], ek + eS) * R[t][r];
                 u[t][r] = be[t][r] * R[t][r];
             }
-        }
         // e = R - X (beta R), u = beta e
+        const int er = wave_exp(u);
+        Op<NO> po[6];
+#pragma unroll
+        for (int f = 0; f < 6; ++f) po[f] = ld_frag<NO>(ps, f, lane);
+        in_order();
         {
             Op<NX> br[2];
+            dl_f4 y[4];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) br[s] = split8<NX>(u[2 * s], u[2 * s + 1]);
+            for (int s = 0; s < 2; ++s) br[s] = split8<NX>(u[2 * s], u[2 * s + 1], pow2(-er));
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                dl_f4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int s = 0; s <= t / 2; ++s) x = mm(ld_frag<NX>(ms, lower_frag(t, s), lane), br[s], x);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    R[t][r] -= x[r];
-                    u[t][r] = be[t][r] * R[t][r];
-                }
+                y[t] = mm(xo[lower_frag(t, 0)], br[0], dl_f4{0.f, 0.f, 0.f, 0.f});
+                if (t >= 2) y[t] = mm(xo[lower_frag(t, 1)], br[1], y[t]);
             }
-        }
-        if (es && on) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) es[(ch * DC + 16 * t + 4 * g4 + r) * a.Dv + col] = R[t][r];
-        }
-        // o, transposed: rows are columns of S, so that a lane holds four consecutive values of one token
-        {
-            Op<NO> uo[2], sh[KS];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) uo[s] = split8<NO>(u[2 * s], u[2 * s + 1]);
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-#pragma unroll
-                for (int p = 0; p < NO; ++p) sh[s].p[p] = so[s].p[p];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                dl_f4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int s = 0; s < KS; ++s) x = mm(sh[s], lds_rows<NT, KS>(qs, t, s, lane), x);
-                const float f = gt->from0[16 * t + c16];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] *= f;
-#pragma unroll
-                for (int s = 0; s <= t / 2; ++s) x = mm(uo[s], ld_frag<NM>(ms + NX * MAT, lower_frag(t, s), lane), x);
-                const int tt = 16 * t + c16;
-                if (on4 && n * DC + tt < a.L) {
-                    const bool real = tt < nt;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] = real ? x[r] * a.scale : 0.f;
-                    T *op = o + ((tok0 + tt) * a.H + h) * a.Dv + c0 + 4 * g4;
-                    if constexpr (DT == F32) *(float4 *)op = make_float4(x[0], x[1], x[2], x[3]);
-                    else *(uint2 *)op = make_uint2(pack_16x2<DT>(x[0], x[1]), pack_16x2<DT>(x[2], x[3]));
+                for (int r = 0; r < 4; ++r) {
+                    R[t][r] -= __builtin_amdgcn_ldexpf(y[t][r], er + ex);
+                    u[t][r] = be[t][r] * R[t][r];
                 }
-            }
         }
-        // S <- exp(G_63) S + K^T (exp(G_63 - G) u)
+        if (es) {
+            float *p = es + (ch * DC + 4 * g4) * dvp + col;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p[(16 * t + r) * dvp] = R[t][r];
+        }
+        const int eu = wave_exp(u);
+        if (exps && lane == 0) exps[ch * kDeltaTiles + c0 / 16] = make_int2(eu, max(min(eS, 114), -126));
+        Op<NT> kc[2][2];
+        dl_f4 te[4];
+        float fo[4];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) kc[0][s] = lds_cols<NT, KS>(ks, 0, s, lane);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            te[t] = *(const dl_f4 *)(gt->toend + 16 * t + 4 * g4);
+            fo[t] = gt->from0[16 * t + c16];
+        }
+        const float fl = gt->from0[DC - 1];
+        in_order();
+        // o = scale (exp(G) Q S + P u)
         {
-            Op<3> wo[2];
+            Op<NO> uo[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) uo[s] = split8<NO>(u[2 * s], u[2 * s + 1], pow2(-eu));
+            const float py = __builtin_amdgcn_ldexpf(a.scale, ep + eu);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const dl_f4 f = *(const dl_f4 *)(gt->toend + 16 * t + 4 * g4);
+                const float px = __builtin_amdgcn_ldexpf(fo[t] * a.scale, eq + eS);
+                dl_f4 y = mm(uo[0], po[lower_frag(t, 0)], dl_f4{0.f, 0.f, 0.f, 0.f});
+                if (t >= 2) y = mm(uo[1], po[lower_frag(t, 1)], y);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) u[t][r] *= f[r];
-            }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) wo[s] = split8<3>(u[2 * s], u[2 * s + 1]);
-            const float f = gt->from0[DC - 1];
-#pragma unroll
-            for (int t = 0; t < 2 * KS; ++t) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) S[t][r] *= f;
-#pragma unroll
-                for (int s = 0; s < 2; ++s) S[t] = mm(lds_cols<NT, KS>(ks, t, s, lane), wo[s], S[t]);
+                for (int r = 0; r < 4; ++r) x[t][r] = x[t][r] * px + y[r] * py;
             }
         }
+        if (nt < DC) {   // the last chunk: places behind the end are 0
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[t][r] = 16 * t + c16 < nt ? x[t][r] : 0.f;
+        }
+        const int room = a.L - n * DC;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            if (on4 && 16 * t + c16 < room) {
+                T *op = o + (((long)b * a.L + n * DC + 16 * t + c16) * a.H + h) * a.Dv + c0 + 4 * g4;
+                if constexpr (DT == F32) *(float4 *)op = make_float4(x[t][0], x[t][1], x[t][2], x[t][3]);
+                else *(uint2 *)op = make_uint2(pack_16x2<DT>(x[t][0], x[t][1]), pack_16x2<DT>(x[t][2], x[t][3]));
+            }
+        // S <- exp(G_63) S + K^T (exp(G_63 - G) u), in units of the keys' times the errors' scale;
+        // of 2^-60 of S where the errors are smaller than that
+        const int En = max(ek + eu + et, max(eS - 60, E - 100)), ew = En - ek;
+        const float fs = fl * pow2(max(E - En, -126)), sw = pow2(max(min(-ew, 127), -126));
+        E = En;
+        Op<2> wo[2];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) u[t][r] *= te[t][r];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) wo[s] = split8<2>(u[2 * s], u[2 * s + 1], sw);
+        dl_f4 y[2];   // summed from zero: added to S step by step, each step would round it
+#pragma unroll
+        for (int t = 0; t < 2 * KS; ++t) {
+            if (t + 1 < 2 * KS) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) kc[(t + 1) & 1][s] = lds_cols<NT, KS>(ks, t + 1, s, lane);
+            }
+            in_order();
+            y[t & 1] = dl_f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < 2; ++s) y[t & 1] = mm(kc[t & 1][s], wo[s], y[t & 1]);
+            if (t > 0) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[t - 1][r] = S[t - 1][r] * fs + y[(t - 1) & 1][r];
+            }
+            in_order();
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[2 * KS - 1][r] = S[2 * KS - 1][r] * fs + y[1][r];
+    }
+    if (on) {
+#pragma unroll
+        for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] = __builtin_amdgcn_ldexpf(S[t][r], E);
     }
     if (!here) return;
     // tokens of chunks behind the end
@@ -374,15 +475,14 @@ hipError_t fwd_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_f
     typedef typename IO<DT>::T T;
     constexpr int NW = 4;
     const long bh = (long)a.B * a.H;
-    delta_chunk_kernel<DT, KS><<<(unsigned)(bh * a.N), 256, 0, st>>>(a, w.X, w.P, w.XT, w.PT, w.gates);
+    delta_chunk_kernel<DT, KS><<<(unsigned)(bh * a.N), 256, 0, st>>>(a, w.rec, w.back, w.kq);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    constexpr int lds = ScanLds<DT, KS, NW, kFullPieces + mat_pieces<DT>()>::total;
+    constexpr int lds = ScanLds<DT, KS, NW, 2 + out_pieces<DT>()>::total;
     const int tiles = (a.Dv + 16 * NW - 1) / (16 * NW);
     if (lds > 65536)
         (void)hipFuncSetAttribute((const void *)delta_scan_kernel<DT, KS, NW>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    delta_scan_kernel<DT, KS, NW><<<(unsigned)(bh * tiles), 64 * NW, lds, st>>>(a, w.X, w.P, w.gates, (T *)o, S_final, w.es,
-                                                                               w.states);
+    delta_scan_kernel<DT, KS, NW><<<(unsigned)(bh * tiles), 64 * NW, lds, st>>>(a, w.rec, w.kq, (T *)o, S_final, w.es, w.states, w.exps);
     return hipGetLastError();
 }
 

@@ -1,14 +1,17 @@
 // What the kernels of the chunked gated delta rule share (delta.hip,
-// delta_bwd.hip): the chunk's matrices, operands cut into bf16 pieces, and
+// delta_bwd.hip): the chunk's matrices, operands cut into fp16 pieces, and
 // the layouts that the matrix cores' operands are kept in.
 //
 // Precision.  States, decays, sums and all results before their one rounding
-// are float32.  A float32 operand of a matrix product goes in as a sum of bf16
-// pieces, each the rounding of what is left: three hold all 24 bits, two are off by
-// 2^-16 at most; a product of pieces i and j is formed where i + j is below the
-// larger number of pieces (so two by two are off by 2^-15 at most, three by
-// three by 2^-22).  bf16 has float32's exponents, so no value needs a scale.  bf16 inputs are one piece,
-// fp16 inputs two, float32 inputs three, all exact.
+// are float32.  A float32 operand of a matrix product goes in as two fp16
+// pieces, the rounding and the rounding of what it leaves: 22 bits; of the four products
+// of pieces the smallest (2^-22 at most) is left out.  fp16 inputs are one piece
+// as they are.  Everything else is scaled by a power of two that takes the
+// largest value of its tile to 2^13 .. 2^14, so that nothing overflows and what
+// fp16 cannot hold is below 2^-38 of that largest value; bf16 inputs are then one
+// exact piece (down to 2^-31 of the largest).  Exponents are kept as integers
+// and undone in float32.  (Three bf16 pieces, which need no scales, cost 182
+// matrix instructions a chunk of 16 columns where these cost 104 to 132.)
 #pragma once
 #include "common.h"
 #include "internal.h"
@@ -17,15 +20,16 @@ namespace h3 {
 
 constexpr int DC = kDeltaChunk;
 
-typedef __bf16 dl_b8 __attribute__((ext_vector_type(8)));
+typedef _Float16 dl_h8 __attribute__((ext_vector_type(8)));
 typedef float dl_f4 __attribute__((ext_vector_type(4)));
 typedef short dl_s4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) dl_s4 dl_lds_s4;
+typedef __attribute__((address_space(3))) void dl_lds_void;
 
-// pieces of the inputs by type, and how far the products of two inputs are
-// taken (both pieces of fp16 are exact: all four)
-template <int DT> constexpr int pieces() { return DT == BF16 ? 1 : DT == F16 ? 2 : 3; }
-template <int DT> constexpr int input_products() { return DT == BF16 ? 1 : 3; }
+// pieces of the inputs by type
+template <int DT> constexpr int pieces() { return DT == F32 ? 2 : 1; }
+// pieces of what only a 16-bit output is made of: bf16 has 8 bits
+template <int DT> constexpr int out_pieces() { return DT == BF16 ? 1 : 2; }
 
 // an operand of eight values a lane in N pieces
 template <int N> struct Op {
@@ -33,11 +37,11 @@ template <int N> struct Op {
 };
 
 __device__ __forceinline__ dl_f4 dl_mfma(uint4 a, uint4 b, dl_f4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(dl_b8, a), __builtin_bit_cast(dl_b8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(dl_h8, a), __builtin_bit_cast(dl_h8, b), c, 0, 0, 0);
 }
-// c + a b, the smallest products first; N: how far products of pieces are taken
-template <int NA, int NB, int N = (NA > NB ? NA : NB)>
-__device__ __forceinline__ dl_f4 mm(const Op<NA> &a, const Op<NB> &b, dl_f4 c) {
+// c + a b, the smallest products first
+template <int NA, int NB> __device__ __forceinline__ dl_f4 mm(const Op<NA> &a, const Op<NB> &b, dl_f4 c) {
+    constexpr int N = NA > NB ? NA : NB;
 #pragma unroll
     for (int s = N - 1; s >= 0; --s)
 #pragma unroll
@@ -46,31 +50,59 @@ __device__ __forceinline__ dl_f4 mm(const Op<NA> &a, const Op<NB> &b, dl_f4 c) {
     return c;
 }
 
-// Two floats as N pieces, a word each: each the rounding of what the pieces
-// before it leave, so that piece n is at most 2^-8n of the value.
-template <int N> __device__ __forceinline__ void split2(float x, float y, uint32_t (&w)[N]) {
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-        w[n] = pack_16x2<BF16>(x, y);
-        x -= __uint_as_float(w[n] << 16);
-        y -= __uint_as_float(w[n] & 0xffff0000u);
-    }
+__device__ __forceinline__ float low_half(uint32_t w) { return f16_to_f32((uint16_t)(w & 0xffffu)); }
+__device__ __forceinline__ float high_half(uint32_t w) { return f16_to_f32((uint16_t)(w >> 16)); }
+
+// Two floats times a power of two as N pieces, a word each.  Written so that a
+// scale, a rounding or a remainder is one mixed-precision instruction.
+template <int N> __device__ __forceinline__ void split2(float x, float y, float s, uint32_t (&w)[N]) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    h2 h = {(_Float16)(x * s), (_Float16)(y * s)};
+    w[0] = __builtin_bit_cast(uint32_t, h);
+    if constexpr (N == 2) w[1] = pack_16x2<F16>(__builtin_fmaf(x, s, -(float)h.x), __builtin_fmaf(y, s, -(float)h.y));
 }
-template <int N> __device__ __forceinline__ Op<N> split8(const float (&x)[8]) {
+template <int N> __device__ __forceinline__ Op<N> split8(const float (&x)[8], float s) {
     Op<N> o;
     uint32_t w[4][N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) split2<N>(x[2 * i], x[2 * i + 1], w[i]);
+    for (int i = 0; i < 4; ++i) split2<N>(x[2 * i], x[2 * i + 1], s, w[i]);
 #pragma unroll
     for (int n = 0; n < N; ++n) o.p[n] = make_uint4(w[0][n], w[1][n], w[2][n], w[3][n]);
     return o;
 }
-template <int N> __device__ __forceinline__ Op<N> split8(dl_f4 a, dl_f4 b) {
+template <int N> __device__ __forceinline__ Op<N> split8(dl_f4 a, dl_f4 b, float s) {
     const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-    return split8<N>(x);
+    return split8<N>(x, s);
 }
 
-// Eight consecutive inputs as their pieces, or as floats; zeros where !on.
+// -------------------------------------------------------------- scales -----
+// The exponent e with largest 2^-e in 2^13 .. 2^14, from the largest magnitude's
+// bits; 0 for zero, Inf and NaN, -126 where 2^-e would leave float32.
+__device__ __forceinline__ int scale_exp(uint32_t bits) {
+    if (bits == 0 || bits >= 0x7f800000u) return 0;
+    const int e = (int)(bits >> 23) - 127 - 13;
+    return e < -126 ? -126 : e;
+}
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }   // -126 .. 127
+__device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+// the larger of m and the magnitudes of two values
+__device__ __forceinline__ float max3_abs(float m, float x, float y) {
+    asm("v_max3_f32 %0, %0, |%1|, |%2|" : "+v"(m) : "v"(x), "v"(y));
+    return m;
+}
+// the exponent for x of the whole wave
+template <int N> __device__ __forceinline__ int wave_exp(const dl_f4 (&x)[N]) {
+    float m = 0.f;
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+        m = max3_abs(m, x[t][0], x[t][1]);
+        m = max3_abs(m, x[t][2], x[t][3]);
+    }
+    return scale_exp(__builtin_amdgcn_readfirstlane(group_max<64>(__float_as_uint(m))));
+}
+
+// Eight consecutive inputs as floats; zeros where !on.
 template <int DT> __device__ __forceinline__ void ld8(const typename IO<DT>::T *p, bool on, float (&x)[8]) {
     if constexpr (DT == F32) {
         float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
@@ -82,36 +114,57 @@ template <int DT> __device__ __forceinline__ void ld8(const typename IO<DT>::T *
         const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            x[2 * i] = DT == BF16 ? bf16_to_f32(w[i] & 0xffffu) : f16_to_f32(w[i] & 0xffffu);
-            x[2 * i + 1] = DT == BF16 ? bf16_to_f32(w[i] >> 16) : f16_to_f32(w[i] >> 16);
+            x[2 * i] = DT == BF16 ? bf16_to_f32(w[i] & 0xffffu) : low_half(w[i]);
+            x[2 * i + 1] = DT == BF16 ? bf16_to_f32(w[i] >> 16) : high_half(w[i]);
         }
     }
+}
+__device__ __forceinline__ uint4 or_zero(uint4 x, bool on) {
+    return make_uint4(on ? x.x : 0u, on ? x.y : 0u, on ? x.z : 0u, on ? x.w : 0u);
 }
 // raw registers of eight inputs, fetched ahead of their use
 template <int DT> struct Raw8 {
     uint4 a[DT == F32 ? 2 : 1];
 };
-template <int DT> __device__ __forceinline__ Raw8<DT> ld8_raw(const typename IO<DT>::T *p, bool on) {
+template <int DT> __device__ __forceinline__ Raw8<DT> ld8_raw(const typename IO<DT>::T *p) {
     Raw8<DT> r;
 #pragma unroll
-    for (int i = 0; i < (DT == F32 ? 2 : 1); ++i) r.a[i] = on ? ((const uint4 *)p)[i] : make_uint4(0u, 0u, 0u, 0u);
+    for (int i = 0; i < (DT == F32 ? 2 : 1); ++i) r.a[i] = ((const uint4 *)p)[i];
     return r;
 }
-template <int DT> __device__ __forceinline__ Op<pieces<DT>()> op_of(const Raw8<DT> &r) {
-    if constexpr (DT == BF16) {
-        Op<1> o;
+template <int DT> __device__ __forceinline__ Raw8<DT> or_zero(Raw8<DT> r, bool on) {
+#pragma unroll
+    for (int i = 0; i < (DT == F32 ? 2 : 1); ++i) r.a[i] = or_zero(r.a[i], on);
+    return r;
+}
+template <int DT> __device__ __forceinline__ void raw_floats(const Raw8<DT> &r, float (&x)[8]) {
+    const uint32_t w[8] = {r.a[0].x, r.a[0].y, r.a[0].z, r.a[0].w, r.a[DT == F32].x, r.a[DT == F32].y, r.a[DT == F32].z, r.a[DT == F32].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (DT == F32) x[i] = __uint_as_float(w[i]);
+        else if constexpr (DT == BF16) x[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        else x[i] = i & 1 ? high_half(w[i / 2]) : low_half(w[i / 2]);
+    }
+}
+template <int DT> __device__ __forceinline__ uint32_t raw_mag(const Raw8<DT> &r) {
+    float x[8];
+    raw_floats<DT>(r, x);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = umax(m, mag(x[i]));
+    return m;
+}
+// its pieces, times scale (fp16: as it is)
+template <int DT> __device__ __forceinline__ Op<pieces<DT>()> op_of(const Raw8<DT> &r, float scale) {
+    Op<pieces<DT>()> o;
+    if constexpr (DT == F16) {
         o.p[0] = r.a[0];
-        return o;
     } else {
         float x[8];
-        const uint32_t *w = (const uint32_t *)&r;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (DT == F32) x[i] = __uint_as_float(w[i]);
-            else x[i] = f16_to_f32((uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu));
-        }
-        return split8<pieces<DT>()>(x);
+        raw_floats<DT>(r, x);
+        o = split8<pieces<DT>()>(x, scale);
     }
+    return o;
 }
 
 // ------------------------------------------------------------- layouts -----
@@ -131,20 +184,23 @@ template <int DT> __device__ __forceinline__ Op<pieces<DT>()> op_of(const Raw8<D
 // 64 lanes of 16 bytes, the two that hold only zeros left out, each piece for itself.
 constexpr int FRAG = 64;                 // uint4 a fragment
 constexpr int MAT = 6 * FRAG;            // uint4 a piece of a matrix
+constexpr int GATES = (int)sizeof(ChunkGates) / 16;
 constexpr int lower_frag(int t, int s) { return t < 2 ? t : 2 * t - 2 + s; }       // s <= t / 2
 constexpr int upper_frag(int t, int s) { return t < 2 ? 2 * t + s : 2 + t; }       // s >= t / 2
 
-// keys and queries of a chunk in LDS: [piece][token][channel], rows padded by
-// 16 bytes, which spreads a tile's 16 rows over the banks
-template <int KS> constexpr int lds_row() { return 32 * KS + 8; }   // elements
+// The keys (queries) of a chunk, in memory and in LDS alike: 1 KB blocks of 16
+// tokens by 32 channels, [piece][token block][channel block], in each the eight
+// channels 8 g of token n at 16-byte place 4 n + (g ^ n / 4).  Sixteen tokens of one
+// g are then on sixteen different places of a 256-byte bank row.
+template <int KS> constexpr int kq_block(int piece, int t, int s) { return (piece * 4 + t) * KS + s; }
+__device__ __forceinline__ int kq_place(int n, int g) { return 4 * n + (g ^ (n >> 2)); }
+template <int KS> constexpr int kq_words(int pieces) { return pieces * 4 * KS * 64; }   // uint4
 
 // the left operand of token rows 16 t .. + 15, channels 32 s .. + 31
-template <int NT, int KS>
-__device__ __forceinline__ Op<NT> lds_rows(const uint16_t *m, int t, int s, int lane) {
+template <int NT, int KS> __device__ __forceinline__ Op<NT> lds_rows(const uint4 *m, int t, int s, int lane) {
     Op<NT> o;
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-        o.p[n] = *(const uint4 *)(m + ((n * DC + 16 * t + (lane & 15)) * lds_row<KS>() + 32 * s + 8 * (lane >> 4)));
+    for (int n = 0; n < NT; ++n) o.p[n] = m[kq_block<KS>(n, t, s) * 64 + kq_place(lane & 15, lane >> 4)];
     return o;
 }
 // the left operand of the transpose: rows = channels of state tile T (or, with
@@ -152,15 +208,16 @@ __device__ __forceinline__ Op<NT> lds_rows(const uint16_t *m, int t, int s, int 
 // token order.  A transposing read gives lane j of 16 the four rows that lanes 4 i + c
 // address, at the j-th of the 16 columns that lanes c = 0 .. 3 address four at a time.
 template <int NT, int KS, bool STATE = true>
-__device__ __forceinline__ Op<NT> lds_cols(const uint16_t *m, int T, int s, int lane) {
-    const int c = lane & 3, row = 32 * s + 4 * (lane >> 4) + ((lane & 15) >> 2);
-    const int col = STATE ? 32 * (T >> 1) + 8 * c + 4 * (T & 1) : 16 * T + 4 * c;
+__device__ __forceinline__ Op<NT> lds_cols(const uint4 *m, int T, int s, int lane) {
+    const int c = lane & 3, row = 4 * (lane >> 4) + ((lane & 15) >> 2);   // and 16 rows on
+    const int g = STATE ? c : 2 * (T & 1) + (c >> 1), half = STATE ? T & 1 : c & 1;
+    const int at = kq_place(row, g) * 8 + 4 * half;   // 16-bit elements in a block
     Op<NT> o;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const uint16_t *p = m + ((n * DC + row) * lds_row<KS>() + col);
-        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((dl_lds_s4 *)p));
-        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((dl_lds_s4 *)(p + 16 * lds_row<KS>())));
+        const uint16_t *p = (const uint16_t *)m + at;
+        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((dl_lds_s4 *)(p + kq_block<KS>(n, 2 * s, T >> 1) * 512)));
+        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((dl_lds_s4 *)(p + kq_block<KS>(n, 2 * s + 1, T >> 1) * 512)));
         o.p[n] = make_uint4(lo.x, lo.y, hi.x, hi.y);
     }
     return o;
@@ -172,6 +229,8 @@ template <int N> __device__ __forceinline__ Op<N> ld_frag(const uint4 *m, int f,
     for (int n = 0; n < N; ++n) o.p[n] = m[n * MAT + f * FRAG + lane];
     return o;
 }
+// Nothing is moved over this point, so that what is asked for ahead of its use is.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
 // rows r0 .. r0 + 3 of this lane's column (c0 + lane % 16) of 16-bit or float32 values in LDS, r0 = a + 4 (lane / 16)
 template <int DT>
@@ -187,8 +246,8 @@ __device__ __forceinline__ dl_f4 lds_column4(const typename IO<DT>::T *m, int ro
         const uint32_t y[2] = {x.x, x.y};
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const uint16_t z = (uint16_t)(r & 1 ? y[r / 2] >> 16 : y[r / 2] & 0xffffu);
-            v[r] = DT == BF16 ? bf16_to_f32(z) : f16_to_f32(z);
+            if constexpr (DT == BF16) v[r] = __uint_as_float(r & 1 ? y[r / 2] & 0xffff0000u : y[r / 2] << 16);
+            else v[r] = r & 1 ? high_half(y[r / 2]) : low_half(y[r / 2]);
         }
     }
     return v;
@@ -220,20 +279,74 @@ __device__ __forceinline__ int tokens_of(const DeltaArgs &a, int b) {
     return n < 0 ? 0 : n > a.L ? a.L : n;
 }
 
-// Pieces of X and of the transposes that the backward pass reads: the states and the
-// gates' gradients are float32 (with X in two pieces beta's gradient was 1.3e-6 off).
-constexpr int kFullPieces = 3;
-// pieces of P, which only o is made of: 16-bit results need 16 bits of it
-template <int DT> constexpr int mat_pieces() { return DT == F32 ? 3 : 2; }
-
-// LDS of a workgroup of NW waves: keys and queries in pieces, two
-// triangular matrices of MP pieces together as fragments, its columns of V (or do) (rows padded by 16 bytes), the gates.
+// ---------------------------------------------- bringing in a scan's chunk ---
+// A workgroup of NW waves keeps in LDS a chunk's keys and queries, its record (MP
+// pieces of triangular matrices and the gates) and the workgroup's columns of V or
+// do.  All of it is copied from memory as it lies there, 1 KB an instruction, without
+// passing through registers, and, where two fit, while the chunk before is worked on.
+// Nothing is cleared: rows behind the end are copies of the last token (their beta
+// is 0, their rows of X and P are 0, and what they would output is not stored), columns behind
+// Dv copies of the first ones (not stored either).
 template <int DT, int KS, int NW, int MP> struct ScanLds {
-    static constexpr int vrow = 16 * NW + 16 / (int)sizeof(typename IO<DT>::T);
-    static constexpr int kq = pieces<DT>() * DC * lds_row<KS>() * 2;
-    static constexpr int k = 0, q = kq, mats = 2 * kq, v = mats + MP * MAT * 16,
-                         gates = v + DC * vrow * (int)sizeof(typename IO<DT>::T), total = gates + (int)sizeof(ChunkGates);
+    static constexpr int words = MP * MAT + GATES, kq = kq_words<KS>(pieces<DT>());   // uint4
+    static constexpr int vrow = 16 * NW, v16 = DC * vrow * (int)sizeof(typename IO<DT>::T) / 16;
+    static constexpr int k = 0, q = kq, v = 2 * kq, rec = v + v16, one = rec + words;
+    static constexpr bool two = 2 * one * 16 <= 160 * 1024;
+    static constexpr int total = (two ? 2 : 1) * one * 16;
     static_assert(total <= 160 * 1024, "LDS of a CU");
+};
+
+template <int DT, int KS, int NW, int MP> struct ChunkCopy {
+    typedef typename IO<DT>::T T;
+    typedef ScanLds<DT, KS, NW, MP> Lds;
+    const uint4 *kq, *rec;   // this key head's and this value head's chunks
+    const T *v;              // this value head's row of the first token, at the workgroup's first column
+    long vstride;            // elements from token to token
+    int cols, len;           // columns from there, tokens
+    uint32_t lds;
+
+    // 64 lanes of 16 bytes, lane i from base + off to the LDS address `to` + 16 i
+    static __device__ __forceinline__ void copy(const void *base, uint32_t off, uint32_t to) {
+        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, %2"
+                     :
+                     : "v"(off), "s"(__builtin_amdgcn_readfirstlane(to)), "s"(base)
+                     : "memory", "m0");
+    }
+    __device__ __forceinline__ void issue(int n, int w, int lane) const {
+        const uint32_t to = lds + (Lds::two ? (uint32_t)(n & 1) * Lds::one * 16 : 0u);
+        const uint4 *kn = kq + (long)n * 2 * Lds::kq, *rn = rec + (long)n * Lds::words;
+#pragma unroll
+        for (int i = 0; i < 2 * Lds::kq / (64 * NW); ++i)
+            copy(kn, ((i * NW + w) * 64 + lane) * 16, to + (Lds::k + (i * NW + w) * 64) * 16);
+        const T *vn = v + (long)n * DC * vstride;
+        const int last = min(DC, len - n * DC) - 1;
+        constexpr int VP = 16 / (int)sizeof(T), VR = Lds::vrow / VP;   // values, words a row
+#pragma unroll
+        for (int i = 0; i < Lds::v16 / (64 * NW); ++i) {
+            const int at = (i * NW + w) * 64 + lane, t = min(at / VR, last), c = VP * (at % VR);
+            copy(vn, (uint32_t)((t * vstride + (c < cols ? c : 0)) * sizeof(T)), to + (Lds::v + (i * NW + w) * 64) * 16);
+        }
+#pragma unroll
+        for (int i = 0; i < (Lds::words + 64 * NW - 1) / (64 * NW); ++i) {
+            const int at = (i * NW + w) * 64 + lane;
+            if (at < Lds::words) copy(rn, (uint32_t)at * 16, to + (Lds::rec + (i * NW + w) * 64) * 16);
+        }
+    }
+    // Chunk n is in LDS, for every wave, and chunk `next` (if `more`) under way.
+    __device__ __forceinline__ const uint4 *arrive(const uint4 *base, int n, int next, bool more, int w, int lane) const {
+        if constexpr (Lds::two) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (more) issue(next, w, lane);
+            return base + (n & 1) * Lds::one;
+        } else {
+            __syncthreads();
+            issue(n, w, lane);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            return base;
+        }
+    }
 };
 
 }  // namespace h3

@@ -173,7 +173,7 @@ hipError_t launch_delta_step(const void *q, const void *k, const void *v, const 
 
 // The gated delta rule over whole sequences, chunks of 64 tokens.
 constexpr int kDeltaChunk = 64;
-constexpr size_t kDeltaMatBytes = 6 * 1024;   // a bf16 piece of a triangular 64 x 64 matrix, 16 x 32 blocks of zeros left out
+constexpr size_t kDeltaMatBytes = 6 * 1024;   // a 16-bit piece of a triangular 64 x 64 matrix, 16 x 32 blocks of zeros left out
 struct DeltaArgs {
     const void *q, *k, *v;
     const float *g, *beta;
@@ -183,20 +183,30 @@ struct DeltaArgs {
     int B, L, H, Hk, Dk, Dv, N;   // N: chunks of a sequence
 };
 // What a chunk keeps beside its matrices: exp(G_i) from the chunk's start,
-// exp(G_63 - G_i) to its end, beta_i (0 behind the sequence's end).
+// exp(G_63 - G_i) to its end, beta_i (0 behind the sequence's end); the exponents
+// of the scales of keys, queries, X and P; 2^et and 2^ef: at least half the largest
+// exp(G_63 - G_i) and exp(G_i).
 struct ChunkGates {
     float from0[kDeltaChunk], toend[kDeltaChunk], beta[kDeltaChunk];
+    int ek, eq, ex, ep, et, ef, unused[2];
 };
-// Buffers of the chunks of every (b, h): operand fragments of X and P (64 x 64,
-// three bf16 pieces, P two for 16-bit types), of their transposes, the gates, the errors e (64,
-// Dv) and the first states (Dk, Dv).  The forward pass writes XT, PT, es and
-// states where they are given (all or none).
+// Buffers of the chunks of every (b, h).  rec: what a scan of the chunks reads
+// of each, delta_rec_bytes: operand fragments of X (64 x 64, two fp16 pieces)
+// and P (two, one for bf16), the gates.  back: the same of the transposes
+// (two pieces each) for the backward pass.  es (64, Dv padded to 16): the errors e;
+// states (Dk padded to 32, Dv padded to 16): the chunks' first states.  The forward pass
+// writes back, es, states and exps where they are given (all or none).
+constexpr size_t delta_rec_bytes(int pieces) { return pieces * kDeltaMatBytes + sizeof(ChunkGates); }
+// kq: the keys and queries of every chunk and key head (room for H heads) in the
+// layout that the matrix cores read.  exps: the exponents of the scales of beta e and of the first state, for every 16
+// columns.
+constexpr int kDeltaTiles = 16;   // 16 columns each, at most
 struct DeltaBuffers {
-    uint4 *X, *P, *XT, *PT;
-    ChunkGates *gates;
+    uint4 *rec, *back, *kq;
     float *es, *states;
+    int2 *exps;   // (chunks, kDeltaTiles)
 };
-// Its backward pass: zs (64, Dv) and dends (Dk, Dv) of every chunk are scratch.
+// Its backward pass: zs (as es) and dends (as states) of every chunk are scratch.
 // dS, dS0 may be null.
 struct DeltaGrads {
     const void *dout;
@@ -204,6 +214,7 @@ struct DeltaGrads {
     void *dq, *dk, *dv;
     float *dg, *dbeta, *dS0;
     float *zs, *dends;
+    int4 *exps;   // (chunks, kDeltaTiles): of beta z, of dends, of the output's gradient, unused
 };
 hipError_t launch_delta_rule_bwd(const DeltaArgs &a, int dtype, const DeltaBuffers &w, const DeltaGrads &d, hipStream_t s);
 hipError_t launch_delta_rule(const DeltaArgs &a, int dtype, const DeltaBuffers &w, void *o, float *S_final, hipStream_t s);
