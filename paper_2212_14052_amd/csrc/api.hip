@@ -53,18 +53,26 @@ struct DeltaBytes {
 };
 
 // Buffers of the delta rule's chunks (each region 256-byte aligned): the forward
-// pass's records, keys and queries; what it leaves for the backward pass (records of the
+// pass's records, keys and queries, segments' maps; what it leaves for the backward pass (records of the
 // transposes, errors, the chunks' first states, scales, keys and queries); the backward pass's scratch (z of every
-// token, the gradient of every chunk's last state, scales).
+// token, the gradient of every chunk's last state, scales, segments' maps).
 struct DeltaWs {
-    size_t kq, es, states, exps, kept_kq, dends, bexps, fwd, saved, bwd;
+    size_t kq, seg, es, states, exps, kept_kq, dends, bexps, bseg, fwd, saved, bwd, maps, ins;
+    int G, Ns;
     DeltaWs(int B, int H, int L, int Dk, int Dv, int dtype) {
         const size_t ch = (size_t)B * H * ((L + kDeltaChunk - 1) / kDeltaChunk);
         const size_t dkp = (Dk + 31) / 32 * 32, dvp = (Dv + 15) / 16 * 16;
         const size_t rows = align_up(ch * kDeltaChunk * dvp * 4), state = align_up(ch * dkp * dvp * 4);
         const size_t keys = align_up(ch * 2 * (dtype == H3_F32 ? 2 : 1) * kDeltaChunk * dkp * 2);
         kq = align_up(ch * delta_rec_bytes(dtype == H3_BF16 ? 3 : 4));
-        fwd = kq + keys;
+        const int N = (L + kDeltaChunk - 1) / kDeltaChunk;
+        G = delta_segments(B, H, N, Dk, Dv);
+        Ns = (N + G - 1) / G;
+        const size_t sgs = G > 1 ? (size_t)B * H * G : 0;
+        maps = align_up(sgs * dkp * (dvp + dkp) * 4);
+        ins = align_up(sgs * Dk * Dv * 4);
+        seg = kq + keys;
+        fwd = seg + maps + ins + align_up(sgs * 8 * 4);
         es = align_up(ch * delta_rec_bytes(4));
         states = es + rows;
         exps = states + state;
@@ -72,7 +80,11 @@ struct DeltaWs {
         saved = kept_kq + keys;
         dends = rows;
         bexps = dends + state;
-        bwd = bexps + align_up(ch * kDeltaTiles * sizeof(int4));
+        bseg = bexps + align_up(ch * kDeltaTiles * sizeof(int4));
+        bwd = bseg + maps + ins + align_up(sgs * 8 * 4);
+    }
+    DeltaSegments segments(char *at) const {
+        return DeltaSegments{G, Ns, (float *)at, (float *)(at + maps), (int *)(at + maps + ins)};
     }
 };
 
@@ -681,6 +693,7 @@ int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, c
     DeltaBuffers d{};
     d.rec = (uint4 *)ws;
     d.kq = (uint4 *)(sv ? sv + w.kept_kq : ws + w.kq);
+    d.seg = w.segments(ws + w.seg);
     if (sv) {
         d.back = (uint4 *)sv;
         d.es = (float *)(sv + w.es);
@@ -720,6 +733,7 @@ int h3_delta_rule_bwd(const void *q, const void *k, const void *v, const float *
     char *ws = (char *)workspace, *sv = (char *)saved;
     DeltaBuffers d{};
     d.back = (uint4 *)sv;
+    d.seg = w.segments(ws + w.bseg);
     d.kq = (uint4 *)(sv + w.kept_kq);
     d.es = (float *)(sv + w.es);
     d.states = (float *)(sv + w.states);

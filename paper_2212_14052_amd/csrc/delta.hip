@@ -16,6 +16,8 @@
 // registers for the whole sequence, and each product's result is, as it lies
 // in the registers, the right operand of the next.  The waves of a workgroup share
 // the chunk's keys and queries in LDS, fetched one chunk ahead.
+#include <math.h>
+
 #include "delta_common.h"
 
 namespace h3 {
@@ -237,8 +239,11 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
 // decays, or on a sum's multiplication.  The registers hold S 2^-E with one exponent
 // E for the wave, that of the last chunk's keys times errors, so that a chunk is
 // added in the same instruction that decays them.
-template <int DT, int KS, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, const uint4 *__restrict__ rec,
+//
+// Sequences may be cut into segments (see DeltaSegments).  With MAPS a workgroup
+// does not produce outputs but its segment's map from state to state.
+template <int DT, int KS, int NW, bool MAPS>
+__global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, DeltaSegments sg, const uint4 *__restrict__ rec,
                                                                const uint4 *__restrict__ kq,
                                                                typename IO<DT>::T *__restrict__ o, float *S_final,
                                                                float *__restrict__ es, float *__restrict__ states,
@@ -249,37 +254,41 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
     typedef typename Copy::Lds Lds;
     extern __shared__ uint4 lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
-    const int tiles = (a.Dv + 16 * NW - 1) / (16 * NW), dvp = (a.Dv + 15) & ~15;
-    const long bh = blockIdx.x / tiles;
-    const int h = (int)(bh % a.H), b = (int)(bh / a.H), hk = h / (a.H / a.Hk);
-    const int cb = (int)(blockIdx.x % tiles) * NW * 16, c0 = cb + 16 * w;   // first column of the workgroup, of the wave
-    const bool here = c0 < a.Dv;            // a wave without columns only helps to copy
+    const int dvp = (a.Dv + 15) & ~15;
+    const ScanPlace<NW, MAPS> at_(a, sg, blockIdx.x, w);
+    const long bh = at_.bh;
+    const int h = at_.h, b = at_.b, hk = h / (a.H / a.Hk), seg = at_.seg, cb = at_.cb, c0 = at_.c0;
+    const bool here = c0 < at_.width;       // a wave without columns only helps to copy
     const int col = c0 + c16;
-    const bool on = col < a.Dv, on4 = c0 + 4 * g4 < a.Dv;
+    const bool on = col < at_.width, on4 = c0 + 4 * g4 < at_.width;
     const int len = tokens_of(a, b), nb = (len + DC - 1) / DC;
+    const int first = seg * sg.Ns, last = min(first + sg.Ns, nb);   // chunks from, and before
+    if (MAPS && last >= nb) return;         // nothing starts behind it
     const Copy in{kq + ((long)b * a.Hk + hk) * a.N * 2 * Lds::kq, rec + bh * a.N * Lds::words,
-                  (const T *)a.v + ((long)b * a.L * a.H + h) * a.Dv + cb, (long)a.H * a.Dv, a.Dv - cb, len,
-                  (uint32_t)(uintptr_t)(dl_lds_void *)lds};
+                  (const T *)a.v + ((long)b * a.L * a.H + h) * a.Dv + (at_.unit ? 0 : cb), (long)a.H * a.Dv,
+                  a.Dv - (at_.unit ? 0 : cb), len, (uint32_t)(uintptr_t)(dl_lds_void *)lds};
 
     dl_f4 S[2 * KS];
     int E = 0;
+    const float *S0 = MAPS ? nullptr : sg.G > 1 ? sg.in + ((long)seg * a.B * a.H) * a.Dk * a.Dv : a.S0;
 #pragma unroll
     for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
-            S[t][r] = a.S0 && on && dk < a.Dk ? a.S0[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
+            S[t][r] = S0 && on && dk < a.Dk ? S0[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
+            if (MAPS && at_.unit && on && dk == col) S[t][r] = 1.f;
         }
-    if (Lds::two && nb > 0) in.issue(0, w, lane);
-    for (int n = 0; n < nb; ++n) {
+    if (Lds::two && first < last) in.issue(first, w, lane);
+    for (int n = first; n < last; ++n) {
         const int nt = min(DC, len - n * DC);
         const long ch = bh * a.N + n;
-        const uint4 *at = in.arrive(lds, n, n + 1, n + 1 < nb, w, lane);
+        const uint4 *at = in.arrive(lds, n, n + 1, n + 1 < last, w, lane);
         if (!here) continue;
         const uint4 *ks = at + Lds::k, *qs = at + Lds::q, *xs = at + Lds::rec, *ps = xs + NX * MAT;
         const T *vs = (const T *)(at + Lds::v);
         const ChunkGates *gt = (const ChunkGates *)(ps + NO * MAT);
-        if (states) {
+        if (!MAPS && states) {
             float *p = states + (ch * 32 * KS + 8 * g4) * dvp + col;
 #pragma unroll
             for (int t = 0; t < 2 * KS; ++t)
@@ -298,7 +307,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
 #pragma unroll
         for (int t = 0; t < 4; ++t) kf[0][t] = lds_rows<NT, KS>(ks, t, 0, lane);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) qf[0][t] = lds_rows<NT, KS>(qs, t, 0, lane);
+        for (int t = 0; t < (MAPS ? 0 : 4); ++t) qf[0][t] = lds_rows<NT, KS>(qs, t, 0, lane);
         const int em = wave_exp(S), eS = em + E;   // of the registers, of S
         const float sc = pow2(-em);
         Op<NX> xo[6];
@@ -309,13 +318,14 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
 #pragma unroll
                 for (int t = 0; t < 4; ++t) kf[(s + 1) & 1][t] = lds_rows<NT, KS>(ks, t, s + 1, lane);
 #pragma unroll
-                for (int t = 0; t < 4; ++t) qf[(s + 1) & 1][t] = lds_rows<NT, KS>(qs, t, s + 1, lane);
+                for (int t = 0; t < (MAPS ? 0 : 4); ++t) qf[(s + 1) & 1][t] = lds_rows<NT, KS>(qs, t, s + 1, lane);
             } else {
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     f0[t] = *(const dl_f4 *)(gt->from0 + 16 * t + 4 * g4);
                     be[t] = *(const dl_f4 *)(gt->beta + 16 * t + 4 * g4);
                     v[t] = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * w, lane);
+                    if (MAPS && at_.unit) v[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
                 }
 #pragma unroll
                 for (int f = 0; f < 6; ++f) xo[f] = ld_frag<NX>(xs, f, lane);
@@ -328,7 +338,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
 #pragma unroll
             for (int t = 0; t < 4; ++t) R[t] = mm(kf[s & 1][t], so, R[t]);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) x[t] = mm(sh, qf[s & 1][t], x[t]);
+            for (int t = 0; t < (MAPS ? 0 : 4); ++t) x[t] = mm(sh, qf[s & 1][t], x[t]);
             in_order();
         }
         // R = V - exp(G) K S
@@ -343,7 +353,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
         const int er = wave_exp(u);
         Op<NO> po[6];
 #pragma unroll
-        for (int f = 0; f < 6; ++f) po[f] = ld_frag<NO>(ps, f, lane);
+        for (int f = 0; f < (MAPS ? 0 : 6); ++f) po[f] = ld_frag<NO>(ps, f, lane);
         in_order();
         {
             Op<NX> br[2];
@@ -363,7 +373,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
                     u[t][r] = be[t][r] * R[t][r];
                 }
         }
-        if (es) {
+        if (!MAPS && es) {
             float *p = es + (ch * DC + 4 * g4) * dvp + col;
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -371,7 +381,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
                 for (int r = 0; r < 4; ++r) p[(16 * t + r) * dvp] = R[t][r];
         }
         const int eu = wave_exp(u);
-        if (exps && lane == 0) exps[ch * kDeltaTiles + c0 / 16] = make_int2(eu, max(min(eS, 114), -126));
+        if (!MAPS && exps && lane == 0) exps[ch * kDeltaTiles + c0 / 16] = make_int2(eu, max(min(eS, 114), -126));
         Op<NT> kc[2][2];
         dl_f4 te[4];
         float fo[4];
@@ -385,7 +395,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
         const float fl = gt->from0[DC - 1];
         in_order();
         // o = scale (exp(G) Q S + P u)
-        {
+        if constexpr (!MAPS) {
             Op<NO> uo[2];
 #pragma unroll
             for (int s = 0; s < 2; ++s) uo[s] = split8<NO>(u[2 * s], u[2 * s + 1], pow2(-eu));
@@ -399,7 +409,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
                 for (int r = 0; r < 4; ++r) x[t][r] = x[t][r] * px + y[r] * py;
             }
         }
-        if (nt < DC) {   // the last chunk: places behind the end are 0
+        if (!MAPS && nt < DC) {   // the last chunk: places behind the end are 0
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -407,7 +417,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
         }
         const int room = a.L - n * DC;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < (MAPS ? 0 : 4); ++t)
             if (on4 && 16 * t + c16 < room) {
                 T *op = o + (((long)b * a.L + n * DC + 16 * t + c16) * a.H + h) * a.Dv + c0 + 4 * g4;
                 if constexpr (DT == F32) *(float4 *)op = make_float4(x[t][0], x[t][1], x[t][2], x[t][3]);
@@ -445,21 +455,23 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
 #pragma unroll
         for (int r = 0; r < 4; ++r) S[2 * KS - 1][r] = S[2 * KS - 1][r] * fs + y[1][r];
     }
-    if (on) {
 #pragma unroll
-        for (int t = 0; t < 2 * KS; ++t)
+    for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][r] = __builtin_amdgcn_ldexpf(S[t][r], E);
-    }
+        for (int r = 0; r < 4; ++r) S[t][r] = __builtin_amdgcn_ldexpf(S[t][r], E);
     if (!here) return;
-    // tokens of chunks behind the end
+    if constexpr (MAPS) {
+        store_map<KS>(a, sg, at_, S, E, lane);
+        return;
+    }
+    // tokens of this segment's chunks behind the end
     if (on4)
-        for (int t = nb * DC + c16; t < a.L; t += 16) {
+        for (int t = max(first, nb) * DC + c16; t < min(a.L, (first + sg.Ns) * DC); t += 16) {
             T *op = o + (((long)b * a.L + t) * a.H + h) * a.Dv + c0 + 4 * g4;
             if constexpr (DT == F32) *(float4 *)op = make_float4(0.f, 0.f, 0.f, 0.f);
             else *(uint2 *)op = make_uint2(0u, 0u);
         }
-    if (on && S_final) {
+    if (on && S_final && (last == nb && (first < last || seg == 0))) {
 #pragma unroll
         for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
@@ -470,6 +482,87 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, con
     }
 }
 
+// The state in front of every segment from the segments' maps, in order (or the
+// gradient of the state behind each, in reverse): S <- F S + D, a wave for 16 columns.
+template <int KS>
+__global__ __launch_bounds__(64, 1) void delta_join_kernel(DeltaArgs a, DeltaSegments sg, const float *__restrict__ S0, bool back) {
+    const int lane = threadIdx.x, g4 = lane >> 4, c16 = lane & 15;
+    const int tiles = (a.Dv + 15) / 16, dvp = 16 * tiles, row = dvp + 32 * KS;
+    const long bh = blockIdx.x / tiles, n = (long)a.B * a.H;
+    const int col = (int)(blockIdx.x % tiles) * 16 + c16;
+    const bool on = col < a.Dv;
+    const int nb = (tokens_of(a, (int)(bh / a.H)) + DC - 1) / DC, segs = (nb + sg.Ns - 1) / sg.Ns;
+    dl_f4 S[2 * KS];
+#pragma unroll
+    for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
+            S[t][r] = S0 && on && dk < a.Dk ? S0[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
+        }
+    // the first one too: the result may go where it came from
+    float *to0 = sg.in + ((back ? max(segs, 1) - 1 : 0) * n + bh) * a.Dk * a.Dv + col;
+#pragma unroll
+    for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
+            if (on && dk < a.Dk) to0[(long)dk * a.Dv] = S[t][r];
+        }
+    for (int i = 0; i + 1 < segs; ++i) {
+        const int seg = back ? segs - 1 - i : i, to = back ? seg - 1 : seg + 1;
+        const float *m = sg.maps + (bh * sg.G + seg) * 32 * KS * row;
+        int ef = -126;
+        for (int j = 0; j < (a.Dk + 15) / 16; ++j) ef = max(ef, sg.exps[(bh * sg.G + seg) * 8 + j]);
+        const int es = wave_exp(S);
+        Op<2> so[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) so[s] = split8<2>(S[2 * s], S[2 * s + 1], pow2(-es));
+#pragma unroll
+        for (int t = 0; t < 2 * KS; ++t) {
+            const float *f = m + (long)(32 * (t >> 1) + 8 * (c16 >> 2) + 4 * (t & 1) + (c16 & 3)) * row + dvp + 8 * g4;
+            dl_f4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                float x[8];
+                ld8<F32>(f + 32 * s, 32 * s + 8 * g4 < a.Dk, x);
+                const Op<2> fo = split8<2>(x, pow2(-ef));
+                y = mm(fo, so[s], y);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
+                S[t][r] = __builtin_amdgcn_ldexpf(y[r], ef + es) + m[(long)dk * row + col];
+                if (on && dk < a.Dk) sg.in[(((long)to * n + bh) * a.Dk + dk) * a.Dv + col] = S[t][r];
+            }
+        }
+    }
+}
+
+}  // namespace
+
+// Segments of a sequence.  A wave takes about one time unit a chunk whatever else
+// runs, and the card holds 256 workgroups of a scan.  Cut into G segments, the
+// maps of G - 1 cost Dk more columns and no outputs (0.8 units a chunk), joining
+// them about 2 units each.
+int delta_segments(int B, int H, int N, int Dk, int Dv) {
+    const double bh = (double)B * H, v = col_tiles(Dv, 4), k = col_tiles(Dk, 4);
+    int best = 1;
+    double least = 0;
+    for (int G = 1; G <= 64 && 4 * G <= N; ++G) {
+        const double Ns = (N + G - 1) / G;
+        double t = ceil(bh * v * G / 256) * Ns;
+        if (G > 1) t += 0.8 * ceil(bh * (v + k) * (G - 1) / 256) * Ns + 2.0 * G + 8;
+        if (G == 1 || t < 0.95 * least) {
+            best = G;
+            least = t;
+        }
+    }
+    return best;
+}
+
+namespace {
+
 template <int DT, int KS>
 hipError_t fwd_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_final, hipStream_t st) {
     typedef typename IO<DT>::T T;
@@ -479,10 +572,19 @@ hipError_t fwd_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_f
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     constexpr int lds = ScanLds<DT, KS, NW, 2 + out_pieces<DT>()>::total;
-    const int tiles = (a.Dv + 16 * NW - 1) / (16 * NW);
-    if (lds > 65536)
-        (void)hipFuncSetAttribute((const void *)delta_scan_kernel<DT, KS, NW>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    delta_scan_kernel<DT, KS, NW><<<(unsigned)(bh * tiles), 64 * NW, lds, st>>>(a, w.rec, w.kq, (T *)o, S_final, w.es, w.states, w.exps);
+    const DeltaSegments sg = w.seg;
+    if (sg.G > 1) {
+        e = lds_room(delta_scan_kernel<DT, KS, NW, true>, lds);
+        if (e != hipSuccess) return e;
+        delta_scan_kernel<DT, KS, NW, true><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW) + col_tiles(a.Dk, NW))), 64 * NW, lds, st>>>(
+            a, sg, w.rec, w.kq, nullptr, nullptr, nullptr, nullptr, nullptr);
+        e = launch_delta_join(a, sg, a.S0, false, st);
+        if (e != hipSuccess) return e;
+    }
+    e = lds_room(delta_scan_kernel<DT, KS, NW, false>, lds);
+    if (e != hipSuccess) return e;
+    delta_scan_kernel<DT, KS, NW, false><<<(unsigned)(bh * sg.G * col_tiles(a.Dv, NW)), 64 * NW, lds, st>>>(
+        a, sg, w.rec, w.kq, (T *)o, S_final, w.es, w.states, w.exps);
     return hipGetLastError();
 }
 
@@ -496,6 +598,17 @@ template <int DT> hipError_t fwd_by(const DeltaArgs &a, const DeltaBuffers &w, v
 }
 
 }  // namespace
+
+hipError_t launch_delta_join(const DeltaArgs &a, const DeltaSegments &sg, const float *S0, bool back, hipStream_t st) {
+    const unsigned grid = (unsigned)((long)a.B * a.H * ((a.Dv + 15) / 16));
+    switch ((a.Dk + 31) / 32) {
+        case 1: delta_join_kernel<1><<<grid, 64, 0, st>>>(a, sg, S0, back); break;
+        case 2: delta_join_kernel<2><<<grid, 64, 0, st>>>(a, sg, S0, back); break;
+        case 3: delta_join_kernel<3><<<grid, 64, 0, st>>>(a, sg, S0, back); break;
+        default: delta_join_kernel<4><<<grid, 64, 0, st>>>(a, sg, S0, back);
+    }
+    return hipGetLastError();
+}
 
 hipError_t launch_delta_rule(const DeltaArgs &a, int dtype, const DeltaBuffers &w, void *o, float *S_final, hipStream_t s) {
     if (dtype == F32) return fwd_by<F32>(a, w, o, S_final, s);

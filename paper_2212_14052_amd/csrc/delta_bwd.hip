@@ -18,8 +18,8 @@
 namespace h3 {
 namespace {
 
-template <int DT, int KS, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a, const uint4 *__restrict__ rec,
+template <int DT, int KS, int NW, bool MAPS>
+__global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a, DeltaSegments sg, const uint4 *__restrict__ rec,
                                                                    const uint4 *__restrict__ kq, DeltaGrads d) {
     typedef typename IO<DT>::T T;
     constexpr int NT = pieces<DT>(), NM = 2;
@@ -27,37 +27,41 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
     typedef typename Copy::Lds Lds;
     extern __shared__ uint4 lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
-    const int tiles = (a.Dv + 16 * NW - 1) / (16 * NW), dvp = (a.Dv + 15) & ~15;
-    const long bh = blockIdx.x / tiles;
-    const int h = (int)(bh % a.H), b = (int)(bh / a.H), hk = h / (a.H / a.Hk);
-    const int cb = (int)(blockIdx.x % tiles) * NW * 16, c0 = cb + 16 * w;
-    const bool here = c0 < a.Dv;
+    const int dvp = (a.Dv + 15) & ~15;
+    const ScanPlace<NW, MAPS, true> at_(a, sg, blockIdx.x, w);
+    const long bh = at_.bh;
+    const int h = at_.h, b = at_.b, hk = h / (a.H / a.Hk), seg = at_.seg, cb = at_.cb, c0 = at_.c0;
+    const bool here = c0 < at_.width;
     const int col = c0 + c16;
-    const bool on = col < a.Dv;
+    const bool on = col < at_.width;
     const int len = tokens_of(a, b), nb = (len + DC - 1) / DC;
+    const int first = seg * sg.Ns, last = min(first + sg.Ns, nb);   // chunks from, and before
+    if (MAPS ? first >= last : first >= last && seg > 0) return;
     const Copy in{kq + ((long)b * a.Hk + hk) * a.N * 2 * Lds::kq, rec + bh * a.N * Lds::words,
-                  (const T *)d.dout + ((long)b * a.L * a.H + h) * a.Dv + cb, (long)a.H * a.Dv, a.Dv - cb, len,
-                  (uint32_t)(uintptr_t)(dl_lds_void *)lds};
+                  (const T *)d.dout + ((long)b * a.L * a.H + h) * a.Dv + (at_.unit ? 0 : cb), (long)a.H * a.Dv,
+                  a.Dv - (at_.unit ? 0 : cb), len, (uint32_t)(uintptr_t)(dl_lds_void *)lds};
 
     dl_f4 S[2 * KS];   // dS' 2^-E
     int E = 0;
+    const float *dS = MAPS ? nullptr : sg.G > 1 ? sg.in + ((long)seg * a.B * a.H) * a.Dk * a.Dv : d.dS;
 #pragma unroll
     for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
-            S[t][r] = d.dS && on && dk < a.Dk ? d.dS[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
+            S[t][r] = dS && on && dk < a.Dk ? dS[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
+            if (MAPS && at_.unit && on && dk == col) S[t][r] = 1.f;
         }
-    if (Lds::two && nb > 0) in.issue(nb - 1, w, lane);
-    for (int n = nb - 1; n >= 0; --n) {
+    if (Lds::two && first < last) in.issue(last - 1, w, lane);
+    for (int n = last - 1; n >= first; --n) {
         const long ch = bh * a.N + n;
-        const uint4 *at = in.arrive(lds, n, n - 1, n > 0, w, lane);
+        const uint4 *at = in.arrive(lds, n, n - 1, n > first, w, lane);
         if (!here) continue;
         const uint4 *ks = at + Lds::k, *qs = at + Lds::q, *xs = at + Lds::rec, *ps = xs + NM * MAT;   // X^T, P^T
         const T *vs = (const T *)(at + Lds::v);
         const ChunkGates *gt = (const ChunkGates *)(ps + NM * MAT);
         const int nt = min(DC, len - n * DC);
-        {
+        if constexpr (!MAPS) {
             float *p = d.dends + (ch * 32 * KS + 8 * g4) * dvp + col;
 #pragma unroll
             for (int t = 0; t < 2 * KS; ++t)
@@ -77,7 +81,10 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
             kf[0][t] = lds_rows<NT, KS>(ks, t, 0, lane);
         }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) dd[t] = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * w, lane);
+        for (int t = 0; t < 4; ++t) {
+            dd[t] = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * w, lane);
+            if (MAPS && at_.unit) dd[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+        }
         const int em = wave_exp(S), eS = em + E;   // of the registers, of dS'
         const float sc = pow2(-em);
 #pragma unroll
@@ -155,7 +162,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float z = u[t][r] - __builtin_amdgcn_ldexpf(x[r], eu + ex);
-                    p[(16 * t + r) * dvp] = z;
+                    if constexpr (!MAPS) p[(16 * t + r) * dvp] = z;
                     y[t][r] = be[t][r] * z;
                     u[t][r] = -f0[t][r] * y[t][r];
                     dd[t][r] *= f0[t][r] * a.scale;
@@ -163,7 +170,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
             }
         }
         const int ez = wave_exp(y), esc = scale_exp(mag(a.scale)) + 13;   // 2^esc: at most the scale
-        if (lane == 0) d.exps[ch * kDeltaTiles + c0 / 16] = make_int4(ez, max(min(eS, 114), -126), ed, 0);
+        if (!MAPS && lane == 0) d.exps[ch * kDeltaTiles + c0 / 16] = make_int4(ez, max(min(eS, 114), -126), ed, 0);
         // dS <- exp(G_63) dS' + Q^T (f do) - K^T (f y), both in units of the larger one's scale; of
         // 2^-60 of dS' where both are smaller than that
         const int En = max(max(ek + ez + ef, eq + ed + ef + esc + 1), max(eS - 60, E - 100));
@@ -201,13 +208,15 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
 #pragma unroll
         for (int r = 0; r < 4; ++r) S[2 * KS - 1][r] = S[2 * KS - 1][r] * fs + x[1][r];
     }
-    if (on) {
 #pragma unroll
-        for (int t = 0; t < 2 * KS; ++t)
+    for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][r] = __builtin_amdgcn_ldexpf(S[t][r], E);
+        for (int r = 0; r < 4; ++r) S[t][r] = __builtin_amdgcn_ldexpf(S[t][r], E);
+    if constexpr (MAPS) {
+        if (here) store_map<KS>(a, sg, at_, S, E, lane);
+        return;
     }
-    if (here && on && d.dS0) {
+    if (here && on && d.dS0 && seg == 0) {
 #pragma unroll
         for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
@@ -540,14 +549,19 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(DeltaArgs a, co
 template <int DT, int KS> hipError_t bwd_of(const DeltaArgs &a, const DeltaBuffers &w, const DeltaGrads &d, hipStream_t st) {
     constexpr int NW = 4;
     constexpr int lds = ScanLds<DT, KS, NW, 4>::total, lds2 = GradLds<DT, KS>::total;
-    if (lds > 65536)
-        (void)hipFuncSetAttribute((const void *)delta_bwd_scan_kernel<DT, KS, NW>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (lds2 > 65536)
-        (void)hipFuncSetAttribute((const void *)delta_bwd_chunk_kernel<DT, KS>, hipFuncAttributeMaxDynamicSharedMemorySize, lds2);
-    const int tiles = (a.Dv + 16 * NW - 1) / (16 * NW);
-    delta_bwd_scan_kernel<DT, KS, NW><<<(unsigned)((long)a.B * a.H * tiles), 64 * NW, lds, st>>>(a, w.back, w.kq, d);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    const DeltaSegments sg = w.seg;
+    const long bh = (long)a.B * a.H;
+    hipError_t e;
+    if (sg.G > 1) {
+        if ((e = lds_room(delta_bwd_scan_kernel<DT, KS, NW, true>, lds)) != hipSuccess) return e;
+        delta_bwd_scan_kernel<DT, KS, NW, true><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW) + col_tiles(a.Dk, NW))), 64 * NW, lds, st>>>(
+            a, sg, w.back, w.kq, d);
+        if ((e = launch_delta_join(a, sg, d.dS, true, st)) != hipSuccess) return e;
+    }
+    if ((e = lds_room(delta_bwd_scan_kernel<DT, KS, NW, false>, lds)) != hipSuccess) return e;
+    delta_bwd_scan_kernel<DT, KS, NW, false><<<(unsigned)(bh * sg.G * col_tiles(a.Dv, NW)), 64 * NW, lds, st>>>(a, sg, w.back, w.kq, d);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if ((e = lds_room(delta_bwd_chunk_kernel<DT, KS>, lds2)) != hipSuccess) return e;
     delta_bwd_chunk_kernel<DT, KS><<<(unsigned)((long)a.B * a.Hk * a.N), 256, lds2, st>>>(a, w.back, w.kq, w.es, w.states, w.exps, d);
     return hipGetLastError();
 }

@@ -349,4 +349,49 @@ template <int DT, int KS, int NW, int MP> struct ChunkCopy {
     }
 };
 
+// ---------------------------------------------------------------- segments ---
+// workgroups of NW waves of 16 columns
+constexpr int col_tiles(int cols, int NW) { return (cols + 16 * NW - 1) / (16 * NW); }
+
+// What a workgroup of a scan works on: a (b, h), a segment, its columns.  With MAPS
+// there are the columns of V from a zero state, and then the unit matrix's
+// from no values; no map is needed of the last segment (BACK: of the first).
+template <int NW, bool MAPS, bool BACK = false> struct ScanPlace {
+    long bh;
+    int b, h, seg, cb, c0, width;   // width: columns there are
+    bool unit;
+    __device__ __forceinline__ ScanPlace(const DeltaArgs &a, const DeltaSegments &sg, unsigned block, int w) {
+        const int v = col_tiles(a.Dv, NW), tiles = v + (MAPS ? col_tiles(a.Dk, NW) : 0), segs = sg.G - (MAPS ? 1 : 0);
+        const int tile = (int)(block % tiles);
+        seg = (int)(block / tiles % segs) + (MAPS && BACK ? 1 : 0);
+        bh = block / tiles / segs;
+        h = (int)(bh % a.H);
+        b = (int)(bh / a.H);
+        unit = tile >= v;
+        width = unit ? a.Dk : a.Dv;
+        cb = (unit ? tile - v : tile) * 16 * NW;
+        c0 = cb + 16 * w;
+    }
+};
+
+// S 2^E as columns of a segment's map: (32 KS, dvp + 32 KS) row-major, its
+// second part with the exponent of its scale for every 16 columns.
+template <int KS, typename P>
+__device__ __forceinline__ void store_map(const DeltaArgs &a, const DeltaSegments &sg, const P &at, const dl_f4 (&S)[2 * KS],
+                                          int E, int lane) {
+    const int dvp = (a.Dv + 15) & ~15, row = dvp + 32 * KS;
+    float *p = sg.maps + ((at.bh * sg.G + at.seg) * 32 * KS + 8 * (lane >> 4)) * row + (at.unit ? dvp : 0) + at.c0 + (lane & 15);
+#pragma unroll
+    for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[(32 * (t >> 1) + 4 * (t & 1) + r) * row] = S[t][r];
+    const int e = wave_exp(S);
+    if (at.unit && lane == 0) sg.exps[(at.bh * sg.G + at.seg) * 8 + at.c0 / 16] = e;
+}
+
+// dynamic LDS above 64 KB has to be asked for
+template <typename K> hipError_t lds_room(K *kernel, int bytes) {
+    return bytes > 65536 ? hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) : hipSuccess;
+}
+
 }  // namespace h3

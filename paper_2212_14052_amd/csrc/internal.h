@@ -200,11 +200,23 @@ constexpr size_t delta_rec_bytes(int pieces) { return pieces * kDeltaMatBytes + 
 // kq: the keys and queries of every chunk and key head (room for H heads) in the
 // layout that the matrix cores read.  exps: the exponents of the scales of beta e and of the first state, for every 16
 // columns.
+// A long sequence of few heads is cut into G segments of Ns chunks (the last may
+// have fewer): a segment maps the state S in front of it to F S + D; maps (b, h,
+// segment: Dk padded to 32 rows of D, Dv padded to 16, and F, Dk padded to 32) are formed
+// for all segments at once, joined in order to the states in front of the segments (in:
+// segment, b, h), and then all segments run at once.  exps: scales of F, every 16 columns.
+struct DeltaSegments {
+    int G, Ns;
+    float *maps, *in;
+    int *exps;
+};
+int delta_segments(int B, int H, int N, int Dk, int Dv);
 constexpr int kDeltaTiles = 16;   // 16 columns each, at most
 struct DeltaBuffers {
     uint4 *rec, *back, *kq;
     float *es, *states;
     int2 *exps;   // (chunks, kDeltaTiles)
+    DeltaSegments seg;
 };
 // Its backward pass: zs (as es) and dends (as states) of every chunk are scratch.
 // dS, dS0 may be null.
@@ -216,6 +228,8 @@ struct DeltaGrads {
     float *zs, *dends;
     int4 *exps;   // (chunks, kDeltaTiles): of beta z, of dends, of the output's gradient, unused
 };
+// back: from the last segment to the first
+hipError_t launch_delta_join(const DeltaArgs &a, const DeltaSegments &sg, const float *S0, bool back, hipStream_t s);
 hipError_t launch_delta_rule_bwd(const DeltaArgs &a, int dtype, const DeltaBuffers &w, const DeltaGrads &d, hipStream_t s);
 hipError_t launch_delta_rule(const DeltaArgs &a, int dtype, const DeltaBuffers &w, void *o, float *S_final, hipStream_t s);
 

@@ -116,6 +116,16 @@ def test_lengths(dtype):
     assert all((t[behind] == 0).all() for t in got[:5]) and torch.equal(got[5][1], dS[1])
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,L,H,Hk,Dk,Dv", [(1, 1300, 1, 1, 40, 72), (2, 1100, 2, 1, 64, 64)])
+def test_few_heads_long(B, L, H, Hk, Dk, Dv, dtype):
+    """Long sequences of few heads, which are worked on in segments."""
+    args = full_inputs(B, L, H, Hk, Dk, Dv, dtype, 8)
+    run_and_check(dtype, *args)
+    for n in (0, 60, L // 2):
+        run_and_check(dtype, *args, None, torch.tensor([n, L][:B], device="cuda", dtype=torch.int32))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_gates_at_their_ends(dtype):
     q, k, v, g, beta, S0, do, dS = full_inputs(2, 100, 2, 2, 32, 32, dtype, 3)

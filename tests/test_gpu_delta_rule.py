@@ -159,6 +159,29 @@ def test_continues_and_meets_the_step():
     assert (S1 - S).abs().max() <= off and (o3 - o2).abs().max() <= 8 * off
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,L,H,Hk,Dk,Dv", [(1, 2600, 1, 1, 40, 72), (2, 1500, 2, 1, 128, 128), (1, 1025, 3, 3, 8, 8)])
+def test_few_heads_long(B, L, H, Hk, Dk, Dv, dtype):
+    """Long sequences of few heads, which are worked on in segments: lengths that end in different ones."""
+    *args, S0 = inputs(B, L, H, Hk, Dk, Dv, dtype, 9)
+    run_and_check(dtype, *args, S0)
+    for n in (0, 60, L // 2, L - 65):
+        lengths = torch.tensor([n, L][:B], device="cuda", dtype=torch.int32)
+        run_and_check(dtype, *args, S0, None, lengths)
+
+
+def test_final_state_over_the_first_one():
+    """The C entry point's S_final may be S0's buffer, also where segments read and write it."""
+    q, k, v, g, beta, S0 = inputs(1, 2600, 2, 2, 64, 64, "bf16", 10)
+    o, S = h3.delta_rule(q, k, v, g, beta, S0=S0)
+    o2, ws = torch.empty_like(o), torch.empty(h3.workspace_size(h3.OP_DELTA, 1, 2, 2600, 64, 64, h3.BF16), dtype=torch.uint8, device="cuda")
+    p = lambda t: t.data_ptr()
+    assert h3.lib().h3_delta_rule(p(q), p(k), p(v), p(g), p(beta), p(S0), None, 0.125, 1, 2600, 2, 2, 64, 64, h3.BF16, p(o2),
+                                  p(S0), None, 0, p(ws), ws.numel(), torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(o2, o) and torch.equal(S0, S)
+
+
 def test_views_stream_workspace_and_out():
     q, k, v, g, beta, S0 = inputs(2, 130, 4, 4, 64, 64, "bf16", 7)
     want = h3.delta_rule(q, k, v, g, beta, S0=S0)
