@@ -23,7 +23,7 @@
 namespace h3 {
 namespace {
 
-constexpr int AROW = DC + 4;   // floats a row of a 64 x 64 matrix in LDS
+constexpr int AROW = DC + 4, TROW = 20;   // floats a row of a 64 x 64, a 16 x 16 matrix in LDS
 
 template <int DT, int KS>
 __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__restrict__ rec, uint4 *__restrict__ back,
@@ -31,10 +31,12 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
     typedef typename IO<DT>::T T;
     constexpr int NT = pieces<DT>(), NM = out_pieces<DT>(), NX = 2;
     constexpr int KQ = kq_words<KS>(NT);
-    __shared__ uint4 ks[KQ];
-    __shared__ __attribute__((aligned(16))) float A[DC * AROW], P[DC * AROW];
+    // the keys, then A and P in their place; the inverses of the diagonal blocks
+    __shared__ uint4 ks[KQ > 2 * DC * AROW / 4 ? KQ : 2 * DC * AROW / 4];
+    float *A = (float *)ks, *P = A + DC * AROW;
+    __shared__ __attribute__((aligned(16))) float inv[4][16 * TROW];
     __shared__ double gd[DC];
-    __shared__ float be[DC];
+    __shared__ __attribute__((aligned(16))) float be[DC];
     __shared__ uint32_t red[2][4];
     const long ch = blockIdx.x;
     const int n = (int)(ch % a.N), h = (int)(ch / a.N % a.H), b = (int)(ch / a.N / a.H);
@@ -131,17 +133,22 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
     }
     __syncthreads();
     // row tile w of A and P
+    dl_f4 ka[4], pa[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        dl_f4 ka = {0.f, 0.f, 0.f, 0.f}, pa = ka;
+        ka[j] = pa[j] = dl_f4{0.f, 0.f, 0.f, 0.f};
         if (j <= w) {
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 const Op<NT> kj = lds_rows<NT, KS>(ks, j, s, lane);
-                ka = mm(lds_rows<NT, KS>(ks, w, s, lane), kj, ka);
-                pa = mm(qo[s], kj, pa);
+                ka[j] = mm(lds_rows<NT, KS>(ks, w, s, lane), kj, ka[j]);
+                pa[j] = mm(qo[s], kj, pa[j]);
             }
         }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
         const int col = 16 * j + c16;
         const double gj = gd[col];
 #pragma unroll
@@ -149,30 +156,70 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
             const int row = 16 * w + 4 * g4 + r;
             float f = 0.f;
             if (row >= col) f = __builtin_amdgcn_exp2f((float)(gd[row] - gj));
-            A[row * AROW + col] = row > col ? __builtin_amdgcn_ldexpf(ka[r], 2 * ek) * f : 0.f;
-            P[row * AROW + col] = row >= col ? __builtin_amdgcn_ldexpf(pa[r], ek + eq) * f : 0.f;
+            A[row * AROW + col] = row > col ? __builtin_amdgcn_ldexpf(ka[j][r], 2 * ek) * f : 0.f;
+            P[row * AROW + col] = row >= col ? __builtin_amdgcn_ldexpf(pa[j][r], ek + eq) * f : 0.f;
         }
     }
     __syncthreads();
-    // X in place of A, row by row: x_i = A_i - sum_m<i A_im beta_m x_m, a column a lane
-    if (w == 0) {
-        float bx[DC];
+    // X = (I + A diag(beta))^-1 A by blocks of 16.  Wave w: the diagonal block w row
+    // by row, x_i = A_i - sum_m<i A_im beta_m x_m, a column a lane (four times over), and
+    // (I + A_ww diag(beta))^-1 = I - X_ww diag(beta).
+    {
+        float *D = A + 16 * w * (AROW + 1);
+        float bx[16];
 #pragma unroll
-        for (int i = 0; i < DC; ++i) {
-            float x[4] = {A[i * AROW + lane], 0.f, 0.f, 0.f};
+        for (int i = 0; i < 16; ++i) {
+            float x[4] = {D[i * AROW + c16], 0.f, 0.f, 0.f};
 #pragma unroll
             for (int m = 0; m < i; m += 4) {
-                const float4 am = *(const float4 *)(A + i * AROW + m);
-                x[0] -= am.x * bx[m];
-                if (m + 1 < i) x[1] -= am.y * bx[m + 1];
-                if (m + 2 < i) x[2] -= am.z * bx[m + 2];
-                if (m + 3 < i) x[3] -= am.w * bx[m + 3];
+                const dl_f4 am = *(const dl_f4 *)(D + i * AROW + m);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (m + j < i) x[j] -= am[j] * bx[m + j];
             }
             const float xi = (x[0] + x[1]) + (x[2] + x[3]);
-            A[i * AROW + lane] = xi;
-            bx[i] = be[i] * xi;
+            bx[i] = be[16 * w + i] * xi;
+            if (g4 == 0) {
+                D[i * AROW + c16] = xi;
+                inv[w][i * TROW + c16] = (i == c16 ? 1.f : 0.f) - xi * be[16 * w + c16];
+            }
         }
     }
+    __syncthreads();
+    // Wave J: the blocks under diagonal block J, X_IJ = (I + A_II diag(beta))^-1 (A_IJ - sum_{J <= M < I}
+    // A_IM diag(beta) X_MJ), float32 products whose results are, as they lie, the next right
+    // operands (summand 4 g + s in step s).  A is overwritten when all are done.
+    dl_f4 X[4], bX[4];
+#pragma unroll
+    for (int I = 0; I < 4; ++I) {
+        if (I < w) continue;
+        const float *AI = A + 16 * I * AROW + 16 * w + c16;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) X[I][r] = AI[(4 * g4 + r) * AROW];
+        if (I > w) {
+            dl_f4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int M = 0; M < I; ++M) {
+                if (M < w) continue;
+                const dl_f4 am = *(const dl_f4 *)(A + (16 * I + c16) * AROW + 16 * M + 4 * g4);
+#pragma unroll
+                for (int s = 0; s < 4; ++s) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(am[s], bX[M][s], sum, 0, 0, 0);
+            }
+            const dl_f4 rhs = X[I] - sum, ti = *(const dl_f4 *)(inv[I] + c16 * TROW + 4 * g4);
+            X[I] = dl_f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < 4; ++s) X[I] = __builtin_amdgcn_mfma_f32_16x16x4f32(ti[s], rhs[s], X[I], 0, 0, 0);
+        }
+        const dl_f4 bt = *(const dl_f4 *)(be + 16 * I + 4 * g4);
+        bX[I] = bt * X[I];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int I = 0; I < 4; ++I)
+        if (I > w) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) A[(16 * I + 4 * g4 + r) * AROW + 16 * w + c16] = X[I][r];
+        }
     __syncthreads();
     // the lower halves' fragments; the transposes for the backward pass
     float xv[2][8], pv[2][8];
@@ -483,58 +530,84 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
 }
 
 // The state in front of every segment from the segments' maps, in order (or the
-// gradient of the state behind each, in reverse): S <- F S + D, a wave for 16 columns.
+// gradient of the state behind each, in reverse): S <- F S + D.  A workgroup takes 16
+// columns, its four waves share the rows: each holds its part of the next map while
+// the states go round through LDS.
 template <int KS>
-__global__ __launch_bounds__(64, 1) void delta_join_kernel(DeltaArgs a, DeltaSegments sg, const float *__restrict__ S0, bool back) {
-    const int lane = threadIdx.x, g4 = lane >> 4, c16 = lane & 15;
+__global__ __launch_bounds__(256, 1) void delta_join_kernel(DeltaArgs a, DeltaSegments sg, const float *__restrict__ S0, bool back) {
+    constexpr int TW = (KS + 1) / 2;   // row tiles a wave
+    __shared__ dl_f4 st[2 * KS][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g4 = lane >> 4, c16 = lane & 15;
     const int tiles = (a.Dv + 15) / 16, dvp = 16 * tiles, row = dvp + 32 * KS;
     const long bh = blockIdx.x / tiles, n = (long)a.B * a.H;
     const int col = (int)(blockIdx.x % tiles) * 16 + c16;
     const bool on = col < a.Dv;
-    const int nb = (tokens_of(a, (int)(bh / a.H)) + DC - 1) / DC, segs = (nb + sg.Ns - 1) / sg.Ns;
-    dl_f4 S[2 * KS];
-#pragma unroll
-    for (int t = 0; t < 2 * KS; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
-            S[t][r] = S0 && on && dk < a.Dk ? S0[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
-        }
-    // the first one too: the result may go where it came from
-    float *to0 = sg.in + ((back ? max(segs, 1) - 1 : 0) * n + bh) * a.Dk * a.Dv + col;
-#pragma unroll
-    for (int t = 0; t < 2 * KS; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
-            if (on && dk < a.Dk) to0[(long)dk * a.Dv] = S[t][r];
-        }
-    for (int i = 0; i + 1 < segs; ++i) {
-        const int seg = back ? segs - 1 - i : i, to = back ? seg - 1 : seg + 1;
+    const int nb = (tokens_of(a, (int)(bh / a.H)) + DC - 1) / DC, segs = max((nb + sg.Ns - 1) / sg.Ns, 1);
+    float fx[TW][KS][8];
+    dl_f4 dx[TW];
+    int ef = 0;
+    auto fetch = [&](int seg) {
         const float *m = sg.maps + (bh * sg.G + seg) * 32 * KS * row;
-        int ef = -126;
+#pragma unroll
+        for (int j = 0; j < TW; ++j) {
+            const int t = w * TW + j;
+            if (t >= 2 * KS) break;
+            const float *f = m + (long)(32 * (t >> 1) + 8 * (c16 >> 2) + 4 * (t & 1) + (c16 & 3)) * row + dvp + 8 * g4;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) ld8<F32>(f + 32 * s, 32 * s + 8 * g4 < a.Dk, fx[j][s]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) dx[j][r] = m[(long)(32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r) * row + col];
+        }
+        ef = -126;
         for (int j = 0; j < (a.Dk + 15) / 16; ++j) ef = max(ef, sg.exps[(bh * sg.G + seg) * 8 + j]);
-        const int es = wave_exp(S);
+    };
+    auto put = [&](int seg, int t, dl_f4 x) {
+        st[t][lane] = x;
+        float *to = sg.in + (seg * n + bh) * a.Dk * a.Dv + col;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
+            if (on && dk < a.Dk) to[(long)dk * a.Dv] = x[r];
+        }
+    };
+    if (segs > 1) fetch(back ? segs - 1 : 0);
+    // the first state too: the last result may go where it came from
+#pragma unroll
+    for (int j = 0; j < TW; ++j) {
+        const int t = w * TW + j;
+        if (t >= 2 * KS) break;
+        dl_f4 x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
+            x[r] = S0 && on && dk < a.Dk ? S0[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
+        }
+        put(back ? segs - 1 : 0, t, x);
+    }
+    for (int i = 0; i + 1 < segs; ++i) {
+        const int seg = back ? segs - 1 - i : i;
+        __syncthreads();
+        dl_f4 S[2 * KS], y[TW];
+#pragma unroll
+        for (int t = 0; t < 2 * KS; ++t) S[t] = st[t][lane];
+        const int es = wave_exp(S), e = es + ef;
         Op<2> so[KS];
 #pragma unroll
         for (int s = 0; s < KS; ++s) so[s] = split8<2>(S[2 * s], S[2 * s + 1], pow2(-es));
 #pragma unroll
-        for (int t = 0; t < 2 * KS; ++t) {
-            const float *f = m + (long)(32 * (t >> 1) + 8 * (c16 >> 2) + 4 * (t & 1) + (c16 & 3)) * row + dvp + 8 * g4;
-            dl_f4 y = {0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < TW; ++j) {
+            y[j] = dl_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                float x[8];
-                ld8<F32>(f + 32 * s, 32 * s + 8 * g4 < a.Dk, x);
-                const Op<2> fo = split8<2>(x, pow2(-ef));
-                y = mm(fo, so[s], y);
-            }
+            for (int s = 0; s < KS; ++s) y[j] = mm(split8<2>(fx[j][s], pow2(-ef)), so[s], y[j]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
-                S[t][r] = __builtin_amdgcn_ldexpf(y[r], ef + es) + m[(long)dk * row + col];
-                if (on && dk < a.Dk) sg.in[(((long)to * n + bh) * a.Dk + dk) * a.Dv + col] = S[t][r];
-            }
+            for (int r = 0; r < 4; ++r) y[j][r] = __builtin_amdgcn_ldexpf(y[j][r], e) + dx[j][r];
+        }
+        if (i + 2 < segs) fetch(back ? seg - 1 : seg + 1);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < TW; ++j) {
+            if (w * TW + j >= 2 * KS) break;
+            put(back ? seg - 1 : seg + 1, w * TW + j, y[j]);
         }
     }
 }
@@ -602,10 +675,10 @@ template <int DT> hipError_t fwd_by(const DeltaArgs &a, const DeltaBuffers &w, v
 hipError_t launch_delta_join(const DeltaArgs &a, const DeltaSegments &sg, const float *S0, bool back, hipStream_t st) {
     const unsigned grid = (unsigned)((long)a.B * a.H * ((a.Dv + 15) / 16));
     switch ((a.Dk + 31) / 32) {
-        case 1: delta_join_kernel<1><<<grid, 64, 0, st>>>(a, sg, S0, back); break;
-        case 2: delta_join_kernel<2><<<grid, 64, 0, st>>>(a, sg, S0, back); break;
-        case 3: delta_join_kernel<3><<<grid, 64, 0, st>>>(a, sg, S0, back); break;
-        default: delta_join_kernel<4><<<grid, 64, 0, st>>>(a, sg, S0, back);
+        case 1: delta_join_kernel<1><<<grid, 256, 0, st>>>(a, sg, S0, back); break;
+        case 2: delta_join_kernel<2><<<grid, 256, 0, st>>>(a, sg, S0, back); break;
+        case 3: delta_join_kernel<3><<<grid, 256, 0, st>>>(a, sg, S0, back); break;
+        default: delta_join_kernel<4><<<grid, 256, 0, st>>>(a, sg, S0, back);
     }
     return hipGetLastError();
 }
