@@ -335,7 +335,7 @@ int h3_delta_step(const void *q, const void *k, const void *v, const float *g, c
  *   nothing that is written overlaps anything.
  * States, gates and sums are float32, differences of summed log decays
  * float64; a NaN or Inf may reach every token of its chunk of 64.
- * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, 2^31 chunks), EWORKSPACE, EDEVICE.
+ * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, 2^31 chunks, H Dv > 2^22), EWORKSPACE, EDEVICE.
  */
 int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, const float *beta, const float *S0,
                   const int *lengths, float scale, int B, int L, int H, int Hk, int Dk, int Dv, int dtype, void *o,
@@ -355,7 +355,7 @@ int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, c
  *               Gradients of tokens from lengths[b] on are 0.
  *   workspace   >= h3_workspace_size(H3_OP_DELTA_BWD, B, H, L, Dk, Dv, dtype).
  * Nothing else that is written overlaps anything.  Results do not depend on timing.
- * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, 2^31 chunks), EWORKSPACE, EDEVICE.
+ * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, 2^31 chunks, H Dv > 2^22), EWORKSPACE, EDEVICE.
  */
 int h3_delta_rule_bwd(const void *q, const void *k, const void *v, const float *g, const float *beta, const void *dout,
                       const float *dS, const void *saved, size_t saved_bytes, const int *lengths, float scale, int B, int L,

@@ -36,9 +36,10 @@ int launched(hipError_t e) { return e == hipSuccess ? H3_OK : H3_EDEVICE; }
 bool delta_sizes_ok(int Dk, int Dv) {
     return Dk >= 8 && Dk % 8 == 0 && Dk <= H3_DELTA_MAX_DK && Dv >= 8 && Dv % 8 == 0 && Dv <= H3_DELTA_MAX_DV;
 }
-// its launches hold one workgroup a chunk: at most 2^31 - 1
+// its launches hold one workgroup a chunk: at most 2^31 - 1; offsets inside a
+// chunk are 32 bits
 bool delta_chunks_ok(int B, int L, int H, int Dv) {
-    return (double)B * H * ((L + kDeltaChunk - 1) / kDeltaChunk) < 2147483647.0 && (double)B * H * ((Dv + 15) / 16) < 2147483647.0;
+    return (double)H * Dv <= 4194304.0 && (double)B * H * ((L + kDeltaChunk - 1) / kDeltaChunk) < 2147483647.0 && (double)B * H * ((Dv + 15) / 16) < 2147483647.0;
 }
 // bytes of its tensors: q or k, v or o, g or beta, a state for each head
 struct DeltaBytes {

@@ -301,7 +301,6 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
     typedef typename Copy::Lds Lds;
     extern __shared__ uint4 lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
-    const int dvp = (a.Dv + 15) & ~15;
     const ScanPlace<NW, MAPS> at_(a, sg, blockIdx.x, w);
     const long bh = at_.bh;
     const int h = at_.h, b = at_.b, hk = h / (a.H / a.Hk), seg = at_.seg, cb = at_.cb, c0 = at_.c0;
@@ -336,11 +335,14 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
         const T *vs = (const T *)(at + Lds::v);
         const ChunkGates *gt = (const ChunkGates *)(ps + NO * MAT);
         if (!MAPS && states) {
-            float *p = states + (ch * 32 * KS + 8 * g4) * dvp + col;
+            dl_f4 *p = (dl_f4 *)states + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;
 #pragma unroll
-            for (int t = 0; t < 2 * KS; ++t)
+            for (int t = 0; t < 2 * KS; ++t) {
+                dl_f4 y;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) p[(32 * (t >> 1) + 4 * (t & 1) + r) * dvp] = __builtin_amdgcn_ldexpf(S[t][r], E);
+                for (int r = 0; r < 4; ++r) y[r] = __builtin_amdgcn_ldexpf(S[t][r], E);
+                p[t * 64] = y;
+            }
         }
         const int ek = __builtin_amdgcn_readfirstlane(gt->ek), eq = __builtin_amdgcn_readfirstlane(gt->eq),
                   ex = __builtin_amdgcn_readfirstlane(gt->ex), ep = __builtin_amdgcn_readfirstlane(gt->ep),
@@ -421,11 +423,9 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
                 }
         }
         if (!MAPS && es) {
-            float *p = es + (ch * DC + 4 * g4) * dvp + col;
+            dl_f4 *p = (dl_f4 *)es + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 4 * 64 + lane;
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) p[(16 * t + r) * dvp] = R[t][r];
+            for (int t = 0; t < 4; ++t) p[t * 64] = R[t];
         }
         const int eu = wave_exp(u);
         if (!MAPS && exps && lane == 0) exps[ch * kDeltaTiles + c0 / 16] = make_int2(eu, max(min(eS, 114), -126));
@@ -463,10 +463,11 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
                 for (int r = 0; r < 4; ++r) x[t][r] = 16 * t + c16 < nt ? x[t][r] : 0.f;
         }
         const int room = a.L - n * DC;
+        T *oc = o + (((long)b * a.L + n * DC) * a.H + h) * a.Dv + c0;
 #pragma unroll
         for (int t = 0; t < (MAPS ? 0 : 4); ++t)
             if (on4 && 16 * t + c16 < room) {
-                T *op = o + (((long)b * a.L + n * DC + 16 * t + c16) * a.H + h) * a.Dv + c0 + 4 * g4;
+                T *op = oc + (uint32_t)((16 * t + c16) * a.H * a.Dv + 4 * g4);
                 if constexpr (DT == F32) *(float4 *)op = make_float4(x[t][0], x[t][1], x[t][2], x[t][3]);
                 else *(uint2 *)op = make_uint2(pack_16x2<DT>(x[t][0], x[t][1]), pack_16x2<DT>(x[t][2], x[t][3]));
             }

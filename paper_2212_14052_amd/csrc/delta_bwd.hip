@@ -27,7 +27,6 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
     typedef typename Copy::Lds Lds;
     extern __shared__ uint4 lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
-    const int dvp = (a.Dv + 15) & ~15;
     const ScanPlace<NW, MAPS, true> at_(a, sg, blockIdx.x, w);
     const long bh = at_.bh;
     const int h = at_.h, b = at_.b, hk = h / (a.H / a.Hk), seg = at_.seg, cb = at_.cb, c0 = at_.c0;
@@ -62,11 +61,14 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
         const ChunkGates *gt = (const ChunkGates *)(ps + NM * MAT);
         const int nt = min(DC, len - n * DC);
         if constexpr (!MAPS) {
-            float *p = d.dends + (ch * 32 * KS + 8 * g4) * dvp + col;
+            dl_f4 *p = (dl_f4 *)d.dends + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;
 #pragma unroll
-            for (int t = 0; t < 2 * KS; ++t)
+            for (int t = 0; t < 2 * KS; ++t) {
+                dl_f4 y;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) p[(32 * (t >> 1) + 4 * (t & 1) + r) * dvp] = __builtin_amdgcn_ldexpf(S[t][r], E);
+                for (int r = 0; r < 4; ++r) y[r] = __builtin_amdgcn_ldexpf(S[t][r], E);
+                p[t * 64] = y;
+            }
         }
         const int ek = __builtin_amdgcn_readfirstlane(gt->ek), eq = __builtin_amdgcn_readfirstlane(gt->eq),
                   ex = __builtin_amdgcn_readfirstlane(gt->ex), ep = __builtin_amdgcn_readfirstlane(gt->ep),
@@ -153,17 +155,19 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
             Op<NM> bu[2];
 #pragma unroll
             for (int s = 0; s < 2; ++s) bu[s] = split8<NM>(y[2 * s], y[2 * s + 1], pow2(-eu));
-            float *p = d.zs + (ch * DC + 4 * g4) * dvp + col;
+            dl_f4 *p = (dl_f4 *)d.zs + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 4 * 64 + lane;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 dl_f4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int s = t / 2; s < 2; ++s) x = mm(xf[upper_frag(t, s)], bu[s], x);
+                dl_f4 z;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) z[r] = u[t][r] - __builtin_amdgcn_ldexpf(x[r], eu + ex);
+                if constexpr (!MAPS) p[t * 64] = z;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float z = u[t][r] - __builtin_amdgcn_ldexpf(x[r], eu + ex);
-                    if constexpr (!MAPS) p[(16 * t + r) * dvp] = z;
-                    y[t][r] = be[t][r] * z;
+                    y[t][r] = be[t][r] * z[r];
                     u[t][r] = -f0[t][r] * y[t][r];
                     dd[t][r] *= f0[t][r] * a.scale;
                 }
@@ -229,199 +233,272 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
 
 constexpr int AROW = DC + 4;   // floats a row of a 64 x 64 matrix in LDS
 
+// LDS of delta_bwd_chunk_kernel, in 16-byte words: first 32 columns at a time of the states, of y and u, and of do,
+// then keys, queries, D and E in the same place.
 template <int DT, int KS> struct GradLds {
-    static constexpr int kq = kq_words<KS>(pieces<DT>());
-    static constexpr int k = 0, q = kq * 16, D = 2 * kq * 16, E = D + DC * AROW * 4, gd = E + DC * AROW * 4, gates = gd + DC * 8,
-                         red = gates + (int)sizeof(ChunkGates), total = red + (4 * DC + 16) * 4;
+    static constexpr int NT = pieces<DT>();
+    static constexpr int S = 0, dS = S + 4 * KS * 64, y = dS + 4 * KS * 64, u = y + 8 * 64, o = u + 8 * 64, stage = o + NT * 4 * 64;
+    static constexpr int kq = kq_words<KS>(NT), k = 0, q = kq, D = 2 * kq, E = D + DC * AROW / 4, after = E + DC * AROW / 4;
+    static constexpr int rest = stage > after ? stage : after;
+    static constexpr int gd = rest, gates = gd + DC / 2, red = gates + GATES, rin = red + DC, big = rin + 2, total = (big + 2) * 16;
     static_assert(total <= 160 * 1024, "LDS of a CU");
 };
 
 // A workgroup of four waves takes a chunk of a key head and goes through the
-// value heads that share it.  Every wave has KS / 2 (rounded up) of the key channels' tiles
-// for all tokens: results are transposed (rows are channels), so that a lane
-// holds four consecutive channels of one token.
-template <int DT, int KS>
-__global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(DeltaArgs a, const uint4 *__restrict__ rec,
-                                                              const uint4 *__restrict__ kq,
-                                                              const float *__restrict__ es,
-                                                              const float *__restrict__ states,
-                                                              const int2 *__restrict__ exps, DeltaGrads d) {
+// value heads that share it (ONE: there is one).  It brings in, 32 columns at a time, the
+// states, z and e of a chunk as the scans left them, cuts them into pieces once for all
+// waves, and reads operands whose summands are columns with transposing reads.  Every wave
+// has KS / 2 (rounded up) of the key channels' tiles for all tokens: results are transposed
+// (rows are channels), so that a lane holds four consecutive channels of one token; and a row tile
+// of D and E.
+//
+// Bound by HBM: the states alone are as many bytes as the chunk's inputs and
+// gradients together.
+template <int DT, int KS, bool ONE>
+__global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
+    DeltaArgs a, const uint4 *__restrict__ rec, const uint4 *__restrict__ kq, const float *__restrict__ es,
+    const float *__restrict__ states, const int2 *__restrict__ exps, DeltaGrads d) {
     typedef typename IO<DT>::T T;
     constexpr int NT = pieces<DT>(), TT = (KS + 1) / 2;
     typedef GradLds<DT, KS> Lds;
     extern __shared__ uint4 lds[];
-    char *l8 = (char *)lds;
-    uint4 *ks = (uint4 *)(l8 + Lds::k), *qs = (uint4 *)(l8 + Lds::q);
-    float *D = (float *)(l8 + Lds::D), *E = (float *)(l8 + Lds::E);
-    double *gd = (double *)(l8 + Lds::gd);
-    ChunkGates *gt = (ChunkGates *)(l8 + Lds::gates);
-    float *red = (float *)(l8 + Lds::red);        // the waves' sums of dG
-    double *rin = (double *)(red + 4 * DC);       // and of <S', dS'>
-    uint32_t *big = (uint32_t *)(rin + 4);   // the waves' largest magnitudes of D and of E
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g4 = lane >> 4, c16 = lane & 15;
-    const int n = (int)(blockIdx.x % a.N), hk = (int)(blockIdx.x / a.N % a.Hk), b = (int)(blockIdx.x / a.N / a.Hk);
-    const int per = a.H / a.Hk, dvp = (a.Dv + 15) & ~15;
+    float *D = (float *)(lds + Lds::D), *E = (float *)(lds + Lds::E);
+    double *gd = (double *)(lds + Lds::gd);
+    ChunkGates *gt = (ChunkGates *)(lds + Lds::gates);
+    float *red = (float *)(lds + Lds::red);        // the waves' sums of dG
+    double *rin = (double *)(lds + Lds::rin);      // and of <S', dS'>
+    uint32_t *big = (uint32_t *)(lds + Lds::big);  // the waves' largest magnitudes of D and of E
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
+    // chunks from the front first: the scan wrote theirs last
+    const int hk = (int)(blockIdx.x % a.Hk), b = (int)(blockIdx.x / a.Hk % a.B), n = (int)(blockIdx.x / a.Hk / a.B);
+    const int per = ONE ? 1 : a.H / a.Hk, ct16 = col_tiles(a.Dv, 1);
     const int nt = min(DC, tokens_of(a, b) - n * DC), room = min(DC, a.L - n * DC);   // tokens, and places, of this chunk
     const long tok0 = (long)b * a.L + n * DC;
     const T *op = (const T *)d.dout;
     T *dqp = (T *)d.dq, *dkp = (T *)d.dk, *dvo = (T *)d.dv;
-    int ek = 0, eq = 0;
-    if (nt > 0) {
-        const ChunkGates *g = (const ChunkGates *)(rec + ((((long)b * a.H + hk * per) * a.N + n) * (4 * MAT + GATES) + 4 * MAT));
-        ek = g->ek;   // the same for every value head
-        eq = g->eq;
-        const uint4 *in = kq + (((long)b * a.Hk + hk) * a.N + n) * 2 * Lds::kq;
+    dl_f4 tq[ONE ? 1 : 4][TT], tk[ONE ? 1 : 4][TT];   // sums over the value heads
 #pragma unroll
-        for (int i = 0; i < 2 * Lds::kq / 256; ++i) ks[i * 256 + tid] = in[i * 256 + tid];
-    }
-    dl_f4 tq[4][TT], tk[4][TT];   // sums over the value heads
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < (ONE ? 1 : 4); ++t)
 #pragma unroll
         for (int j = 0; j < TT; ++j) tq[t][j] = tk[t][j] = dl_f4{0.f, 0.f, 0.f, 0.f};
+    auto store = [&](int t, int j, dl_f4 x, dl_f4 y) {   // dq and dk of this wave's channel tile j, token tile t
+        const int row = 16 * t + c16, dk = 16 * (w * TT + j) + 4 * g4;
+        if (row >= room || dk >= a.Dk) return;
+        const bool real = row < nt;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            x[r] = real ? x[r] : 0.f;
+            y[r] = real ? y[r] : 0.f;
+        }
+        const long at = ((tok0 + row) * a.Hk + hk) * a.Dk + dk;
+        if constexpr (DT == F32) {
+            *(float4 *)(dqp + at) = make_float4(x[0], x[1], x[2], x[3]);
+            *(float4 *)(dkp + at) = make_float4(y[0], y[1], y[2], y[3]);
+        } else {
+            *(uint2 *)(dqp + at) = make_uint2(pack_16x2<DT>(x[0], x[1]), pack_16x2<DT>(x[2], x[3]));
+            *(uint2 *)(dkp + at) = make_uint2(pack_16x2<DT>(y[0], y[1]), pack_16x2<DT>(y[2], y[3]));
+        }
+    };
 
     for (int hh = 0; hh < per; ++hh) {
         const int h = hk * per + hh;
         const long ch = ((long)b * a.H + h) * a.N + n;
-        __syncthreads();   // keys and queries are there; the last head's matrices are read
+        __syncthreads();   // the last head's matrices are read
         if (nt <= 0) {     // nothing behind a sequence's end has a gradient
             for (int it = tid; it < room * a.Dv; it += 256) IO<DT>::st(dvo + ((tok0 + it / a.Dv) * a.H + h) * a.Dv, it % a.Dv, 0.f);
             if (tid < room) d.dg[(tok0 + tid) * a.H + h] = d.dbeta[(tok0 + tid) * a.H + h] = 0.f;
             continue;
         }
+        const dl_f4 *Sp = (const dl_f4 *)states + ch * ct16 * 2 * KS * 64, *Ep = (const dl_f4 *)d.dends + ch * ct16 * 2 * KS * 64;
+        const dl_f4 *ep = (const dl_f4 *)es + ch * ct16 * 4 * 64, *zp = (const dl_f4 *)d.zs + ch * ct16 * 4 * 64;
+        // 32 columns: states of KS (column tile, row tile)s a wave, e and z of token tile w, do of token tile w
+        dl_f4 xs[KS], xe[KS], x_e[2], x_z[2], xo[2];
+        auto fetch = [&](int c2) {
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const int at = i * 4 + w, ct = min(c2 + at / (2 * KS), ct16 - 1);
+                xs[i] = Sp[(ct * 2 * KS + at % (2 * KS)) * 64 + lane];
+                xe[i] = Ep[(ct * 2 * KS + at % (2 * KS)) * 64 + lane];
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int ct = min(c2 + i, ct16 - 1);
+                x_e[i] = ep[(ct * 4 + w) * 64 + lane];
+                x_z[i] = zp[(ct * 4 + w) * 64 + lane];
+                const int c = 16 * (c2 + i) + 4 * g4;
+                const T *p = op + ((tok0 + min(16 * w + c16, nt - 1)) * a.H + h) * a.Dv + (c < a.Dv ? c : 0);
+                if constexpr (DT == F32) {
+                    xo[i] = *(const dl_f4 *)p;
+                } else {
+                    const uint2 v = *(const uint2 *)p;
+                    xo[i] = dl_f4{__uint_as_float(v.x), __uint_as_float(v.y), 0.f, 0.f};
+                }
+            }
+        };
+        fetch(0);
         if (w == 0) gd[lane] = decay_sum(lane < nt ? a.g[(tok0 + lane) * a.H + h] : 0.f, lane < nt, lane);
         if (tid < GATES) ((uint4 *)gt)[tid] = rec[(ch + 1) * (4 * MAT + GATES) - GATES + tid];
         // scales over all columns
         int eu = -126, eS = -126, ey = -126, eE = -126, eo = -126;
-        for (int i = 0; i < (a.Dv + 15) / 16; ++i) {
+        for (int i = 0; i < ct16; ++i) {
             const int2 f = exps[ch * kDeltaTiles + i];
             const int4 g = d.exps[ch * kDeltaTiles + i];
             eu = max(eu, f.x); eS = max(eS, f.y);
             ey = max(ey, g.x); eE = max(eE, g.y); eo = max(eo, DT == F16 ? 0 : g.z);   // fp16 goes in as it is
         }
         const float su = pow2(-eu), sS = pow2(-eS), sy = pow2(-ey), sE = pow2(-eE), sd = pow2(-eo);
-        __syncthreads();
-        const float *ep = es + ch * DC * dvp, *zp = d.zs + ch * DC * dvp;
-        const float *Sp = states + ch * 32 * KS * dvp, *Ep = d.dends + ch * 32 * KS * dvp;
-        // row tile w of D and E; dv and dbeta of its tokens
-        {
-            dl_f4 ad[4], ae[4];
+        dl_f4 dq[4][TT], kr[4][TT], kw[4][TT], ad[4], ae[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) ad[j] = ae[j] = dl_f4{0.f, 0.f, 0.f, 0.f};
-            const int row = 16 * w + c16;
-            const float be = gt->beta[row];
-            float dot = 0.f;
-            uint32_t md = 0, me = 0;
-            for (int c = 8 * g4; c < ((a.Dv + 31) & ~31); c += 32) {
-                const bool on = c < a.Dv;
-                float z[8], e[8], y[8];
-                ld8<F32>(zp + (long)row * dvp + c, on, z);
-                ld8<F32>(ep + (long)row * dvp + c, on, e);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    dot += z[i] * e[i];
-                    y[i] = row < nt ? be * z[i] : 0.f;
-                }
-                if (on && row < room) {
-                    T *p = dvo + ((tok0 + row) * a.H + h) * a.Dv + c;
-                    if constexpr (DT == F32) {
-                        *(float4 *)p = make_float4(y[0], y[1], y[2], y[3]);
-                        *(float4 *)(p + 4) = make_float4(y[4], y[5], y[6], y[7]);
-                    } else {
-                        *(uint4 *)p = make_uint4(pack_16x2<DT>(y[0], y[1]), pack_16x2<DT>(y[2], y[3]),
-                                                 pack_16x2<DT>(y[4], y[5]), pack_16x2<DT>(y[6], y[7]));
-                    }
-                }
-                const Op<2> yo = split8<2>(y, sy);
-                const Op<NT> oo = op_of<DT>(or_zero<DT>(ld8_raw<DT>(op + ((tok0 + min(row, nt - 1)) * a.H + h) * a.Dv + (on ? c : 0)), on && row < nt), sd);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (j > w) break;
-                    float u[8];
-                    const int r = 16 * j + c16;
-                    ld8<F32>(ep + (long)r * dvp + c, on, u);
-                    const float bj = gt->beta[r];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) u[i] *= bj;
-                    const Op<2> uo = split8<2>(u, su);
-                    ad[j] = mm(oo, uo, ad[j]);
-                    ae[j] = mm(yo, uo, ae[j]);
-                }
-            }
-            dot += __shfl_xor(dot, 16);
-            dot += __shfl_xor(dot, 32);
-            if (g4 == 0 && row < room) d.dbeta[(tok0 + row) * a.H + h] = row < nt ? dot : 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int col = 16 * j + c16;
-                const double gj = gd[col];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int i = 16 * w + 4 * g4 + r;
-                    float f = 0.f;
-                    if (i >= col) f = __builtin_amdgcn_exp2f((float)(gd[i] - gj));
-                    const float x = i >= col ? a.scale * __builtin_amdgcn_ldexpf(ad[j][r], eo + eu) * f : 0.f;
-                    const float y = i > col ? -__builtin_amdgcn_ldexpf(ae[j][r], ey + eu) * f : 0.f;
-                    D[i * AROW + col] = x;
-                    E[i * AROW + col] = y;
-                    md = umax(md, mag(x));
-                    me = umax(me, mag(y));
-                }
-            }
-            md = group_max<64>(md);
-            me = group_max<64>(me);
-            if (lane == 0) {
-                big[w] = md;
-                big[4 + w] = me;
-            }
-        }
-        // products with the states
-        dl_f4 dq[4][TT], kr[4][TT], kw[4][TT];
-        float inner[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};   // short sums: <S, dS'> cancels
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t) {
+            ad[t] = ae[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < TT; ++j) dq[t][j] = kr[t][j] = kw[t][j] = dl_f4{0.f, 0.f, 0.f, 0.f};
-        for (int c = 8 * g4; c < ((a.Dv + 31) & ~31); c += 32) {
-            const bool on = c < a.Dv;
+        }
+        float inner[4] = {0.f, 0.f, 0.f, 0.f}, dot[4] = {0.f, 0.f, 0.f, 0.f};   // short sums: <S, dS'> cancels
+        __syncthreads();
+        const dl_f4 be = *(const dl_f4 *)(gt->beta + 16 * w + 4 * g4);
+        for (int c2 = 0; c2 < ct16; c2 += 2) {
+            if (c2) __syncthreads();   // the columns before are read
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const int at = i * 4 + w, ct = at / (2 * KS), t = at % (2 * KS);
+                const bool on = 16 * (c2 + ct) + c16 < a.Dv;
+                const int to = (kq_block<KS, 2>(0, ct, t >> 1) * 64 + kq_place(c16, g4)) * 2 + (t & 1);
+                dl_f4 x, y;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    x[r] = on ? xs[i][r] : 0.f;
+                    y[r] = on ? xe[i][r] : 0.f;
+                    inner[r] += x[r] * y[r];
+                }
+                uint32_t p[2][2], q[2][2];
+                split2<2>(x[0], x[1], sS, p[0]); split2<2>(x[2], x[3], sS, p[1]);
+                split2<2>(y[0], y[1], sE, q[0]); split2<2>(y[2], y[3], sE, q[1]);
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    ((uint2 *)(lds + Lds::S))[to + m * 2 * KS * 128] = make_uint2(p[0][m], p[1][m]);
+                    ((uint2 *)(lds + Lds::dS))[to + m * 2 * KS * 128] = make_uint2(q[0][m], q[1][m]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int c = 16 * (c2 + i) + c16;
+                const bool on = c < a.Dv;
+                const int to = (kq_block<2, 2>(0, i, w >> 1) * 64 + kq_place(c16, 2 * (w & 1) + (g4 >> 1))) * 2 + (g4 & 1);
+                dl_f4 x, y;
+                T *p = dvo + ((tok0 + 16 * w + 4 * g4) * a.H + h) * a.Dv + c;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    dot[r] += on ? x_z[i][r] * x_e[i][r] : 0.f;
+                    x[r] = on ? be[r] * x_z[i][r] : 0.f;
+                    y[r] = on ? be[r] * x_e[i][r] : 0.f;
+                    const int row = 16 * w + 4 * g4 + r;
+                    if (on && row < room) IO<DT>::st(p, (long)r * a.H * a.Dv, row < nt ? x[r] : 0.f);
+                }
+                uint32_t f[2][2], q[2][2];
+                split2<2>(x[0], x[1], sy, f[0]); split2<2>(x[2], x[3], sy, f[1]);
+                split2<2>(y[0], y[1], su, q[0]); split2<2>(y[2], y[3], su, q[1]);
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    ((uint2 *)(lds + Lds::y))[to + m * 4 * 128] = make_uint2(f[0][m], f[1][m]);
+                    ((uint2 *)(lds + Lds::u))[to + m * 4 * 128] = make_uint2(q[0][m], q[1][m]);
+                }
+            }
+            {
+                Raw8<DT> v;
+                if constexpr (DT == F32) {
+                    v.a[0] = __builtin_bit_cast(uint4, xo[0]);
+                    v.a[1] = __builtin_bit_cast(uint4, xo[1]);
+                } else {
+                    v.a[0] = make_uint4(__float_as_uint(xo[0][0]), __float_as_uint(xo[0][1]), __float_as_uint(xo[1][0]), __float_as_uint(xo[1][1]));
+                }
+                const bool row = 16 * w + c16 < nt, lo = 16 * c2 + 4 * g4 < a.Dv, hi = 16 * c2 + 16 + 4 * g4 < a.Dv;
+                if constexpr (DT == F32) {
+                    v.a[0] = or_zero(v.a[0], row && lo);
+                    v.a[1] = or_zero(v.a[1], row && hi);
+                } else {
+                    if (!(row && lo)) v.a[0].x = v.a[0].y = 0u;
+                    if (!(row && hi)) v.a[0].z = v.a[0].w = 0u;
+                }
+                const Op<NT> oo = op_of<DT>(v, sd);
+#pragma unroll
+                for (int m = 0; m < NT; ++m) lds[Lds::o + (m * 4 + w) * 64 + lane] = oo.p[m];
+            }
+            if (c2 + 2 < ct16) fetch(c2 + 2);
+            __syncthreads();
             Op<2> so[TT], to[TT];
 #pragma unroll
             for (int j = 0; j < TT; ++j) {
-                const int dk = 16 * (w * TT + j) + c16;
-                float x[8], y[8];
-                ld8<F32>(Sp + (long)dk * dvp + c, on && dk < a.Dk, x);
-                ld8<F32>(Ep + (long)dk * dvp + c, on && dk < a.Dk, y);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) inner[i] += x[i] * y[i];
-                so[j] = split8<2>(x, sS);
-                to[j] = split8<2>(y, sE);
+                const int ct = min(w * TT + j, 2 * KS - 1);   // a tile too many is not stored
+                so[j] = lds_cols<2, KS, false, 2>(lds + Lds::S, ct, 0, lane);
+                to[j] = lds_cols<2, KS, false, 2>(lds + Lds::dS, ct, 0, lane);
             }
+            Op<NT> ow;
+            const Op<2> yw = lds_cols<2, 2, false, 2>(lds + Lds::y, w, 0, lane);
+#pragma unroll
+            for (int m = 0; m < NT; ++m) ow.p[m] = lds[Lds::o + (m * 4 + w) * 64 + lane];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const int row = 16 * t + c16;
-                const float be = gt->beta[row];
-                float y[8], u[8];
-                ld8<F32>(zp + (long)row * dvp + c, on, y);
-                ld8<F32>(ep + (long)row * dvp + c, on, u);
+                const Op<2> yo = lds_cols<2, 2, false, 2>(lds + Lds::y, t, 0, lane), uo = lds_cols<2, 2, false, 2>(lds + Lds::u, t, 0, lane);
+                Op<NT> oo;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    y[i] *= be;
-                    u[i] *= be;
-                }
-                const Op<2> yo = split8<2>(y, sy), uo = split8<2>(u, su);
-                const Op<NT> oo = op_of<DT>(or_zero<DT>(ld8_raw<DT>(op + ((tok0 + min(row, nt - 1)) * a.H + h) * a.Dv + (on ? c : 0)), on && row < nt), sd);
+                for (int m = 0; m < NT; ++m) oo.p[m] = lds[Lds::o + (m * 4 + t) * 64 + lane];
 #pragma unroll
                 for (int j = 0; j < TT; ++j) {
                     dq[t][j] = mm(so[j], oo, dq[t][j]);
                     kr[t][j] = mm(so[j], yo, kr[t][j]);
                     kw[t][j] = mm(to[j], uo, kw[t][j]);
                 }
+                if (t <= w) {
+                    ad[t] = mm(ow, uo, ad[t]);
+                    ae[t] = mm(yw, uo, ae[t]);
+                }
             }
+        }
+        // dbeta of token tile w: the sum over a row's 16 lanes
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+#pragma unroll
+            for (int m = 1; m < 16; m *= 2) dot[r] += __shfl_xor(dot[r], m);
+            const int row = 16 * w + 4 * g4 + r;
+            if (c16 == 0 && row < room) d.dbeta[(tok0 + row) * a.H + h] = row < nt ? dot[r] : 0.f;
         }
         double in64 = 0.0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) in64 += inner[i];
+        for (int i = 0; i < 4; ++i) in64 += inner[i];
         in64 *= gt->from0[DC - 1];
+        __syncthreads();   // the columns are read: keys, queries, D and E take their place
+        {
+            const uint4 *in = kq + (((long)b * a.Hk + hk) * a.N + n) * 2 * Lds::kq;
+#pragma unroll
+            for (int i = 0; i < 2 * Lds::kq / 256; ++i) lds[i * 256 + tid] = in[i * 256 + tid];
+        }
+        const uint4 *ks = lds + Lds::k, *qs = lds + Lds::q;
+        const int ek = gt->ek, eq = gt->eq;
+        uint32_t md = 0, me = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int col = 16 * j + c16;
+            const double gj = gd[col];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * w + 4 * g4 + r;
+                float f = 0.f;
+                if (i >= col) f = __builtin_amdgcn_exp2f((float)(gd[i] - gj));
+                const float x = i >= col ? a.scale * __builtin_amdgcn_ldexpf(ad[j][r], eo + eu) * f : 0.f;
+                const float y = i > col ? -__builtin_amdgcn_ldexpf(ae[j][r], ey + eu) * f : 0.f;
+                D[i * AROW + col] = x;
+                E[i * AROW + col] = y;
+                md = umax(md, mag(x));
+                me = umax(me, mag(y));
+            }
+        }
+        md = group_max<64>(md);
+        me = group_max<64>(me);
+        if (lane == 0) {
+            big[w] = md;
+            big[4 + w] = me;
+        }
         float kx = 0.f;   // sum of k . t (u dS'^T)
         __syncthreads();  // D and E are there
         const int eD = scale_exp(umax(umax(big[0], big[1]), umax(big[2], big[3])));
@@ -494,8 +571,13 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(DeltaArgs a, co
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     dG += qv[r] * dq[t][j][r] + kv[r] * (kr[t][j][r] - kw[t][j][r]);
-                    tq[t][j][r] += dq[t][j][r];
-                    tk[t][j][r] += kr[t][j][r] + kw[t][j][r];
+                    kr[t][j][r] += kw[t][j][r];
+                }
+                if constexpr (ONE) {
+                    store(t, j, dq[t][j], kr[t][j]);
+                } else {
+                    tq[t][j] += dq[t][j];
+                    tk[t][j] += kr[t][j];
                 }
             }
             dG += __shfl_xor(dG, 16);
@@ -519,31 +601,12 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(DeltaArgs a, co
             if (lane < room) d.dg[(tok0 + lane) * a.H + h] = lane < nt ? (float)x : 0.f;
         }
     }
+    if (ONE && nt > 0) return;
+    const dl_f4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        const int row = 16 * t + c16;
-        if (row >= room) continue;
-        const bool real = row < nt;
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int j = 0; j < TT; ++j) {
-            const int dk = 16 * (w * TT + j) + 4 * g4;
-            if (dk >= a.Dk) continue;
-            const long at = ((tok0 + row) * a.Hk + hk) * a.Dk + dk;
-            dl_f4 x = tq[t][j], y = tk[t][j];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                x[r] = real ? x[r] : 0.f;
-                y[r] = real ? y[r] : 0.f;
-            }
-            if constexpr (DT == F32) {
-                *(float4 *)(dqp + at) = make_float4(x[0], x[1], x[2], x[3]);
-                *(float4 *)(dkp + at) = make_float4(y[0], y[1], y[2], y[3]);
-            } else {
-                *(uint2 *)(dqp + at) = make_uint2(pack_16x2<DT>(x[0], x[1]), pack_16x2<DT>(x[2], x[3]));
-                *(uint2 *)(dkp + at) = make_uint2(pack_16x2<DT>(y[0], y[1]), pack_16x2<DT>(y[2], y[3]));
-            }
-        }
-    }
+        for (int j = 0; j < TT; ++j) store(t, j, ONE ? zero : tq[ONE ? 0 : t][j], ONE ? zero : tk[ONE ? 0 : t][j]);
 }
 
 template <int DT, int KS> hipError_t bwd_of(const DeltaArgs &a, const DeltaBuffers &w, const DeltaGrads &d, hipStream_t st) {
@@ -561,8 +624,14 @@ template <int DT, int KS> hipError_t bwd_of(const DeltaArgs &a, const DeltaBuffe
     if ((e = lds_room(delta_bwd_scan_kernel<DT, KS, NW, false>, lds)) != hipSuccess) return e;
     delta_bwd_scan_kernel<DT, KS, NW, false><<<(unsigned)(bh * sg.G * col_tiles(a.Dv, NW)), 64 * NW, lds, st>>>(a, sg, w.back, w.kq, d);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if ((e = lds_room(delta_bwd_chunk_kernel<DT, KS>, lds2)) != hipSuccess) return e;
-    delta_bwd_chunk_kernel<DT, KS><<<(unsigned)((long)a.B * a.Hk * a.N), 256, lds2, st>>>(a, w.back, w.kq, w.es, w.states, w.exps, d);
+    const unsigned grid = (unsigned)((long)a.B * a.Hk * a.N);
+    if (a.H == a.Hk) {
+        if ((e = lds_room(delta_bwd_chunk_kernel<DT, KS, true>, lds2)) != hipSuccess) return e;
+        delta_bwd_chunk_kernel<DT, KS, true><<<grid, 256, lds2, st>>>(a, w.back, w.kq, w.es, w.states, w.exps, d);
+    } else {
+        if ((e = lds_room(delta_bwd_chunk_kernel<DT, KS, false>, lds2)) != hipSuccess) return e;
+        delta_bwd_chunk_kernel<DT, KS, false><<<grid, 256, lds2, st>>>(a, w.back, w.kq, w.es, w.states, w.exps, d);
+    }
     return hipGetLastError();
 }
 

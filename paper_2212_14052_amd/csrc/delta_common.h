@@ -192,7 +192,8 @@ constexpr int upper_frag(int t, int s) { return t < 2 ? 2 * t + s : 2 + t; }    
 // tokens by 32 channels, [piece][token block][channel block], in each the eight
 // channels 8 g of token n at 16-byte place 4 n + (g ^ n / 4).  Sixteen tokens of one
 // g are then on sixteen different places of a 256-byte bank row.
-template <int KS> constexpr int kq_block(int piece, int t, int s) { return (piece * 4 + t) * KS + s; }
+// (RB: blocks of 16 rows; the backward pass keeps other matrices so, too.)
+template <int KS, int RB = 4> constexpr int kq_block(int piece, int t, int s) { return (piece * RB + t) * KS + s; }
 __device__ __forceinline__ int kq_place(int n, int g) { return 4 * n + (g ^ (n >> 2)); }
 template <int KS> constexpr int kq_words(int pieces) { return pieces * 4 * KS * 64; }   // uint4
 
@@ -207,7 +208,7 @@ template <int NT, int KS> __device__ __forceinline__ Op<NT> lds_rows(const uint4
 // natural order, channels 16 T + 0 .. 15), summands = tokens 32 s .. + 31 in
 // token order.  A transposing read gives lane j of 16 the four rows that lanes 4 i + c
 // address, at the j-th of the 16 columns that lanes c = 0 .. 3 address four at a time.
-template <int NT, int KS, bool STATE = true>
+template <int NT, int KS, bool STATE = true, int RB = 4>
 __device__ __forceinline__ Op<NT> lds_cols(const uint4 *m, int T, int s, int lane) {
     const int c = lane & 3, row = 4 * (lane >> 4) + ((lane & 15) >> 2);   // and 16 rows on
     const int g = STATE ? c : 2 * (T & 1) + (c >> 1), half = STATE ? T & 1 : c & 1;
@@ -216,8 +217,8 @@ __device__ __forceinline__ Op<NT> lds_cols(const uint4 *m, int T, int s, int lan
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const uint16_t *p = (const uint16_t *)m + at;
-        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((dl_lds_s4 *)(p + kq_block<KS>(n, 2 * s, T >> 1) * 512)));
-        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((dl_lds_s4 *)(p + kq_block<KS>(n, 2 * s + 1, T >> 1) * 512)));
+        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((dl_lds_s4 *)(p + kq_block<KS, RB>(n, 2 * s, T >> 1) * 512)));
+        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((dl_lds_s4 *)(p + kq_block<KS, RB>(n, 2 * s + 1, T >> 1) * 512)));
         o.p[n] = make_uint4(lo.x, lo.y, hi.x, hi.y);
     }
     return o;
