@@ -5,7 +5,7 @@
 // inside a chunk of 64 tokens, S the state at its start, K, Q, V its rows and
 //     A = strictly lower part of (K K^T)_ij exp(G_i - G_j),   P = lower part of (Q K^T)_ij exp(G_i - G_j)
 // the chunk's errors e solve (I + A diag(beta)) e = R with R = V - diag(exp G) K S, so
-//     e = R - X (beta R),  X = (I + A diag(beta))^-1 A  (strictly lower),  u = beta e,
+//     e = R - X diag(beta) R,  X = (I + A diag(beta))^-1 A  (strictly lower),  u = beta e,
 //     o = scale (diag(exp G) Q S + P u),   S' = exp(G_63) S + K^T diag(exp(G_63 - G)) u.
 // No decay is ever divided by, and differences of G are taken in float64.
 //
@@ -110,8 +110,8 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
             mq = umax(mq, raw_mag<DT>(qr[i]));
         }
         const int2 e = largest(mk, mq);
-        ek = e.x;
-        eq = e.y;
+        ek = max(e.x, kLeast);
+        eq = max(e.y, kLeast);
     }
     // the first value head of a key head leaves its keys and queries for the scans
     uint4 *ki = h % (a.H / a.Hk) == 0 ? kq + (((long)b * a.Hk + hk) * a.N + n) * 2 * KQ : nullptr;
@@ -223,20 +223,23 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
     __syncthreads();
     // the lower halves' fragments; the transposes for the backward pass
     float xv[2][8], pv[2][8];
-    uint32_t mx = 0, mp = 0;
+    uint32_t mx = 0, mp = 0, mb = 0;
     const int row = 16 * w + c16;
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int at = row * AROW + 32 * s + 4 * g4 + (j & 3) + 16 * (j >> 2);
-            xv[s][j] = A[at];
+            const float x = A[at];
+            xv[s][j] = x * be[32 * s + 4 * g4 + (j & 3) + 16 * (j >> 2)];   // X diag(beta)
             pv[s][j] = P[at];
             mx = umax(mx, mag(xv[s][j]));
             mp = umax(mp, mag(pv[s][j]));
+            mb = umax(mb, mag(x * be[row]));                                // diag(beta) X, whose transpose it is backward
         }
     const int2 em = largest(mx, mp);
-    const float sx = pow2(-em.x), sp = pow2(-em.y);
+    const int eb = back ? max(largest(mb, 0).x, kLeast) : 0, ex = max(em.x, kLeast), ep = max(em.y, kLeast);
+    const float sx = pow2(-ex), sp = pow2(-ep), sb = pow2(-eb);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         if (s <= w / 2) {
@@ -254,10 +257,10 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int at = (32 * s + 4 * g4 + (j & 3) + 16 * (j >> 2)) * AROW + row;
-                x[j] = A[at];
+                x[j] = A[at] * be[32 * s + 4 * g4 + (j & 3) + 16 * (j >> 2)];
                 p[j] = P[at];
             }
-            const Op<NX> xo = split8<NX>(x, sx), po = split8<NX>(p, sp);
+            const Op<NX> xo = split8<NX>(x, sb), po = split8<NX>(p, sp);
 #pragma unroll
             for (int i = 0; i < NX; ++i) {
                 xt[i * MAT + f] = xo.p[i];
@@ -268,18 +271,18 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
     if (tid == 0) {
         gf->ek = ek;
         gf->eq = eq;
-        gf->ex = em.x;
-        gf->ep = em.y;
+        gf->ex = ex;
+        gf->ep = ep;
         if (back) {
             gb->ek = ek;
             gb->eq = eq;
-            gb->ex = em.x;
-            gb->ep = em.y;
+            gb->ex = eb;
+            gb->ep = ep;
         }
     }
 }
 
-// NW waves of 16 columns.  es, states, exps: for the backward pass, or null.
+// NW waves of NC times 16 columns.  es, states, exps: for the backward pass, or null.
 //
 // A wave's vector instructions take longer than its matrix instructions here,
 // so scales cost nothing of their own: they ride on the rounding to pieces, on the
@@ -289,7 +292,7 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
 //
 // Sequences may be cut into segments (see DeltaSegments).  With MAPS a workgroup
 // does not produce outputs but its segment's map from state to state.
-template <int DT, int KS, int NW, bool MAPS>
+template <int DT, int KS, int NW, int NC, bool MAPS>
 __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, DeltaSegments sg, const uint4 *__restrict__ rec,
                                                                const uint4 *__restrict__ kq,
                                                                typename IO<DT>::T *__restrict__ o, float *S_final,
@@ -297,16 +300,14 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
                                                                int2 *__restrict__ exps) {
     typedef typename IO<DT>::T T;
     constexpr int NT = pieces<DT>(), NX = 2, NO = out_pieces<DT>();
-    typedef ChunkCopy<DT, KS, NW, NX + NO> Copy;
+    typedef ChunkCopy<DT, KS, NW, NW * NC, NX + NO> Copy;
     typedef typename Copy::Lds Lds;
     extern __shared__ uint4 lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
-    const ScanPlace<NW, MAPS> at_(a, sg, blockIdx.x, w);
+    const ScanPlace<NW, NC, MAPS> at_(a, sg, blockIdx.x, w);
     const long bh = at_.bh;
     const int h = at_.h, b = at_.b, hk = h / (a.H / a.Hk), seg = at_.seg, cb = at_.cb, c0 = at_.c0;
     const bool here = c0 < at_.width;       // a wave without columns only helps to copy
-    const int col = c0 + c16;
-    const bool on = col < at_.width, on4 = c0 + 4 * g4 < at_.width;
     const int len = tokens_of(a, b), nb = (len + DC - 1) / DC;
     const int first = seg * sg.Ns, last = min(first + sg.Ns, nb);   // chunks from, and before
     if (MAPS && last >= nb) return;         // nothing starts behind it
@@ -314,17 +315,19 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
                   (const T *)a.v + ((long)b * a.L * a.H + h) * a.Dv + (at_.unit ? 0 : cb), (long)a.H * a.Dv,
                   a.Dv - (at_.unit ? 0 : cb), len, (uint32_t)(uintptr_t)(dl_lds_void *)lds};
 
-    dl_f4 S[2 * KS];
+    dl_f4 S[NC][2 * KS];
     int E = 0;
     const float *S0 = MAPS ? nullptr : sg.G > 1 ? sg.in + ((long)seg * a.B * a.H) * a.Dk * a.Dv : a.S0;
 #pragma unroll
-    for (int t = 0; t < 2 * KS; ++t)
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
-            S[t][r] = S0 && on && dk < a.Dk ? S0[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
-            if (MAPS && at_.unit && on && dk == col) S[t][r] = 1.f;
-        }
+        for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r, col = c0 + 16 * c + c16;
+                S[c][t][r] = S0 && col < a.Dv && dk < a.Dk ? S0[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
+                if (MAPS && at_.unit && dk < a.Dk && dk == col) S[c][t][r] = 1.f;
+            }
     if (Lds::two && first < last) in.issue(first, w, lane);
     for (int n = first; n < last; ++n) {
         const int nt = min(DC, len - n * DC);
@@ -337,11 +340,15 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
         if (!MAPS && states) {
             dl_f4 *p = (dl_f4 *)states + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;
 #pragma unroll
-            for (int t = 0; t < 2 * KS; ++t) {
-                dl_f4 y;
+            for (int c = 0; c < NC; ++c) {
+                if (c0 + 16 * c >= a.Dv) break;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) y[r] = __builtin_amdgcn_ldexpf(S[t][r], E);
-                p[t * 64] = y;
+                for (int t = 0; t < 2 * KS; ++t) {
+                    dl_f4 y;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) y[r] = __builtin_amdgcn_ldexpf(S[c][t][r], E);
+                    p[(c * 2 * KS + t) * 64] = y;
+                }
             }
         }
         const int ek = __builtin_amdgcn_readfirstlane(gt->ek), eq = __builtin_amdgcn_readfirstlane(gt->eq),
@@ -349,18 +356,20 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
                   et = __builtin_amdgcn_readfirstlane(gt->et);
         // K S and, transposed (rows are columns of S, so that a lane will hold four
         // consecutive values of one token), Q S
-        dl_f4 R[4], u[4], x[4];
+        dl_f4 R[NC][4], u[NC][4], x[NC][4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) R[t] = x[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) R[c][t] = x[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
         Op<NT> kf[2][4], qf[2][4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) kf[0][t] = lds_rows<NT, KS>(ks, t, 0, lane);
 #pragma unroll
         for (int t = 0; t < (MAPS ? 0 : 4); ++t) qf[0][t] = lds_rows<NT, KS>(qs, t, 0, lane);
-        const int em = wave_exp(S), eS = em + E;   // of the registers, of S
+        const int em = max(wave_exp(S), kLeast), eS = em + E;   // of the registers, of S
         const float sc = pow2(-em);
         Op<NX> xo[6];
-        dl_f4 be[4], v[4], f0[4];
+        dl_f4 be[4], v[NC][4], f0[4];
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             if (s + 1 < KS) {
@@ -373,21 +382,27 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
                 for (int t = 0; t < 4; ++t) {
                     f0[t] = *(const dl_f4 *)(gt->from0 + 16 * t + 4 * g4);
                     be[t] = *(const dl_f4 *)(gt->beta + 16 * t + 4 * g4);
-                    v[t] = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * w, lane);
-                    if (MAPS && at_.unit) v[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) {
+                        v[c][t] = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * (w * NC + c), lane);
+                        if (MAPS && at_.unit) v[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+                    }
                 }
 #pragma unroll
                 for (int f = 0; f < 6; ++f) xo[f] = ld_frag<NX>(xs, f, lane);
             }
             in_order();
-            const Op<2> so = split8<2>(S[2 * s], S[2 * s + 1], sc);
-            Op<NO> sh;
 #pragma unroll
-            for (int p = 0; p < NO; ++p) sh.p[p] = so.p[p];
+            for (int c = 0; c < NC; ++c) {
+                const Op<2> so = split8<2>(S[c][2 * s], S[c][2 * s + 1], sc);
+                Op<NO> sh;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) R[t] = mm(kf[s & 1][t], so, R[t]);
+                for (int p = 0; p < NO; ++p) sh.p[p] = so.p[p];
 #pragma unroll
-            for (int t = 0; t < (MAPS ? 0 : 4); ++t) x[t] = mm(sh, qf[s & 1][t], x[t]);
+                for (int t = 0; t < 4; ++t) R[c][t] = mm(kf[s & 1][t], so, R[c][t]);
+#pragma unroll
+                for (int t = 0; t < (MAPS ? 0 : 4); ++t) x[c][t] = mm(sh, qf[s & 1][t], x[c][t]);
+            }
             in_order();
         }
         // R = V - exp(G) K S
@@ -395,20 +410,23 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                R[t][r] = v[t][r] - __builtin_amdgcn_ldexpf(f0[t][r], ek + eS) * R[t][r];
-                u[t][r] = be[t][r] * R[t][r];
+                const float f = __builtin_amdgcn_ldexpf(f0[t][r], ek + eS);
+#pragma unroll
+                for (int c = 0; c < NC; ++c) R[c][t][r] = v[c][t][r] - f * R[c][t][r];
             }
-        // e = R - X (beta R), u = beta e
-        const int er = wave_exp(u);
+        // e = R - (X diag(beta)) R, u = beta e
+        const int er = max(wave_exp(R), kLeast);
+        const float px = pow2_sum(er + ex), sr = pow2(-er);
         Op<NO> po[6];
 #pragma unroll
         for (int f = 0; f < (MAPS ? 0 : 6); ++f) po[f] = ld_frag<NO>(ps, f, lane);
         in_order();
-        {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
             Op<NX> br[2];
             dl_f4 y[4];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) br[s] = split8<NX>(u[2 * s], u[2 * s + 1], pow2(-er));
+            for (int s = 0; s < 2; ++s) br[s] = split8<NX>(R[c][2 * s], R[c][2 * s + 1], sr);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 y[t] = mm(xo[lower_frag(t, 0)], br[0], dl_f4{0.f, 0.f, 0.f, 0.f});
@@ -418,17 +436,21 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    R[t][r] -= __builtin_amdgcn_ldexpf(y[t][r], er + ex);
-                    u[t][r] = be[t][r] * R[t][r];
+                    R[c][t][r] -= px * y[t][r];
+                    u[c][t][r] = be[t][r] * R[c][t][r];
                 }
         }
+        const int eu = max(wave_exp(u), kLeast);
         if (!MAPS && es) {
             dl_f4 *p = (dl_f4 *)es + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 4 * 64 + lane;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) p[t * 64] = R[t];
+            for (int c = 0; c < NC; ++c) {
+                if (c0 + 16 * c >= a.Dv) break;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) p[(4 * c + t) * 64] = R[c][t];
+                if (lane == 0) exps[ch * kDeltaTiles + c0 / 16 + c] = make_int2(eu, max(min(eS, 114), -126));
+            }
         }
-        const int eu = wave_exp(u);
-        if (!MAPS && exps && lane == 0) exps[ch * kDeltaTiles + c0 / 16] = make_int2(eu, max(min(eS, 114), -126));
         Op<NT> kc[2][2];
         dl_f4 te[4];
         float fo[4];
@@ -443,47 +465,56 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
         in_order();
         // o = scale (exp(G) Q S + P u)
         if constexpr (!MAPS) {
-            Op<NO> uo[2];
+            const float py = __builtin_amdgcn_ldexpf(a.scale, ep + eu), su = pow2(-eu);
+            float px[4];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) uo[s] = split8<NO>(u[2 * s], u[2 * s + 1], pow2(-eu));
-            const float py = __builtin_amdgcn_ldexpf(a.scale, ep + eu);
+            for (int t = 0; t < 4; ++t) px[t] = __builtin_amdgcn_ldexpf(fo[t] * a.scale, eq + eS);
+            T *oc = o + (((long)b * a.L + n * DC) * a.H + h) * a.Dv + c0;
+            const int room = a.L - n * DC;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const float px = __builtin_amdgcn_ldexpf(fo[t] * a.scale, eq + eS);
-                dl_f4 y = mm(uo[0], po[lower_frag(t, 0)], dl_f4{0.f, 0.f, 0.f, 0.f});
-                if (t >= 2) y = mm(uo[1], po[lower_frag(t, 1)], y);
+            for (int c = 0; c < NC; ++c) {
+                Op<NO> uo[2];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[t][r] = x[t][r] * px + y[r] * py;
+                for (int s = 0; s < 2; ++s) uo[s] = split8<NO>(u[c][2 * s], u[c][2 * s + 1], su);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    dl_f4 y = mm(uo[0], po[lower_frag(t, 0)], dl_f4{0.f, 0.f, 0.f, 0.f});
+                    if (t >= 2) y = mm(uo[1], po[lower_frag(t, 1)], y);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[c][t][r] = x[c][t][r] * px[t] + y[r] * py;
+                }
             }
-        }
-        if (!MAPS && nt < DC) {   // the last chunk: places behind the end are 0
+            if (nt < DC) {   // the last chunk: places behind the end are 0
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) x[c][t][r] = 16 * t + c16 < nt ? x[c][t][r] : 0.f;
+            }
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[t][r] = 16 * t + c16 < nt ? x[t][r] : 0.f;
+                for (int c = 0; c < NC; ++c)
+                    if (c0 + 16 * c + 4 * g4 < a.Dv && 16 * t + c16 < room) {
+                        T *op = oc + (uint32_t)((16 * t + c16) * a.H * a.Dv + 16 * c + 4 * g4);
+                        if constexpr (DT == F32) *(float4 *)op = make_float4(x[c][t][0], x[c][t][1], x[c][t][2], x[c][t][3]);
+                        else *(uint2 *)op = make_uint2(pack_16x2<DT>(x[c][t][0], x[c][t][1]), pack_16x2<DT>(x[c][t][2], x[c][t][3]));
+                    }
         }
-        const int room = a.L - n * DC;
-        T *oc = o + (((long)b * a.L + n * DC) * a.H + h) * a.Dv + c0;
-#pragma unroll
-        for (int t = 0; t < (MAPS ? 0 : 4); ++t)
-            if (on4 && 16 * t + c16 < room) {
-                T *op = oc + (uint32_t)((16 * t + c16) * a.H * a.Dv + 4 * g4);
-                if constexpr (DT == F32) *(float4 *)op = make_float4(x[t][0], x[t][1], x[t][2], x[t][3]);
-                else *(uint2 *)op = make_uint2(pack_16x2<DT>(x[t][0], x[t][1]), pack_16x2<DT>(x[t][2], x[t][3]));
-            }
         // S <- exp(G_63) S + K^T (exp(G_63 - G) u), in units of the keys' times the errors' scale;
         // of 2^-60 of S where the errors are smaller than that
         const int En = max(ek + eu + et, max(eS - 60, E - 100)), ew = En - ek;
         const float fs = fl * pow2(max(E - En, -126)), sw = pow2(max(min(-ew, 127), -126));
         E = En;
-        Op<2> wo[2];
+        Op<2> wo[NC][2];
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t) te[t] *= sw;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) u[t][r] *= te[t][r];
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) wo[s] = split8<2>(u[2 * s], u[2 * s + 1], sw);
-        dl_f4 y[2];   // summed from zero: added to S step by step, each step would round it
+            for (int s = 0; s < 2; ++s) wo[c][s] = split8<2>(u[c][2 * s], u[c][2 * s + 1], te[2 * s], te[2 * s + 1]);
+        dl_f4 y[2][NC];   // summed from zero: added to S step by step, each step would round it
 #pragma unroll
         for (int t = 0; t < 2 * KS; ++t) {
             if (t + 1 < 2 * KS) {
@@ -491,42 +522,54 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
                 for (int s = 0; s < 2; ++s) kc[(t + 1) & 1][s] = lds_cols<NT, KS>(ks, t + 1, s, lane);
             }
             in_order();
-            y[t & 1] = dl_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int s = 0; s < 2; ++s) y[t & 1] = mm(kc[t & 1][s], wo[s], y[t & 1]);
-            if (t > 0) {
+            for (int c = 0; c < NC; ++c) {
+                y[t & 1][c] = dl_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int r = 0; r < 4; ++r) S[t - 1][r] = S[t - 1][r] * fs + y[(t - 1) & 1][r];
+                for (int s = 0; s < 2; ++s) y[t & 1][c] = mm(kc[t & 1][s], wo[c][s], y[t & 1][c]);
+                if (t > 0) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[c][t - 1][r] = S[c][t - 1][r] * fs + y[(t - 1) & 1][c][r];
+                }
             }
             in_order();
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[2 * KS - 1][r] = S[2 * KS - 1][r] * fs + y[1][r];
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[c][2 * KS - 1][r] = S[c][2 * KS - 1][r] * fs + y[1][c][r];
     }
-#pragma unroll
-    for (int t = 0; t < 2 * KS; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S[t][r] = __builtin_amdgcn_ldexpf(S[t][r], E);
     if (!here) return;
-    if constexpr (MAPS) {
-        store_map<KS>(a, sg, at_, S, E, lane);
-        return;
-    }
-    // tokens of this segment's chunks behind the end
-    if (on4)
-        for (int t = max(first, nb) * DC + c16; t < min(a.L, (first + sg.Ns) * DC); t += 16) {
-            T *op = o + (((long)b * a.L + t) * a.H + h) * a.Dv + c0 + 4 * g4;
-            if constexpr (DT == F32) *(float4 *)op = make_float4(0.f, 0.f, 0.f, 0.f);
-            else *(uint2 *)op = make_uint2(0u, 0u);
-        }
-    if (on && S_final && (last == nb && (first < last || seg == 0))) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
-                if (dk < a.Dk) S_final[(bh * a.Dk + dk) * a.Dv + col] = S[t][r];
+            for (int r = 0; r < 4; ++r) S[c][t][r] = __builtin_amdgcn_ldexpf(S[c][t][r], E);
+    if constexpr (MAPS) {
+        store_map<KS>(a, sg, at_, S, lane);
+        return;
+    }
+    const bool write = S_final && last == nb && (first < last || seg == 0);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        // tokens of this segment's chunks behind the end
+        if (c0 + 16 * c + 4 * g4 < a.Dv)
+            for (int t = max(first, nb) * DC + c16; t < min(a.L, (first + sg.Ns) * DC); t += 16) {
+                T *op = o + (((long)b * a.L + t) * a.H + h) * a.Dv + c0 + 16 * c + 4 * g4;
+                if constexpr (DT == F32) *(float4 *)op = make_float4(0.f, 0.f, 0.f, 0.f);
+                else *(uint2 *)op = make_uint2(0u, 0u);
             }
+        const int col = c0 + 16 * c + c16;
+        if (write && col < a.Dv) {
+#pragma unroll
+            for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
+                    if (dk < a.Dk) S_final[(bh * a.Dk + dk) * a.Dv + col] = S[c][t][r];
+                }
+        }
     }
 }
 
@@ -588,13 +631,13 @@ __global__ __launch_bounds__(256, 1) void delta_join_kernel(DeltaArgs a, DeltaSe
     for (int i = 0; i + 1 < segs; ++i) {
         const int seg = back ? segs - 1 - i : i;
         __syncthreads();
-        dl_f4 S[2 * KS], y[TW];
+        dl_f4 S[1][2 * KS], y[TW];
 #pragma unroll
-        for (int t = 0; t < 2 * KS; ++t) S[t] = st[t][lane];
+        for (int t = 0; t < 2 * KS; ++t) S[0][t] = st[t][lane];
         const int es = wave_exp(S), e = es + ef;
         Op<2> so[KS];
 #pragma unroll
-        for (int s = 0; s < KS; ++s) so[s] = split8<2>(S[2 * s], S[2 * s + 1], pow2(-es));
+        for (int s = 0; s < KS; ++s) so[s] = split8<2>(S[0][2 * s], S[0][2 * s + 1], pow2(-es));
 #pragma unroll
         for (int j = 0; j < TW; ++j) {
             y[j] = dl_f4{0.f, 0.f, 0.f, 0.f};
@@ -615,51 +658,57 @@ __global__ __launch_bounds__(256, 1) void delta_join_kernel(DeltaArgs a, DeltaSe
 
 }  // namespace
 
-// Segments of a sequence.  A wave takes about one time unit a chunk whatever else
-// runs, and the card holds 256 workgroups of a scan.  Cut into G segments, the
-// maps of G - 1 cost Dk more columns and no outputs (0.8 units a chunk), joining
-// them about 2 units each.
-int delta_segments(int B, int H, int N, int Dk, int Dv) {
-    const double bh = (double)B * H, v = col_tiles(Dv, 4), k = col_tiles(Dk, 4);
-    int best = 1;
+// How a launch's scans are cut.  A wave of 16 columns takes about one time unit a
+// chunk whatever else runs, one of 32 kWide, and the card holds 256 workgroups of
+// four; the maps of G - 1 of G segments have Dk more columns and no outputs (0.8 units a
+// chunk), joining them takes about one unit each.
+DeltaCut delta_cut(int B, int H, int N, int Dk, int Dv, int dtype) {
+    constexpr double kWide = 1.25;
+    const double bh = (double)B * H;
+    DeltaCut best{1, 1};
     double least = 0;
-    for (int G = 1; G <= 64 && 4 * G <= N; ++G) {
-        const double Ns = (N + G - 1) / G;
-        double t = ceil(bh * v * G / 256) * Ns;
-        if (G > 1) t += 0.8 * ceil(bh * (v + k) * (G - 1) / 256) * Ns + 2.0 * G + 8;
-        if (G == 1 || t < 0.95 * least) {
-            best = G;
-            least = t;
+    for (int NC = 1; NC <= (dtype == F32 ? 1 : 2); ++NC)
+        for (int G = 1; G <= 64 && (G == 1 || 4 * G <= N); ++G) {
+            const double v = col_tiles(Dv, 4 * NC), k = col_tiles(Dk, 4 * NC), Ns = (N + G - 1) / G, unit = NC == 1 ? 1.0 : kWide;
+            double t = unit * ceil(bh * v * G / 256) * Ns;
+            if (G > 1) t += unit * 0.8 * ceil(bh * (v + k) * (G - 1) / 256) * Ns + G + 5;
+            if ((NC == 1 && G == 1) || t < 0.95 * least) {
+                best = DeltaCut{G, NC};
+                least = t;
+            }
         }
-    }
     return best;
 }
 
 namespace {
 
-template <int DT, int KS>
-hipError_t fwd_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_final, hipStream_t st) {
+template <int DT, int KS, int NC>
+hipError_t scans_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_final, hipStream_t st) {
     typedef typename IO<DT>::T T;
-    constexpr int NW = 4;
-    const long bh = (long)a.B * a.H;
-    delta_chunk_kernel<DT, KS><<<(unsigned)(bh * a.N), 256, 0, st>>>(a, w.rec, w.back, w.kq);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    constexpr int lds = ScanLds<DT, KS, NW, 2 + out_pieces<DT>()>::total;
+    constexpr int NW = 4, lds = ScanLds<DT, KS, NW * NC, 2 + out_pieces<DT>()>::total;
     const DeltaSegments sg = w.seg;
+    const long bh = (long)a.B * a.H;
+    hipError_t e;
     if (sg.G > 1) {
-        e = lds_room(delta_scan_kernel<DT, KS, NW, true>, lds);
-        if (e != hipSuccess) return e;
-        delta_scan_kernel<DT, KS, NW, true><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW) + col_tiles(a.Dk, NW))), 64 * NW, lds, st>>>(
+        if ((e = lds_room(delta_scan_kernel<DT, KS, NW, NC, true>, lds)) != hipSuccess) return e;
+        delta_scan_kernel<DT, KS, NW, NC, true><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW * NC) + col_tiles(a.Dk, NW * NC))), 64 * NW, lds, st>>>(
             a, sg, w.rec, w.kq, nullptr, nullptr, nullptr, nullptr, nullptr);
-        e = launch_delta_join(a, sg, a.S0, false, st);
-        if (e != hipSuccess) return e;
+        if ((e = launch_delta_join(a, sg, a.S0, false, st)) != hipSuccess) return e;
     }
-    e = lds_room(delta_scan_kernel<DT, KS, NW, false>, lds);
-    if (e != hipSuccess) return e;
-    delta_scan_kernel<DT, KS, NW, false><<<(unsigned)(bh * sg.G * col_tiles(a.Dv, NW)), 64 * NW, lds, st>>>(
+    if ((e = lds_room(delta_scan_kernel<DT, KS, NW, NC, false>, lds)) != hipSuccess) return e;
+    delta_scan_kernel<DT, KS, NW, NC, false><<<(unsigned)(bh * sg.G * col_tiles(a.Dv, NW * NC)), 64 * NW, lds, st>>>(
         a, sg, w.rec, w.kq, (T *)o, S_final, w.es, w.states, w.exps);
     return hipGetLastError();
+}
+
+template <int DT, int KS>
+hipError_t fwd_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_final, hipStream_t st) {
+    delta_chunk_kernel<DT, KS><<<(unsigned)((long)a.B * a.H * a.N), 256, 0, st>>>(a, w.rec, w.back, w.kq);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if constexpr (DT != F32)
+        if (w.seg.NC == 2) return scans_of<DT, KS, 2>(a, w, o, S_final, st);
+    return scans_of<DT, KS, 1>(a, w, o, S_final, st);
 }
 
 template <int DT> hipError_t fwd_by(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_final, hipStream_t st) {

@@ -3,7 +3,7 @@
 // With a chunk's G, A, X, P, e, u, S of the forward pass (delta.hip), f_i = exp(G_i), t_i =
 // exp(G_63 - G_i), do the output's gradient times the scale, and dS' the gradient of the state
 // behind the chunk:
-//     du = P^T do + t (K dS'),   z = du - X^T (beta du),   y = beta z = dv,
+//     du = P^T do + t (K dS'),   z = du - (diag(beta) X)^T du,   y = beta z = dv,
 //     dS = exp(G_63) dS' + Q^T (f do) - K^T (f y)
 // is again a scan whose columns do not meet, in the order from the end
 // (delta_bwd_scan_kernel); it leaves z and dS' of every chunk.  Then every chunk for itself
@@ -18,21 +18,19 @@
 namespace h3 {
 namespace {
 
-template <int DT, int KS, int NW, bool MAPS>
+template <int DT, int KS, int NW, int NC, bool MAPS>
 __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a, DeltaSegments sg, const uint4 *__restrict__ rec,
                                                                    const uint4 *__restrict__ kq, DeltaGrads d) {
     typedef typename IO<DT>::T T;
     constexpr int NT = pieces<DT>(), NM = 2;
-    typedef ChunkCopy<DT, KS, NW, 2 * NM> Copy;
+    typedef ChunkCopy<DT, KS, NW, NW * NC, 2 * NM> Copy;
     typedef typename Copy::Lds Lds;
     extern __shared__ uint4 lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
-    const ScanPlace<NW, MAPS, true> at_(a, sg, blockIdx.x, w);
+    const ScanPlace<NW, NC, MAPS, true> at_(a, sg, blockIdx.x, w);
     const long bh = at_.bh;
     const int h = at_.h, b = at_.b, hk = h / (a.H / a.Hk), seg = at_.seg, cb = at_.cb, c0 = at_.c0;
     const bool here = c0 < at_.width;
-    const int col = c0 + c16;
-    const bool on = col < at_.width;
     const int len = tokens_of(a, b), nb = (len + DC - 1) / DC;
     const int first = seg * sg.Ns, last = min(first + sg.Ns, nb);   // chunks from, and before
     if (MAPS ? first >= last : first >= last && seg > 0) return;
@@ -40,54 +38,60 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
                   (const T *)d.dout + ((long)b * a.L * a.H + h) * a.Dv + (at_.unit ? 0 : cb), (long)a.H * a.Dv,
                   a.Dv - (at_.unit ? 0 : cb), len, (uint32_t)(uintptr_t)(dl_lds_void *)lds};
 
-    dl_f4 S[2 * KS];   // dS' 2^-E
+    dl_f4 S[NC][2 * KS];   // dS' 2^-E
     int E = 0;
     const float *dS = MAPS ? nullptr : sg.G > 1 ? sg.in + ((long)seg * a.B * a.H) * a.Dk * a.Dv : d.dS;
 #pragma unroll
-    for (int t = 0; t < 2 * KS; ++t)
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
-            S[t][r] = dS && on && dk < a.Dk ? dS[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
-            if (MAPS && at_.unit && on && dk == col) S[t][r] = 1.f;
-        }
+        for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r, col = c0 + 16 * c + c16;
+                S[c][t][r] = dS && col < a.Dv && dk < a.Dk ? dS[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
+                if (MAPS && at_.unit && dk < a.Dk && dk == col) S[c][t][r] = 1.f;
+            }
     if (Lds::two && first < last) in.issue(last - 1, w, lane);
     for (int n = last - 1; n >= first; --n) {
         const long ch = bh * a.N + n;
         const uint4 *at = in.arrive(lds, n, n - 1, n > first, w, lane);
         if (!here) continue;
-        const uint4 *ks = at + Lds::k, *qs = at + Lds::q, *xs = at + Lds::rec, *ps = xs + NM * MAT;   // X^T, P^T
+        const uint4 *ks = at + Lds::k, *qs = at + Lds::q, *xs = at + Lds::rec, *ps = xs + NM * MAT;   // (diag(beta) X)^T, P^T
         const T *vs = (const T *)(at + Lds::v);
         const ChunkGates *gt = (const ChunkGates *)(ps + NM * MAT);
         const int nt = min(DC, len - n * DC);
         if constexpr (!MAPS) {
             dl_f4 *p = (dl_f4 *)d.dends + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;
 #pragma unroll
-            for (int t = 0; t < 2 * KS; ++t) {
-                dl_f4 y;
+            for (int c = 0; c < NC; ++c) {
+                if (c0 + 16 * c >= a.Dv) break;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) y[r] = __builtin_amdgcn_ldexpf(S[t][r], E);
-                p[t * 64] = y;
+                for (int t = 0; t < 2 * KS; ++t) {
+                    dl_f4 y;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) y[r] = __builtin_amdgcn_ldexpf(S[c][t][r], E);
+                    p[(c * 2 * KS + t) * 64] = y;
+                }
             }
         }
         const int ek = __builtin_amdgcn_readfirstlane(gt->ek), eq = __builtin_amdgcn_readfirstlane(gt->eq),
                   ex = __builtin_amdgcn_readfirstlane(gt->ex), ep = __builtin_amdgcn_readfirstlane(gt->ep),
                   ef = __builtin_amdgcn_readfirstlane(gt->ef);
         // du = t (K dS') + P^T do
-        dl_f4 u[4], dd[4], te[4], be[4];
+        dl_f4 u[NC][4], dd[NC][4], te[4], be[4];
         Op<NM> pf[6], xf[6];
         Op<NT> kf[2][4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            u[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
-            kf[0][t] = lds_rows<NT, KS>(ks, t, 0, lane);
-        }
+        for (int t = 0; t < 4; ++t) kf[0][t] = lds_rows<NT, KS>(ks, t, 0, lane);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            dd[t] = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * w, lane);
-            if (MAPS && at_.unit) dd[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
-        }
-        const int em = wave_exp(S), eS = em + E;   // of the registers, of dS'
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                u[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+                dd[c][t] = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * (w * NC + c), lane);
+                if (MAPS && at_.unit) dd[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+            }
+        const int em = max(wave_exp(S), kLeast), eS = em + E;   // of the registers, of dS'
         const float sc = pow2(-em);
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
@@ -104,42 +108,52 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
                 }
             }
             in_order();
-            const Op<2> so = split8<2>(S[2 * s], S[2 * s + 1], sc);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) u[t] = mm(kf[s & 1][t], so, u[t]);
+            for (int c = 0; c < NC; ++c) {
+                const Op<2> so = split8<2>(S[c][2 * s], S[c][2 * s + 1], sc);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) u[c][t] = mm(kf[s & 1][t], so, u[c][t]);
+            }
             in_order();
         }
         if (nt < DC) {   // the last chunk: nothing comes from behind the end
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int c = 0; c < NC; ++c)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) dd[t][r] = 16 * t + 4 * g4 + r < nt ? dd[t][r] : 0.f;
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) dd[c][t][r] = 16 * t + 4 * g4 + r < nt ? dd[c][t][r] : 0.f;
         }
-        const int ed = wave_exp(dd);
+        const int ed = max(wave_exp(dd), kLeast);
 #pragma unroll
         for (int f = 0; f < 6; ++f) xf[f] = ld_frag<NM>(xs, f, lane);
         in_order();
-        dl_f4 y[4];
+        dl_f4 y[NC][4];
         {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) te[t][r] = __builtin_amdgcn_ldexpf(te[t][r], ek + eS);
             const int e = DT == F16 ? 0 : ed;
             const float py = __builtin_amdgcn_ldexpf(a.scale, ep + e);
-            Op<NT> od[2];   // do as it came
 #pragma unroll
-            for (int s = 0; s < 2; ++s) od[s] = split8<NT>(dd[2 * s], dd[2 * s + 1], pow2(-e));
+            for (int c = 0; c < NC; ++c) {
+                Op<NT> od[2];   // do as it came
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                dl_f4 x = {0.f, 0.f, 0.f, 0.f};
+                for (int s = 0; s < 2; ++s) od[s] = split8<NT>(dd[c][2 * s], dd[c][2 * s + 1], pow2(-e));
 #pragma unroll
-                for (int s = t / 2; s < 2; ++s) x = mm(pf[upper_frag(t, s)], od[s], x);
+                for (int t = 0; t < 4; ++t) {
+                    dl_f4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    u[t][r] = __builtin_amdgcn_ldexpf(te[t][r], ek + eS) * u[t][r] + py * x[r];
-                    y[t][r] = be[t][r] * u[t][r];
+                    for (int s = t / 2; s < 2; ++s) x = mm(pf[upper_frag(t, s)], od[s], x);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) u[c][t][r] = te[t][r] * u[c][t][r] + py * x[r];
                 }
             }
         }
-        // z = du - X^T (beta du); then f y and f do for the state
-        const int eu = wave_exp(y);
+        // z = du - (diag(beta) X)^T du; then y for the state
+        const int eu = max(wave_exp(u), kLeast);
+        const float px = pow2_sum(eu + ex), su = pow2(-eu);
         Op<NT> kc[2][2], qc[2][2];
         dl_f4 f0[4];
 #pragma unroll
@@ -151,42 +165,48 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
             qc[0][s] = lds_cols<NT, KS>(qs, 0, s, lane);
         }
         in_order();
-        {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
             Op<NM> bu[2];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) bu[s] = split8<NM>(y[2 * s], y[2 * s + 1], pow2(-eu));
-            dl_f4 *p = (dl_f4 *)d.zs + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 4 * 64 + lane;
+            for (int s = 0; s < 2; ++s) bu[s] = split8<NM>(u[c][2 * s], u[c][2 * s + 1], su);
+            dl_f4 *p = (dl_f4 *)d.zs + (ch * col_tiles(a.Dv, 1) + c0 / 16 + c) * 4 * 64 + lane;
+            const bool keep = !MAPS && c0 + 16 * c < a.Dv;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                dl_f4 x = {0.f, 0.f, 0.f, 0.f};
+                dl_f4 x = {0.f, 0.f, 0.f, 0.f}, z;
 #pragma unroll
                 for (int s = t / 2; s < 2; ++s) x = mm(xf[upper_frag(t, s)], bu[s], x);
-                dl_f4 z;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) z[r] = u[t][r] - __builtin_amdgcn_ldexpf(x[r], eu + ex);
-                if constexpr (!MAPS) p[t * 64] = z;
+                for (int r = 0; r < 4; ++r) z[r] = u[c][t][r] - px * x[r];
+                if (keep) p[t * 64] = z;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    y[t][r] = be[t][r] * z[r];
-                    u[t][r] = -f0[t][r] * y[t][r];
-                    dd[t][r] *= f0[t][r] * a.scale;
-                }
+                for (int r = 0; r < 4; ++r) y[c][t][r] = be[t][r] * z[r];
             }
         }
-        const int ez = wave_exp(y), esc = scale_exp(mag(a.scale)) + 13;   // 2^esc: at most the scale
-        if (!MAPS && lane == 0) d.exps[ch * kDeltaTiles + c0 / 16] = make_int4(ez, max(min(eS, 114), -126), ed, 0);
+        const int ez = max(wave_exp(y), kLeast), esc = scale_exp(mag(a.scale)) + 13;   // 2^esc: at most the scale
+        if (!MAPS && lane < NC && c0 + 16 * lane < a.Dv)
+            d.exps[ch * kDeltaTiles + c0 / 16 + lane] = make_int4(ez, max(min(eS, 114), -126), ed, 0);
         // dS <- exp(G_63) dS' + Q^T (f do) - K^T (f y), both in units of the larger one's scale; of
         // 2^-60 of dS' where both are smaller than that
         const int En = max(max(ek + ez + ef, eq + ed + ef + esc + 1), max(eS - 60, E - 100));
         const float fs = fl * pow2(max(E - En, -126)), sy = pow2(max(min(ek - En, 127), -126)), so_ = pow2(max(min(eq - En, 127), -126));
         E = En;
-        Op<2> yo[2], qo[2];
+        Op<2> yo[NC][2], qo[NC][2];
+        dl_f4 fy[4];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            yo[s] = split8<2>(u[2 * s], u[2 * s + 1], sy);
-            qo[s] = split8<2>(dd[2 * s], dd[2 * s + 1], so_);
+        for (int t = 0; t < 4; ++t) {
+            fy[t] = f0[t] * -sy;
+            f0[t] *= a.scale * so_;
         }
-        dl_f4 x[2];
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                yo[c][s] = split8<2>(y[c][2 * s], y[c][2 * s + 1], fy[2 * s], fy[2 * s + 1]);
+                qo[c][s] = split8<2>(dd[c][2 * s], dd[c][2 * s + 1], f0[2 * s], f0[2 * s + 1]);
+            }
+        dl_f4 x[2][NC];
 #pragma unroll
         for (int t = 0; t < 2 * KS; ++t) {
             if (t + 1 < 2 * KS) {
@@ -197,37 +217,48 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
                 }
             }
             in_order();
-            x[t & 1] = dl_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                x[t & 1] = mm(kc[t & 1][s], yo[s], x[t & 1]);
-                x[t & 1] = mm(qc[t & 1][s], qo[s], x[t & 1]);
-            }
-            if (t > 0) {
+            for (int c = 0; c < NC; ++c) {
+                x[t & 1][c] = dl_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int r = 0; r < 4; ++r) S[t - 1][r] = S[t - 1][r] * fs + x[(t - 1) & 1][r];
+                for (int s = 0; s < 2; ++s) {
+                    x[t & 1][c] = mm(kc[t & 1][s], yo[c][s], x[t & 1][c]);
+                    x[t & 1][c] = mm(qc[t & 1][s], qo[c][s], x[t & 1][c]);
+                }
+                if (t > 0) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[c][t - 1][r] = S[c][t - 1][r] * fs + x[(t - 1) & 1][c][r];
+                }
             }
             in_order();
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[2 * KS - 1][r] = S[2 * KS - 1][r] * fs + x[1][r];
-    }
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-    for (int t = 0; t < 2 * KS; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S[t][r] = __builtin_amdgcn_ldexpf(S[t][r], E);
-    if constexpr (MAPS) {
-        if (here) store_map<KS>(a, sg, at_, S, E, lane);
-        return;
+            for (int r = 0; r < 4; ++r) S[c][2 * KS - 1][r] = S[c][2 * KS - 1][r] * fs + x[1][c][r];
     }
-    if (here && on && d.dS0 && seg == 0) {
+    if (!here) return;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
-                if (dk < a.Dk) d.dS0[(bh * a.Dk + dk) * a.Dv + col] = S[t][r];
-            }
+            for (int r = 0; r < 4; ++r) S[c][t][r] = __builtin_amdgcn_ldexpf(S[c][t][r], E);
+    if constexpr (MAPS) {
+        store_map<KS>(a, sg, at_, S, lane);
+    } else if (d.dS0 && seg == 0) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = c0 + 16 * c + c16;
+            if (col >= a.Dv) continue;
+#pragma unroll
+            for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
+                    if (dk < a.Dk) d.dS0[(bh * a.Dk + dk) * a.Dv + col] = S[c][t][r];
+                }
+        }
     }
 }
 
@@ -372,8 +403,8 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
                     inner[r] += x[r] * y[r];
                 }
                 uint32_t p[2][2], q[2][2];
-                split2<2>(x[0], x[1], sS, p[0]); split2<2>(x[2], x[3], sS, p[1]);
-                split2<2>(y[0], y[1], sE, q[0]); split2<2>(y[2], y[3], sE, q[1]);
+                split2<2>(x[0], sS, x[1], sS, p[0]); split2<2>(x[2], sS, x[3], sS, p[1]);
+                split2<2>(y[0], sE, y[1], sE, q[0]); split2<2>(y[2], sE, y[3], sE, q[1]);
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
                     ((uint2 *)(lds + Lds::S))[to + m * 2 * KS * 128] = make_uint2(p[0][m], p[1][m]);
@@ -396,8 +427,8 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
                     if (on && row < room) IO<DT>::st(p, (long)r * a.H * a.Dv, row < nt ? x[r] : 0.f);
                 }
                 uint32_t f[2][2], q[2][2];
-                split2<2>(x[0], x[1], sy, f[0]); split2<2>(x[2], x[3], sy, f[1]);
-                split2<2>(y[0], y[1], su, q[0]); split2<2>(y[2], y[3], su, q[1]);
+                split2<2>(x[0], sy, x[1], sy, f[0]); split2<2>(x[2], sy, x[3], sy, f[1]);
+                split2<2>(y[0], su, y[1], su, q[0]); split2<2>(y[2], su, y[3], su, q[1]);
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
                     ((uint2 *)(lds + Lds::y))[to + m * 4 * 128] = make_uint2(f[0][m], f[1][m]);
@@ -609,21 +640,31 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
         for (int j = 0; j < TT; ++j) store(t, j, ONE ? zero : tq[ONE ? 0 : t][j], ONE ? zero : tk[ONE ? 0 : t][j]);
 }
 
-template <int DT, int KS> hipError_t bwd_of(const DeltaArgs &a, const DeltaBuffers &w, const DeltaGrads &d, hipStream_t st) {
-    constexpr int NW = 4;
-    constexpr int lds = ScanLds<DT, KS, NW, 4>::total, lds2 = GradLds<DT, KS>::total;
+template <int DT, int KS, int NC>
+hipError_t scans_of(const DeltaArgs &a, const DeltaBuffers &w, const DeltaGrads &d, hipStream_t st) {
+    constexpr int NW = 4, lds = ScanLds<DT, KS, NW * NC, 4>::total;
     const DeltaSegments sg = w.seg;
     const long bh = (long)a.B * a.H;
     hipError_t e;
     if (sg.G > 1) {
-        if ((e = lds_room(delta_bwd_scan_kernel<DT, KS, NW, true>, lds)) != hipSuccess) return e;
-        delta_bwd_scan_kernel<DT, KS, NW, true><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW) + col_tiles(a.Dk, NW))), 64 * NW, lds, st>>>(
+        if ((e = lds_room(delta_bwd_scan_kernel<DT, KS, NW, NC, true>, lds)) != hipSuccess) return e;
+        delta_bwd_scan_kernel<DT, KS, NW, NC, true><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW * NC) + col_tiles(a.Dk, NW * NC))), 64 * NW, lds, st>>>(
             a, sg, w.back, w.kq, d);
         if ((e = launch_delta_join(a, sg, d.dS, true, st)) != hipSuccess) return e;
     }
-    if ((e = lds_room(delta_bwd_scan_kernel<DT, KS, NW, false>, lds)) != hipSuccess) return e;
-    delta_bwd_scan_kernel<DT, KS, NW, false><<<(unsigned)(bh * sg.G * col_tiles(a.Dv, NW)), 64 * NW, lds, st>>>(a, sg, w.back, w.kq, d);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if ((e = lds_room(delta_bwd_scan_kernel<DT, KS, NW, NC, false>, lds)) != hipSuccess) return e;
+    delta_bwd_scan_kernel<DT, KS, NW, NC, false><<<(unsigned)(bh * sg.G * col_tiles(a.Dv, NW * NC)), 64 * NW, lds, st>>>(a, sg, w.back, w.kq, d);
+    return hipGetLastError();
+}
+
+template <int DT, int KS> hipError_t bwd_of(const DeltaArgs &a, const DeltaBuffers &w, const DeltaGrads &d, hipStream_t st) {
+    constexpr int lds2 = GradLds<DT, KS>::total;
+    hipError_t e;
+    if constexpr (DT != F32)
+        e = w.seg.NC == 2 ? scans_of<DT, KS, 2>(a, w, d, st) : scans_of<DT, KS, 1>(a, w, d, st);
+    else
+        e = scans_of<DT, KS, 1>(a, w, d, st);
+    if (e != hipSuccess) return e;
     const unsigned grid = (unsigned)((long)a.B * a.Hk * a.N);
     if (a.H == a.Hk) {
         if ((e = lds_room(delta_bwd_chunk_kernel<DT, KS, true>, lds2)) != hipSuccess) return e;

@@ -53,19 +53,26 @@ template <int NA, int NB> __device__ __forceinline__ dl_f4 mm(const Op<NA> &a, c
 __device__ __forceinline__ float low_half(uint32_t w) { return f16_to_f32((uint16_t)(w & 0xffffu)); }
 __device__ __forceinline__ float high_half(uint32_t w) { return f16_to_f32((uint16_t)(w >> 16)); }
 
-// Two floats times a power of two as N pieces, a word each.  Written so that a
-// scale, a rounding or a remainder is one mixed-precision instruction.
-template <int N> __device__ __forceinline__ void split2(float x, float y, float s, uint32_t (&w)[N]) {
-    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-    h2 h = {(_Float16)(x * s), (_Float16)(y * s)};
-    w[0] = __builtin_bit_cast(uint32_t, h);
-    if constexpr (N == 2) w[1] = pack_16x2<F16>(__builtin_fmaf(x, s, -(float)h.x), __builtin_fmaf(y, s, -(float)h.y));
+// x s and y t as N pieces, a word each: mixed-precision instructions take the
+// product, its rounding to half a word and the remainder, which is exact to
+// float32's rounding, in one step each (written in C the compiler forms the halves twice).
+template <int N> __device__ __forceinline__ void split2(float x, float s, float y, float t, uint32_t (&w)[N]) {
+    uint32_t h;
+    asm("v_fma_mixlo_f16 %0, %1, %2, 0" : "=v"(h) : "v"(x), "v"(s));
+    asm("v_fma_mixhi_f16 %0, %1, %2, 0" : "+v"(h) : "v"(y), "v"(t));
+    w[0] = h;
+    if constexpr (N == 2) {
+        float p, q;
+        asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel_hi:[0,0,1]" : "=v"(p) : "v"(x), "v"(s), "v"(h));
+        asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel:[0,0,1] op_sel_hi:[0,0,1]" : "=v"(q) : "v"(y), "v"(t), "v"(h));
+        w[1] = pack_16x2<F16>(p, q);
+    }
 }
 template <int N> __device__ __forceinline__ Op<N> split8(const float (&x)[8], float s) {
     Op<N> o;
     uint32_t w[4][N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) split2<N>(x[2 * i], x[2 * i + 1], s, w[i]);
+    for (int i = 0; i < 4; ++i) split2<N>(x[2 * i], s, x[2 * i + 1], s, w[i]);
 #pragma unroll
     for (int n = 0; n < N; ++n) o.p[n] = make_uint4(w[0][n], w[1][n], w[2][n], w[3][n]);
     return o;
@@ -73,6 +80,19 @@ template <int N> __device__ __forceinline__ Op<N> split8(const float (&x)[8], fl
 template <int N> __device__ __forceinline__ Op<N> split8(dl_f4 a, dl_f4 b, float s) {
     const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     return split8<N>(x, s);
+}
+
+// each row times its own factor
+template <int N> __device__ __forceinline__ Op<N> split8(dl_f4 a, dl_f4 b, dl_f4 s, dl_f4 t) {
+    Op<N> o;
+    uint32_t w[4][N];
+    split2<N>(a[0], s[0], a[1], s[1], w[0]);
+    split2<N>(a[2], s[2], a[3], s[3], w[1]);
+    split2<N>(b[0], t[0], b[1], t[1], w[2]);
+    split2<N>(b[2], t[2], b[3], t[3], w[3]);
+#pragma unroll
+    for (int n = 0; n < N; ++n) o.p[n] = make_uint4(w[0][n], w[1][n], w[2][n], w[3][n]);
+    return o;
 }
 
 // -------------------------------------------------------------- scales -----
@@ -84,6 +104,11 @@ __device__ __forceinline__ int scale_exp(uint32_t bits) {
     return e < -126 ? -126 : e;
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }   // -126 .. 127
+// the same for sums of exponents: 0 where it would leave float32 at the bottom.  Exponents of
+// operands are kLeast at least, so that what this drops is no part of the sum it belongs to
+// (of a value of 2^-67 or less fewer bits go in).
+constexpr int kLeast = -80;
+__device__ __forceinline__ float pow2_sum(int e) { return e < -126 ? 0.f : pow2(e > 127 ? 127 : e); }
 __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
 // the larger of m and the magnitudes of two values
@@ -92,13 +117,15 @@ __device__ __forceinline__ float max3_abs(float m, float x, float y) {
     return m;
 }
 // the exponent for x of the whole wave
-template <int N> __device__ __forceinline__ int wave_exp(const dl_f4 (&x)[N]) {
+template <int M, int N> __device__ __forceinline__ int wave_exp(const dl_f4 (&x)[M][N]) {
     float m = 0.f;
 #pragma unroll
-    for (int t = 0; t < N; ++t) {
-        m = max3_abs(m, x[t][0], x[t][1]);
-        m = max3_abs(m, x[t][2], x[t][3]);
-    }
+    for (int c = 0; c < M; ++c)
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            m = max3_abs(m, x[c][t][0], x[c][t][1]);
+            m = max3_abs(m, x[c][t][2], x[c][t][3]);
+        }
     return scale_exp(__builtin_amdgcn_readfirstlane(group_max<64>(__float_as_uint(m))));
 }
 
@@ -281,25 +308,25 @@ __device__ __forceinline__ int tokens_of(const DeltaArgs &a, int b) {
 }
 
 // ---------------------------------------------- bringing in a scan's chunk ---
-// A workgroup of NW waves keeps in LDS a chunk's keys and queries, its record (MP
+// A workgroup of NW waves, CT columns of 16, keeps in LDS a chunk's keys and queries, its record (MP
 // pieces of triangular matrices and the gates) and the workgroup's columns of V or
 // do.  All of it is copied from memory as it lies there, 1 KB an instruction, without
 // passing through registers, and, where two fit, while the chunk before is worked on.
 // Nothing is cleared: rows behind the end are copies of the last token (their beta
 // is 0, their rows of X and P are 0, and what they would output is not stored), columns behind
 // Dv copies of the first ones (not stored either).
-template <int DT, int KS, int NW, int MP> struct ScanLds {
+template <int DT, int KS, int CT, int MP> struct ScanLds {
     static constexpr int words = MP * MAT + GATES, kq = kq_words<KS>(pieces<DT>());   // uint4
-    static constexpr int vrow = 16 * NW, v16 = DC * vrow * (int)sizeof(typename IO<DT>::T) / 16;
+    static constexpr int vrow = 16 * CT, v16 = DC * vrow * (int)sizeof(typename IO<DT>::T) / 16;
     static constexpr int k = 0, q = kq, v = 2 * kq, rec = v + v16, one = rec + words;
     static constexpr bool two = 2 * one * 16 <= 160 * 1024;
     static constexpr int total = (two ? 2 : 1) * one * 16;
     static_assert(total <= 160 * 1024, "LDS of a CU");
 };
 
-template <int DT, int KS, int NW, int MP> struct ChunkCopy {
+template <int DT, int KS, int NW, int CT, int MP> struct ChunkCopy {
     typedef typename IO<DT>::T T;
-    typedef ScanLds<DT, KS, NW, MP> Lds;
+    typedef ScanLds<DT, KS, CT, MP> Lds;
     const uint4 *kq, *rec;   // this key head's and this value head's chunks
     const T *v;              // this value head's row of the first token, at the workgroup's first column
     long vstride;            // elements from token to token
@@ -351,18 +378,18 @@ template <int DT, int KS, int NW, int MP> struct ChunkCopy {
 };
 
 // ---------------------------------------------------------------- segments ---
-// workgroups of NW waves of 16 columns
-constexpr int col_tiles(int cols, int NW) { return (cols + 16 * NW - 1) / (16 * NW); }
+// workgroups of n times 16 columns
+constexpr int col_tiles(int cols, int n) { return (cols + 16 * n - 1) / (16 * n); }
 
 // What a workgroup of a scan works on: a (b, h), a segment, its columns.  With MAPS
 // there are the columns of V from a zero state, and then the unit matrix's
 // from no values; no map is needed of the last segment (BACK: of the first).
-template <int NW, bool MAPS, bool BACK = false> struct ScanPlace {
+template <int NW, int NC, bool MAPS, bool BACK = false> struct ScanPlace {
     long bh;
     int b, h, seg, cb, c0, width;   // width: columns there are
     bool unit;
     __device__ __forceinline__ ScanPlace(const DeltaArgs &a, const DeltaSegments &sg, unsigned block, int w) {
-        const int v = col_tiles(a.Dv, NW), tiles = v + (MAPS ? col_tiles(a.Dk, NW) : 0), segs = sg.G - (MAPS ? 1 : 0);
+        const int v = col_tiles(a.Dv, NW * NC), tiles = v + (MAPS ? col_tiles(a.Dk, NW * NC) : 0), segs = sg.G - (MAPS ? 1 : 0);
         const int tile = (int)(block % tiles);
         seg = (int)(block / tiles % segs) + (MAPS && BACK ? 1 : 0);
         bh = block / tiles / segs;
@@ -370,24 +397,27 @@ template <int NW, bool MAPS, bool BACK = false> struct ScanPlace {
         b = (int)(bh / a.H);
         unit = tile >= v;
         width = unit ? a.Dk : a.Dv;
-        cb = (unit ? tile - v : tile) * 16 * NW;
-        c0 = cb + 16 * w;
+        cb = (unit ? tile - v : tile) * 16 * NW * NC;
+        c0 = cb + 16 * NC * w;
     }
 };
 
-// S 2^E as columns of a segment's map: (32 KS, dvp + 32 KS) row-major, its
+// S as columns of a segment's map: (32 KS, dvp + 32 KS) row-major, its
 // second part with the exponent of its scale for every 16 columns.
-template <int KS, typename P>
-__device__ __forceinline__ void store_map(const DeltaArgs &a, const DeltaSegments &sg, const P &at, const dl_f4 (&S)[2 * KS],
-                                          int E, int lane) {
-    const int dvp = (a.Dv + 15) & ~15, row = dvp + 32 * KS;
+template <int KS, int NC, typename P>
+__device__ __forceinline__ void store_map(const DeltaArgs &a, const DeltaSegments &sg, const P &at, const dl_f4 (&S)[NC][2 * KS],
+                                          int lane) {
+    const int dvp = (a.Dv + 15) & ~15, row = dvp + 32 * KS, e = wave_exp(S);
     float *p = sg.maps + ((at.bh * sg.G + at.seg) * 32 * KS + 8 * (lane >> 4)) * row + (at.unit ? dvp : 0) + at.c0 + (lane & 15);
 #pragma unroll
-    for (int t = 0; t < 2 * KS; ++t)
+    for (int c = 0; c < NC; ++c) {
+        if (at.c0 + 16 * c >= at.width) break;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) p[(32 * (t >> 1) + 4 * (t & 1) + r) * row] = S[t][r];
-    const int e = wave_exp(S);
-    if (at.unit && lane == 0) sg.exps[(at.bh * sg.G + at.seg) * 8 + at.c0 / 16] = e;
+        for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) p[(32 * (t >> 1) + 4 * (t & 1) + r) * row + 16 * c] = S[c][t][r];
+        if (at.unit && lane == 0) sg.exps[(at.bh * sg.G + at.seg) * 8 + at.c0 / 16 + c] = e;
+    }
 }
 
 // dynamic LDS above 64 KB has to be asked for

@@ -207,11 +207,15 @@ constexpr size_t delta_rec_bytes(int pieces) { return pieces * kDeltaMatBytes + 
 // for all segments at once, joined in order to the states in front of the segments (in:
 // segment, b, h), and then all segments run at once.  exps: scales of F, every 16 columns.
 struct DeltaSegments {
-    int G, Ns;
+    int G, Ns, NC;   // NC: columns of 16 a wave
     float *maps, *in;
     int *exps;
 };
-int delta_segments(int B, int H, int N, int Dk, int Dv);
+// segments, and columns of 16 a wave
+struct DeltaCut {
+    int G, NC;
+};
+DeltaCut delta_cut(int B, int H, int N, int Dk, int Dv, int dtype);
 constexpr int kDeltaTiles = 16;   // 16 columns each, at most
 struct DeltaBuffers {
     uint4 *rec, *back, *kq;
