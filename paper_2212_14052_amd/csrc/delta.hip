@@ -392,17 +392,14 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
                 for (int f = 0; f < 6; ++f) xo[f] = ld_frag<NX>(xs, f, lane);
             }
             in_order();
+            Op<2> so[NC];
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const Op<2> so = split8<2>(S[c][2 * s], S[c][2 * s + 1], sc);
-                Op<NO> sh;
-#pragma unroll
-                for (int p = 0; p < NO; ++p) sh.p[p] = so.p[p];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) R[c][t] = mm(kf[s & 1][t], so, R[c][t]);
-#pragma unroll
-                for (int t = 0; t < (MAPS ? 0 : 4); ++t) x[c][t] = mm(sh, qf[s & 1][t], x[c][t]);
-            }
+            for (int c = 0; c < NC; ++c) so[c] = split8<2>(S[c][2 * s], S[c][2 * s + 1], sc);
+            mm_each<NT, 2, 4 * NC>([&](int m) -> const Op<NT> & { return kf[s & 1][m % 4]; }, [&](int m) -> const Op<2> & { return so[m / 4]; },
+                                   [&](int m) -> dl_f4 & { return R[m / 4][m % 4]; });
+            if constexpr (!MAPS)
+                mm_each<NO, NT, 4 * NC>([&](int m) -> const Op<2> & { return so[m / 4]; }, [&](int m) -> const Op<NT> & { return qf[s & 1][m % 4]; },
+                                        [&](int m) -> dl_f4 & { return x[m / 4][m % 4]; });
             in_order();
         }
         // R = V - exp(G) K S
@@ -421,24 +418,29 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
 #pragma unroll
         for (int f = 0; f < (MAPS ? 0 : 6); ++f) po[f] = ld_frag<NO>(ps, f, lane);
         in_order();
+        {
+            Op<NX> br[NC][2];
+            dl_f4 y[NC][4];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            Op<NX> br[2];
-            dl_f4 y[4];
+            for (int c = 0; c < NC; ++c) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) br[s] = split8<NX>(R[c][2 * s], R[c][2 * s + 1], sr);
+                for (int s = 0; s < 2; ++s) br[c][s] = split8<NX>(R[c][2 * s], R[c][2 * s + 1], sr);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                y[t] = mm(xo[lower_frag(t, 0)], br[0], dl_f4{0.f, 0.f, 0.f, 0.f});
-                if (t >= 2) y[t] = mm(xo[lower_frag(t, 1)], br[1], y[t]);
+                for (int t = 0; t < 4; ++t) y[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
             }
+            mm_each<NX, NX, 4 * NC>([&](int m) -> const Op<NX> & { return xo[lower_frag(m % 4, 0)]; }, [&](int m) -> const Op<NX> & { return br[m / 4][0]; },
+                                    [&](int m) -> dl_f4 & { return y[m / 4][m % 4]; });
+            mm_each<NX, NX, 2 * NC>([&](int m) -> const Op<NX> & { return xo[lower_frag(2 + m % 2, 1)]; }, [&](int m) -> const Op<NX> & { return br[m / 2][1]; },
+                                    [&](int m) -> dl_f4 & { return y[m / 2][2 + m % 2]; });
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int c = 0; c < NC; ++c)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    R[c][t][r] -= px * y[t][r];
-                    u[c][t][r] = be[t][r] * R[c][t][r];
-                }
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        R[c][t][r] -= px * y[c][t][r];
+                        u[c][t][r] = be[t][r] * R[c][t][r];
+                    }
         }
         const int eu = max(wave_exp(u), kLeast);
         if (!MAPS && es) {
@@ -451,11 +453,14 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
                 if (lane == 0) exps[ch * kDeltaTiles + c0 / 16 + c] = make_int2(eu, max(min(eS, 114), -126));
             }
         }
-        Op<NT> kc[2][2];
+        constexpr int TG = NC == 1 && KS % 2 == 0 ? 4 : 2;   // state tiles at a time
+        Op<NT> kc[2][TG][2];
         dl_f4 te[4];
         float fo[4];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) kc[0][s] = lds_cols<NT, KS>(ks, 0, s, lane);
+        for (int t = 0; t < TG; ++t)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) kc[0][t][s] = lds_cols<NT, KS>(ks, t, s, lane);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             te[t] = *(const dl_f4 *)(gt->toend + 16 * t + 4 * g4);
@@ -471,19 +476,25 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
             for (int t = 0; t < 4; ++t) px[t] = __builtin_amdgcn_ldexpf(fo[t] * a.scale, eq + eS);
             T *oc = o + (((long)b * a.L + n * DC) * a.H + h) * a.Dv + c0;
             const int room = a.L - n * DC;
+            Op<NO> uo[NC][2];
+            dl_f4 y[NC][4];
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                Op<NO> uo[2];
 #pragma unroll
-                for (int s = 0; s < 2; ++s) uo[s] = split8<NO>(u[c][2 * s], u[c][2 * s + 1], su);
+                for (int s = 0; s < 2; ++s) uo[c][s] = split8<NO>(u[c][2 * s], u[c][2 * s + 1], su);
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    dl_f4 y = mm(uo[0], po[lower_frag(t, 0)], dl_f4{0.f, 0.f, 0.f, 0.f});
-                    if (t >= 2) y = mm(uo[1], po[lower_frag(t, 1)], y);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) x[c][t][r] = x[c][t][r] * px[t] + y[r] * py;
-                }
+                for (int t = 0; t < 4; ++t) y[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
             }
+            mm_each<NO, NO, 4 * NC>([&](int m) -> const Op<NO> & { return uo[m / 4][0]; }, [&](int m) -> const Op<NO> & { return po[lower_frag(m % 4, 0)]; },
+                                    [&](int m) -> dl_f4 & { return y[m / 4][m % 4]; });
+            mm_each<NO, NO, 2 * NC>([&](int m) -> const Op<NO> & { return uo[m / 2][1]; }, [&](int m) -> const Op<NO> & { return po[lower_frag(2 + m % 2, 1)]; },
+                                    [&](int m) -> dl_f4 & { return y[m / 2][2 + m % 2]; });
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[c][t][r] = x[c][t][r] * px[t] + y[c][t][r] * py;
             if (nt < DC) {   // the last chunk: places behind the end are 0
 #pragma unroll
                 for (int c = 0; c < NC; ++c)
@@ -514,30 +525,36 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
         for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int s = 0; s < 2; ++s) wo[c][s] = split8<2>(u[c][2 * s], u[c][2 * s + 1], te[2 * s], te[2 * s + 1]);
-        dl_f4 y[2][NC];   // summed from zero: added to S step by step, each step would round it
+        dl_f4 y[2][TG][NC];   // summed from zero: added to S step by step, each step would round it
+        auto add = [&](int q) {
 #pragma unroll
-        for (int t = 0; t < 2 * KS; ++t) {
-            if (t + 1 < 2 * KS) {
+            for (int t = 0; t < TG; ++t)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) kc[(t + 1) & 1][s] = lds_cols<NT, KS>(ks, t + 1, s, lane);
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[c][q * TG + t][r] = S[c][q * TG + t][r] * fs + y[q & 1][t][c][r];
+        };
+#pragma unroll
+        for (int q = 0; q < 2 * KS / TG; ++q) {
+            if (q + 1 < 2 * KS / TG) {
+#pragma unroll
+                for (int t = 0; t < TG; ++t)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) kc[(q + 1) & 1][t][s] = lds_cols<NT, KS>(ks, (q + 1) * TG + t, s, lane);
             }
             in_order();
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                y[t & 1][c] = dl_f4{0.f, 0.f, 0.f, 0.f};
+            for (int t = 0; t < TG; ++t)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) y[t & 1][c] = mm(kc[t & 1][s], wo[c][s], y[t & 1][c]);
-                if (t > 0) {
+                for (int c = 0; c < NC; ++c) y[q & 1][t][c] = dl_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) S[c][t - 1][r] = S[c][t - 1][r] * fs + y[(t - 1) & 1][c][r];
-                }
-            }
+            for (int s = 0; s < 2; ++s)
+                mm_each<NT, 2, TG * NC>([&](int m) -> const Op<NT> & { return kc[q & 1][m / NC][s]; }, [&](int m) -> const Op<2> & { return wo[m % NC][s]; },
+                                        [&](int m) -> dl_f4 & { return y[q & 1][m / NC][m % NC]; });
+            if (q > 0) add(q - 1);
             in_order();
         }
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[c][2 * KS - 1][r] = S[c][2 * KS - 1][r] * fs + y[1][c][r];
+        add(2 * KS / TG - 1);
     }
     if (!here) return;
 #pragma unroll

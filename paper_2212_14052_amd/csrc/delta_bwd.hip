@@ -108,12 +108,11 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
                 }
             }
             in_order();
+            Op<2> so[NC];
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const Op<2> so = split8<2>(S[c][2 * s], S[c][2 * s + 1], sc);
-#pragma unroll
-                for (int t = 0; t < 4; ++t) u[c][t] = mm(kf[s & 1][t], so, u[c][t]);
-            }
+            for (int c = 0; c < NC; ++c) so[c] = split8<2>(S[c][2 * s], S[c][2 * s + 1], sc);
+            mm_each<NT, 2, 4 * NC>([&](int m) -> const Op<NT> & { return kf[s & 1][m % 4]; }, [&](int m) -> const Op<2> & { return so[m / 4]; },
+                                   [&](int m) -> dl_f4 & { return u[m / 4][m % 4]; });
             in_order();
         }
         if (nt < DC) {   // the last chunk: nothing comes from behind the end
@@ -136,52 +135,69 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
                 for (int r = 0; r < 4; ++r) te[t][r] = __builtin_amdgcn_ldexpf(te[t][r], ek + eS);
             const int e = DT == F16 ? 0 : ed;
             const float py = __builtin_amdgcn_ldexpf(a.scale, ep + e);
+            Op<NT> od[NC][2];   // do as it came
+            dl_f4 x[NC][4];
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                Op<NT> od[2];   // do as it came
 #pragma unroll
-                for (int s = 0; s < 2; ++s) od[s] = split8<NT>(dd[c][2 * s], dd[c][2 * s + 1], pow2(-e));
+                for (int s = 0; s < 2; ++s) od[c][s] = split8<NT>(dd[c][2 * s], dd[c][2 * s + 1], pow2(-e));
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    dl_f4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int s = t / 2; s < 2; ++s) x = mm(pf[upper_frag(t, s)], od[s], x);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) u[c][t][r] = te[t][r] * u[c][t][r] + py * x[r];
-                }
+                for (int t = 0; t < 4; ++t) x[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
             }
+            mm_each<NM, NT, 4 * NC>([&](int m) -> const Op<NM> & { return pf[upper_frag(m % 4, 1)]; }, [&](int m) -> const Op<NT> & { return od[m / 4][1]; },
+                                    [&](int m) -> dl_f4 & { return x[m / 4][m % 4]; });
+            mm_each<NM, NT, 2 * NC>([&](int m) -> const Op<NM> & { return pf[upper_frag(m % 2, 0)]; }, [&](int m) -> const Op<NT> & { return od[m / 2][0]; },
+                                    [&](int m) -> dl_f4 & { return x[m / 2][m % 2]; });
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) u[c][t][r] = te[t][r] * u[c][t][r] + py * x[c][t][r];
         }
         // z = du - (diag(beta) X)^T du; then y for the state
         const int eu = max(wave_exp(u), kLeast);
         const float px = pow2_sum(eu + ex), su = pow2(-eu);
-        Op<NT> kc[2][2], qc[2][2];
+        Op<NT> kc[2][2][2], qc[2][2][2];   // two state tiles at a time
         dl_f4 f0[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) f0[t] = *(const dl_f4 *)(gt->from0 + 16 * t + 4 * g4);
         const float fl = gt->from0[DC - 1];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            kc[0][s] = lds_cols<NT, KS>(ks, 0, s, lane);
-            qc[0][s] = lds_cols<NT, KS>(qs, 0, s, lane);
-        }
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                kc[0][t][s] = lds_cols<NT, KS>(ks, t, s, lane);
+                qc[0][t][s] = lds_cols<NT, KS>(qs, t, s, lane);
+            }
         in_order();
+        {
+            Op<NM> bu[NC][2];
+            dl_f4 x[NC][4];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            Op<NM> bu[2];
+            for (int c = 0; c < NC; ++c) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) bu[s] = split8<NM>(u[c][2 * s], u[c][2 * s + 1], su);
-            dl_f4 *p = (dl_f4 *)d.zs + (ch * col_tiles(a.Dv, 1) + c0 / 16 + c) * 4 * 64 + lane;
-            const bool keep = !MAPS && c0 + 16 * c < a.Dv;
+                for (int s = 0; s < 2; ++s) bu[c][s] = split8<NM>(u[c][2 * s], u[c][2 * s + 1], su);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                dl_f4 x = {0.f, 0.f, 0.f, 0.f}, z;
+                for (int t = 0; t < 4; ++t) x[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+            }
+            mm_each<NM, NM, 4 * NC>([&](int m) -> const Op<NM> & { return xf[upper_frag(m % 4, 1)]; }, [&](int m) -> const Op<NM> & { return bu[m / 4][1]; },
+                                    [&](int m) -> dl_f4 & { return x[m / 4][m % 4]; });
+            mm_each<NM, NM, 2 * NC>([&](int m) -> const Op<NM> & { return xf[upper_frag(m % 2, 0)]; }, [&](int m) -> const Op<NM> & { return bu[m / 2][0]; },
+                                    [&](int m) -> dl_f4 & { return x[m / 2][m % 2]; });
 #pragma unroll
-                for (int s = t / 2; s < 2; ++s) x = mm(xf[upper_frag(t, s)], bu[s], x);
+            for (int c = 0; c < NC; ++c) {
+                dl_f4 *p = (dl_f4 *)d.zs + (ch * col_tiles(a.Dv, 1) + c0 / 16 + c) * 4 * 64 + lane;
+                const bool keep = !MAPS && c0 + 16 * c < a.Dv;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) z[r] = u[c][t][r] - px * x[r];
-                if (keep) p[t * 64] = z;
+                for (int t = 0; t < 4; ++t) {
+                    dl_f4 z;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) y[c][t][r] = be[t][r] * z[r];
+                    for (int r = 0; r < 4; ++r) z[r] = u[c][t][r] - px * x[c][t][r];
+                    if (keep) p[t * 64] = z;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) y[c][t][r] = be[t][r] * z[r];
+                }
             }
         }
         const int ez = max(wave_exp(y), kLeast), esc = scale_exp(mag(a.scale)) + 13;   // 2^esc: at most the scale
@@ -206,36 +222,42 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
                 yo[c][s] = split8<2>(y[c][2 * s], y[c][2 * s + 1], fy[2 * s], fy[2 * s + 1]);
                 qo[c][s] = split8<2>(dd[c][2 * s], dd[c][2 * s + 1], f0[2 * s], f0[2 * s + 1]);
             }
-        dl_f4 x[2][NC];
+        dl_f4 x[2][2][NC];
+        auto add = [&](int q) {
 #pragma unroll
-        for (int t = 0; t < 2 * KS; ++t) {
-            if (t + 1 < 2 * KS) {
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    kc[(t + 1) & 1][s] = lds_cols<NT, KS>(ks, t + 1, s, lane);
-                    qc[(t + 1) & 1][s] = lds_cols<NT, KS>(qs, t + 1, s, lane);
-                }
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[c][2 * q + t][r] = S[c][2 * q + t][r] * fs + x[q & 1][t][c][r];
+        };
+#pragma unroll
+        for (int q = 0; q < KS; ++q) {
+            if (q + 1 < KS) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        kc[(q + 1) & 1][t][s] = lds_cols<NT, KS>(ks, 2 * q + 2 + t, s, lane);
+                        qc[(q + 1) & 1][t][s] = lds_cols<NT, KS>(qs, 2 * q + 2 + t, s, lane);
+                    }
             }
             in_order();
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                x[t & 1][c] = dl_f4{0.f, 0.f, 0.f, 0.f};
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    x[t & 1][c] = mm(kc[t & 1][s], yo[c][s], x[t & 1][c]);
-                    x[t & 1][c] = mm(qc[t & 1][s], qo[c][s], x[t & 1][c]);
-                }
-                if (t > 0) {
+                for (int c = 0; c < NC; ++c) x[q & 1][t][c] = dl_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) S[c][t - 1][r] = S[c][t - 1][r] * fs + x[(t - 1) & 1][c][r];
-                }
+            for (int s = 0; s < 2; ++s) {
+                mm_each<NT, 2, 2 * NC>([&](int m) -> const Op<NT> & { return kc[q & 1][m / NC][s]; }, [&](int m) -> const Op<2> & { return yo[m % NC][s]; },
+                                       [&](int m) -> dl_f4 & { return x[q & 1][m / NC][m % NC]; });
+                mm_each<NT, 2, 2 * NC>([&](int m) -> const Op<NT> & { return qc[q & 1][m / NC][s]; }, [&](int m) -> const Op<2> & { return qo[m % NC][s]; },
+                                       [&](int m) -> dl_f4 & { return x[q & 1][m / NC][m % NC]; });
             }
+            if (q > 0) add(q - 1);
             in_order();
         }
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[c][2 * KS - 1][r] = S[c][2 * KS - 1][r] * fs + x[1][c][r];
+        add(KS - 1);
     }
     if (!here) return;
 #pragma unroll
@@ -474,12 +496,9 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
                 Op<NT> oo;
 #pragma unroll
                 for (int m = 0; m < NT; ++m) oo.p[m] = lds[Lds::o + (m * 4 + t) * 64 + lane];
-#pragma unroll
-                for (int j = 0; j < TT; ++j) {
-                    dq[t][j] = mm(so[j], oo, dq[t][j]);
-                    kr[t][j] = mm(so[j], yo, kr[t][j]);
-                    kw[t][j] = mm(to[j], uo, kw[t][j]);
-                }
+                mm_each<2, NT, TT>([&](int j) -> const Op<2> & { return so[j]; }, [&](int) -> const Op<NT> & { return oo; }, [&](int j) -> dl_f4 & { return dq[t][j]; });
+                mm_each<2, 2, 2 * TT>([&](int j) -> const Op<2> & { return j < TT ? so[j % TT] : to[j % TT]; }, [&](int j) -> const Op<2> & { return j < TT ? yo : uo; },
+                                      [&](int j) -> dl_f4 & { return j < TT ? kr[t][j % TT] : kw[t][j % TT]; });
                 if (t <= w) {
                     ad[t] = mm(ow, uo, ad[t]);
                     ae[t] = mm(yw, uo, ae[t]);

@@ -50,6 +50,21 @@ template <int NA, int NB> __device__ __forceinline__ dl_f4 mm(const Op<NA> &a, c
     return c;
 }
 
+// M sums at once, product by product, so that no instruction waits for the one
+// before it: c(m) += a(m) b(m).
+template <int NA, int NB, int M, typename A, typename B, typename C>
+__device__ __forceinline__ void mm_each(A a, B b, C c) {
+    constexpr int N = NA > NB ? NA : NB;
+#pragma unroll
+    for (int s = N - 1; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            if (s - i >= 0 && s - i < NB) {
+#pragma unroll
+                for (int m = 0; m < M; ++m) c(m) = dl_mfma(a(m).p[i], b(m).p[s - i], c(m));
+            }
+}
+
 __device__ __forceinline__ float low_half(uint32_t w) { return f16_to_f32((uint16_t)(w & 0xffffu)); }
 __device__ __forceinline__ float high_half(uint32_t w) { return f16_to_f32((uint16_t)(w >> 16)); }
 
