@@ -59,7 +59,7 @@ struct DeltaBytes {
 // token, the gradient of every chunk's last state, scales, segments' maps).
 struct DeltaWs {
     size_t kq, seg, es, states, exps, kept_kq, dends, bexps, bseg, fwd, saved, bwd, maps, ins;
-    int G, Ns, NC;
+    int G, Ns, NW;
     DeltaWs(int B, int H, int L, int Dk, int Dv, int dtype) {
         const size_t ch = (size_t)B * H * ((L + kDeltaChunk - 1) / kDeltaChunk);
         const size_t dkp = (Dk + 31) / 32 * 32, dvp = (Dv + 15) / 16 * 16;
@@ -69,7 +69,7 @@ struct DeltaWs {
         const int N = (L + kDeltaChunk - 1) / kDeltaChunk;
         const DeltaCut cut = delta_cut(B, H, N, Dk, Dv, dtype);
         G = cut.G;
-        NC = cut.NC;
+        NW = cut.NW;
         Ns = (N + G - 1) / G;
         const size_t sgs = G > 1 ? (size_t)B * H * G : 0;
         maps = align_up(sgs * dkp * (dvp + dkp) * 4);
@@ -87,7 +87,7 @@ struct DeltaWs {
         bwd = bseg + maps + ins + align_up(sgs * 8 * 4);
     }
     DeltaSegments segments(char *at) const {
-        return DeltaSegments{G, Ns, NC, (float *)at, (float *)(at + maps), (int *)(at + maps + ins)};
+        return DeltaSegments{G, Ns, NW, (float *)at, (float *)(at + maps), (int *)(at + maps + ins)};
     }
 };
 

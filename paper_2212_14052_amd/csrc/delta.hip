@@ -282,7 +282,7 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
     }
 }
 
-// NW waves of NC times 16 columns.  es, states, exps: for the backward pass, or null.
+// NW waves of 16 columns.  es, states, exps: for the backward pass, or null.
 //
 // A wave's vector instructions take longer than its matrix instructions here,
 // so scales cost nothing of their own: they ride on the rounding to pieces, on the
@@ -292,19 +292,20 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
 //
 // Sequences may be cut into segments (see DeltaSegments).  With MAPS a workgroup
 // does not produce outputs but its segment's map from state to state.
-template <int DT, int KS, int NW, int NC, bool MAPS>
-__global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, DeltaSegments sg, const uint4 *__restrict__ rec,
+template <int DT, int KS, int NW, bool MAPS>
+__global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_kernel(DeltaArgs a, DeltaSegments sg, const uint4 *__restrict__ rec,
                                                                const uint4 *__restrict__ kq,
                                                                typename IO<DT>::T *__restrict__ o, float *S_final,
                                                                float *__restrict__ es, float *__restrict__ states,
                                                                int2 *__restrict__ exps) {
     typedef typename IO<DT>::T T;
     constexpr int NT = pieces<DT>(), NX = 2, NO = out_pieces<DT>();
-    typedef ChunkCopy<DT, KS, NW, NW * NC, NX + NO> Copy;
+    constexpr int NC = 1;
+    typedef ChunkCopy<DT, KS, NW, NW, NX + NO, MAPS> Copy;
     typedef typename Copy::Lds Lds;
     extern __shared__ uint4 lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
-    const ScanPlace<NW, NC, MAPS> at_(a, sg, blockIdx.x, w);
+    const ScanPlace<NW, MAPS> at_(a, sg, blockIdx.x, w);
     const long bh = at_.bh;
     const int h = at_.h, b = at_.b, hk = h / (a.H / a.Hk), seg = at_.seg, cb = at_.cb, c0 = at_.c0;
     const bool here = c0 < at_.width;       // a wave without columns only helps to copy
@@ -336,7 +337,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
         if (!here) continue;
         const uint4 *ks = at + Lds::k, *qs = at + Lds::q, *xs = at + Lds::rec, *ps = xs + NX * MAT;
         const T *vs = (const T *)(at + Lds::v);
-        const ChunkGates *gt = (const ChunkGates *)(ps + NO * MAT);
+        const ChunkGates *gt = (const ChunkGates *)(at + Lds::gates);
         if (!MAPS && states) {
             dl_f4 *p = (dl_f4 *)states + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;
 #pragma unroll
@@ -391,7 +392,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
 #pragma unroll
                 for (int f = 0; f < 6; ++f) xo[f] = ld_frag<NX>(xs, f, lane);
             }
-            in_order();
+            in_order<NW == 4>();
             Op<2> so[NC];
 #pragma unroll
             for (int c = 0; c < NC; ++c) so[c] = split8<2>(S[c][2 * s], S[c][2 * s + 1], sc);
@@ -400,7 +401,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
             if constexpr (!MAPS)
                 mm_each<NO, NT, 4 * NC>([&](int m) -> const Op<2> & { return so[m / 4]; }, [&](int m) -> const Op<NT> & { return qf[s & 1][m % 4]; },
                                         [&](int m) -> dl_f4 & { return x[m / 4][m % 4]; });
-            in_order();
+            in_order<NW == 4>();
         }
         // R = V - exp(G) K S
 #pragma unroll
@@ -417,7 +418,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
         Op<NO> po[6];
 #pragma unroll
         for (int f = 0; f < (MAPS ? 0 : 6); ++f) po[f] = ld_frag<NO>(ps, f, lane);
-        in_order();
+        in_order<NW == 4>();
         {
             Op<NX> br[NC][2];
             dl_f4 y[NC][4];
@@ -467,7 +468,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
             fo[t] = gt->from0[16 * t + c16];
         }
         const float fl = gt->from0[DC - 1];
-        in_order();
+        in_order<NW == 4>();
         // o = scale (exp(G) Q S + P u)
         if constexpr (!MAPS) {
             const float py = __builtin_amdgcn_ldexpf(a.scale, ep + eu), su = pow2(-eu);
@@ -542,7 +543,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
 #pragma unroll
                     for (int s = 0; s < 2; ++s) kc[(q + 1) & 1][t][s] = lds_cols<NT, KS>(ks, (q + 1) * TG + t, s, lane);
             }
-            in_order();
+            in_order<NW == 4>();
 #pragma unroll
             for (int t = 0; t < TG; ++t)
 #pragma unroll
@@ -552,7 +553,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(DeltaArgs a, Del
                 mm_each<NT, 2, TG * NC>([&](int m) -> const Op<NT> & { return kc[q & 1][m / NC][s]; }, [&](int m) -> const Op<2> & { return wo[m % NC][s]; },
                                         [&](int m) -> dl_f4 & { return y[q & 1][m / NC][m % NC]; });
             if (q > 0) add(q - 1);
-            in_order();
+            in_order<NW == 4>();
         }
         add(2 * KS / TG - 1);
     }
@@ -675,22 +676,21 @@ __global__ __launch_bounds__(256, 1) void delta_join_kernel(DeltaArgs a, DeltaSe
 
 }  // namespace
 
-// How a launch's scans are cut.  A wave of 16 columns takes about one time unit a
-// chunk whatever else runs, one of 32 kWide, and the card holds 256 workgroups of
-// four; the maps of G - 1 of G segments have Dk more columns and no outputs (0.8 units a
-// chunk), joining them takes about one unit each.
+// How a launch's scans are cut.  A workgroup of four waves takes about one time
+// unit (4 us) a chunk on a CU of its own, one of eight 1.5; two workgroups of eight that form
+// maps share a CU and take kMaps; joining takes about 1.3 units a segment.
 DeltaCut delta_cut(int B, int H, int N, int Dk, int Dv, int dtype) {
-    constexpr double kWide = 1.25;
+    constexpr double kMaps = 1.3;
     const double bh = (double)B * H;
-    DeltaCut best{1, 1};
+    DeltaCut best{1, 4};
     double least = 0;
-    for (int NC = 1; NC <= (dtype == F32 ? 1 : 2); ++NC)
+    for (int NW = 4; NW <= (dtype == F32 ? 4 : 8); NW += 4)
         for (int G = 1; G <= 64 && (G == 1 || 4 * G <= N); ++G) {
-            const double v = col_tiles(Dv, 4 * NC), k = col_tiles(Dk, 4 * NC), Ns = (N + G - 1) / G, unit = NC == 1 ? 1.0 : kWide;
-            double t = unit * ceil(bh * v * G / 256) * Ns;
-            if (G > 1) t += unit * 0.8 * ceil(bh * (v + k) * (G - 1) / 256) * Ns + G + 5;
-            if ((NC == 1 && G == 1) || t < 0.95 * least) {
-                best = DeltaCut{G, NC};
+            const double Ns = (N + G - 1) / G;
+            double t = (NW == 4 ? 1.0 : 1.5) * ceil(bh * col_tiles(Dv, NW) * G / 256) * Ns;
+            if (G > 1) t += kMaps * ceil(bh * (col_tiles(Dv, 8) + col_tiles(Dk, 8)) * (G - 1) / 512) * Ns + 1.3 * G + 5;
+            if ((NW == 4 && G == 1) || t < 0.95 * least) {
+                best = DeltaCut{G, NW};
                 least = t;
             }
         }
@@ -699,33 +699,34 @@ DeltaCut delta_cut(int B, int H, int N, int Dk, int Dv, int dtype) {
 
 namespace {
 
-template <int DT, int KS, int NC>
-hipError_t scans_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_final, hipStream_t st) {
+template <int DT, int KS, int NW>
+hipError_t scan_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_final, hipStream_t st) {
     typedef typename IO<DT>::T T;
-    constexpr int NW = 4, lds = ScanLds<DT, KS, NW * NC, 2 + out_pieces<DT>()>::total;
-    const DeltaSegments sg = w.seg;
-    const long bh = (long)a.B * a.H;
-    hipError_t e;
-    if (sg.G > 1) {
-        if ((e = lds_room(delta_scan_kernel<DT, KS, NW, NC, true>, lds)) != hipSuccess) return e;
-        delta_scan_kernel<DT, KS, NW, NC, true><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW * NC) + col_tiles(a.Dk, NW * NC))), 64 * NW, lds, st>>>(
-            a, sg, w.rec, w.kq, nullptr, nullptr, nullptr, nullptr, nullptr);
-        if ((e = launch_delta_join(a, sg, a.S0, false, st)) != hipSuccess) return e;
-    }
-    if ((e = lds_room(delta_scan_kernel<DT, KS, NW, NC, false>, lds)) != hipSuccess) return e;
-    delta_scan_kernel<DT, KS, NW, NC, false><<<(unsigned)(bh * sg.G * col_tiles(a.Dv, NW * NC)), 64 * NW, lds, st>>>(
-        a, sg, w.rec, w.kq, (T *)o, S_final, w.es, w.states, w.exps);
+    constexpr int lds = ScanLds<DT, KS, NW, 2 + out_pieces<DT>()>::total;
+    const hipError_t e = lds_room(delta_scan_kernel<DT, KS, NW, false>, lds);
+    if (e != hipSuccess) return e;
+    delta_scan_kernel<DT, KS, NW, false><<<(unsigned)((long)a.B * a.H * w.seg.G * col_tiles(a.Dv, NW)), 64 * NW, lds, st>>>(
+        a, w.seg, w.rec, w.kq, (T *)o, S_final, w.es, w.states, w.exps);
     return hipGetLastError();
 }
 
 template <int DT, int KS>
 hipError_t fwd_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_final, hipStream_t st) {
-    delta_chunk_kernel<DT, KS><<<(unsigned)((long)a.B * a.H * a.N), 256, 0, st>>>(a, w.rec, w.back, w.kq);
-    const hipError_t e = hipGetLastError();
+    const long bh = (long)a.B * a.H;
+    delta_chunk_kernel<DT, KS><<<(unsigned)(bh * a.N), 256, 0, st>>>(a, w.rec, w.back, w.kq);
+    hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
+    const DeltaSegments sg = w.seg;
+    if (sg.G > 1) {
+        constexpr int NW = 8, lds = ScanLds<DT, KS, NW, 2 + out_pieces<DT>(), true>::total;
+        if ((e = lds_room(delta_scan_kernel<DT, KS, NW, true>, lds)) != hipSuccess) return e;
+        delta_scan_kernel<DT, KS, NW, true><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW) + col_tiles(a.Dk, NW))), 64 * NW, lds, st>>>(
+            a, sg, w.rec, w.kq, nullptr, nullptr, nullptr, nullptr, nullptr);
+        if ((e = launch_delta_join(a, sg, a.S0, false, st)) != hipSuccess) return e;
+    }
     if constexpr (DT != F32)
-        if (w.seg.NC == 2) return scans_of<DT, KS, 2>(a, w, o, S_final, st);
-    return scans_of<DT, KS, 1>(a, w, o, S_final, st);
+        if (sg.NW == 8) return scan_of<DT, KS, 8>(a, w, o, S_final, st);
+    return scan_of<DT, KS, 4>(a, w, o, S_final, st);
 }
 
 template <int DT> hipError_t fwd_by(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_final, hipStream_t st) {

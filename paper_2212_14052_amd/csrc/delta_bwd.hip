@@ -18,16 +18,17 @@
 namespace h3 {
 namespace {
 
-template <int DT, int KS, int NW, int NC, bool MAPS>
-__global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a, DeltaSegments sg, const uint4 *__restrict__ rec,
+template <int DT, int KS, int NW, bool MAPS>
+__global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaArgs a, DeltaSegments sg, const uint4 *__restrict__ rec,
                                                                    const uint4 *__restrict__ kq, DeltaGrads d) {
     typedef typename IO<DT>::T T;
     constexpr int NT = pieces<DT>(), NM = 2;
-    typedef ChunkCopy<DT, KS, NW, NW * NC, 2 * NM> Copy;
+    constexpr int NC = 1;
+    typedef ChunkCopy<DT, KS, NW, NW, 2 * NM> Copy;
     typedef typename Copy::Lds Lds;
     extern __shared__ uint4 lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
-    const ScanPlace<NW, NC, MAPS, true> at_(a, sg, blockIdx.x, w);
+    const ScanPlace<NW, MAPS, true> at_(a, sg, blockIdx.x, w);
     const long bh = at_.bh;
     const int h = at_.h, b = at_.b, hk = h / (a.H / a.Hk), seg = at_.seg, cb = at_.cb, c0 = at_.c0;
     const bool here = c0 < at_.width;
@@ -58,7 +59,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
         if (!here) continue;
         const uint4 *ks = at + Lds::k, *qs = at + Lds::q, *xs = at + Lds::rec, *ps = xs + NM * MAT;   // (diag(beta) X)^T, P^T
         const T *vs = (const T *)(at + Lds::v);
-        const ChunkGates *gt = (const ChunkGates *)(ps + NM * MAT);
+        const ChunkGates *gt = (const ChunkGates *)(at + Lds::gates);
         const int nt = min(DC, len - n * DC);
         if constexpr (!MAPS) {
             dl_f4 *p = (dl_f4 *)d.dends + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;
@@ -107,13 +108,13 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
                     be[t] = *(const dl_f4 *)(gt->beta + 16 * t + 4 * g4);
                 }
             }
-            in_order();
+            in_order<NW == 4>();
             Op<2> so[NC];
 #pragma unroll
             for (int c = 0; c < NC; ++c) so[c] = split8<2>(S[c][2 * s], S[c][2 * s + 1], sc);
             mm_each<NT, 2, 4 * NC>([&](int m) -> const Op<NT> & { return kf[s & 1][m % 4]; }, [&](int m) -> const Op<2> & { return so[m / 4]; },
                                    [&](int m) -> dl_f4 & { return u[m / 4][m % 4]; });
-            in_order();
+            in_order<NW == 4>();
         }
         if (nt < DC) {   // the last chunk: nothing comes from behind the end
 #pragma unroll
@@ -126,7 +127,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
         const int ed = max(wave_exp(dd), kLeast);
 #pragma unroll
         for (int f = 0; f < 6; ++f) xf[f] = ld_frag<NM>(xs, f, lane);
-        in_order();
+        in_order<NW == 4>();
         dl_f4 y[NC][4];
         {
 #pragma unroll
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
                 kc[0][t][s] = lds_cols<NT, KS>(ks, t, s, lane);
                 qc[0][t][s] = lds_cols<NT, KS>(qs, t, s, lane);
             }
-        in_order();
+        in_order<NW == 4>();
         {
             Op<NM> bu[NC][2];
             dl_f4 x[NC][4];
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
                         qc[(q + 1) & 1][t][s] = lds_cols<NT, KS>(qs, 2 * q + 2 + t, s, lane);
                     }
             }
-            in_order();
+            in_order<NW == 4>();
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -255,7 +256,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_bwd_scan_kernel(DeltaArgs a,
                                        [&](int m) -> dl_f4 & { return x[q & 1][m / NC][m % NC]; });
             }
             if (q > 0) add(q - 1);
-            in_order();
+            in_order<NW == 4>();
         }
         add(KS - 1);
     }
@@ -659,20 +660,20 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
         for (int j = 0; j < TT; ++j) store(t, j, ONE ? zero : tq[ONE ? 0 : t][j], ONE ? zero : tk[ONE ? 0 : t][j]);
 }
 
-template <int DT, int KS, int NC>
+template <int DT, int KS, int NW>
 hipError_t scans_of(const DeltaArgs &a, const DeltaBuffers &w, const DeltaGrads &d, hipStream_t st) {
-    constexpr int NW = 4, lds = ScanLds<DT, KS, NW * NC, 4>::total;
+    constexpr int lds = ScanLds<DT, KS, NW, 4>::total;
     const DeltaSegments sg = w.seg;
     const long bh = (long)a.B * a.H;
     hipError_t e;
     if (sg.G > 1) {
-        if ((e = lds_room(delta_bwd_scan_kernel<DT, KS, NW, NC, true>, lds)) != hipSuccess) return e;
-        delta_bwd_scan_kernel<DT, KS, NW, NC, true><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW * NC) + col_tiles(a.Dk, NW * NC))), 64 * NW, lds, st>>>(
+        if ((e = lds_room(delta_bwd_scan_kernel<DT, KS, NW, true>, lds)) != hipSuccess) return e;
+        delta_bwd_scan_kernel<DT, KS, NW, true><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW) + col_tiles(a.Dk, NW))), 64 * NW, lds, st>>>(
             a, sg, w.back, w.kq, d);
         if ((e = launch_delta_join(a, sg, d.dS, true, st)) != hipSuccess) return e;
     }
-    if ((e = lds_room(delta_bwd_scan_kernel<DT, KS, NW, NC, false>, lds)) != hipSuccess) return e;
-    delta_bwd_scan_kernel<DT, KS, NW, NC, false><<<(unsigned)(bh * sg.G * col_tiles(a.Dv, NW * NC)), 64 * NW, lds, st>>>(a, sg, w.back, w.kq, d);
+    if ((e = lds_room(delta_bwd_scan_kernel<DT, KS, NW, false>, lds)) != hipSuccess) return e;
+    delta_bwd_scan_kernel<DT, KS, NW, false><<<(unsigned)(bh * sg.G * col_tiles(a.Dv, NW)), 64 * NW, lds, st>>>(a, sg, w.back, w.kq, d);
     return hipGetLastError();
 }
 
@@ -680,9 +681,9 @@ template <int DT, int KS> hipError_t bwd_of(const DeltaArgs &a, const DeltaBuffe
     constexpr int lds2 = GradLds<DT, KS>::total;
     hipError_t e;
     if constexpr (DT != F32)
-        e = w.seg.NC == 2 ? scans_of<DT, KS, 2>(a, w, d, st) : scans_of<DT, KS, 1>(a, w, d, st);
+        e = w.seg.NW == 8 ? scans_of<DT, KS, 8>(a, w, d, st) : scans_of<DT, KS, 4>(a, w, d, st);
     else
-        e = scans_of<DT, KS, 1>(a, w, d, st);
+        e = scans_of<DT, KS, 4>(a, w, d, st);
     if (e != hipSuccess) return e;
     const unsigned grid = (unsigned)((long)a.B * a.Hk * a.N);
     if (a.H == a.Hk) {

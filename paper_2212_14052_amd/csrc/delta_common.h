@@ -272,8 +272,11 @@ template <int N> __device__ __forceinline__ Op<N> ld_frag(const uint4 *m, int f,
     for (int n = 0; n < N; ++n) o.p[n] = m[n * MAT + f * FRAG + lane];
     return o;
 }
-// Nothing is moved over this point, so that what is asked for ahead of its use is.
-__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+// Nothing is moved over this point, so that what is asked for ahead of its use is
+// (where a wave has a vector unit for itself; waves that share one need the registers).
+template <bool ON> __device__ __forceinline__ void in_order() {
+    if constexpr (ON) __builtin_amdgcn_sched_barrier(0);
+}
 
 // rows r0 .. r0 + 3 of this lane's column (c0 + lane % 16) of 16-bit or float32 values in LDS, r0 = a + 4 (lane / 16)
 template <int DT>
@@ -323,25 +326,28 @@ __device__ __forceinline__ int tokens_of(const DeltaArgs &a, int b) {
 }
 
 // ---------------------------------------------- bringing in a scan's chunk ---
-// A workgroup of NW waves, CT columns of 16, keeps in LDS a chunk's keys and queries, its record (MP
-// pieces of triangular matrices and the gates) and the workgroup's columns of V or
-// do.  All of it is copied from memory as it lies there, 1 KB an instruction, without
-// passing through registers, and, where two fit, while the chunk before is worked on.
-// Nothing is cleared: rows behind the end are copies of the last token (their beta
-// is 0, their rows of X and P are 0, and what they would output is not stored), columns behind
-// Dv copies of the first ones (not stored either).
-template <int DT, int KS, int CT, int MP> struct ScanLds {
+// A workgroup of NW waves, CT columns of 16, keeps in LDS a chunk's keys and
+// queries, its record (MP pieces of triangular matrices and the gates) and the
+// workgroup's columns of V or do.  All of it is copied from memory as it lies there,
+// 1 KB an instruction, without passing through registers, and, where two fit, while the
+// chunk before is worked on.  Nothing is cleared: rows behind the end are copies of the
+// last token (their beta is 0, their rows of X and P are 0, and what they would output is not
+// stored), columns behind Dv copies of the first ones (not stored either).
+// LEAN: no queries and no P (the first half of a forward record), one chunk at a
+// time, small enough that two workgroups share a CU and wait for each other's turn.
+template <int DT, int KS, int CT, int MP, bool LEAN = false> struct ScanLds {
     static constexpr int words = MP * MAT + GATES, kq = kq_words<KS>(pieces<DT>());   // uint4
     static constexpr int vrow = 16 * CT, v16 = DC * vrow * (int)sizeof(typename IO<DT>::T) / 16;
-    static constexpr int k = 0, q = kq, v = 2 * kq, rec = v + v16, one = rec + words;
-    static constexpr bool two = 2 * one * 16 <= 160 * 1024;
+    static constexpr int k = 0, q = kq, v = LEAN ? kq : 2 * kq, rec = v + v16, mats = LEAN ? 2 * MAT : MP * MAT, gates = rec + mats,
+                         one = gates + GATES;
+    static constexpr bool two = !LEAN && 2 * one * 16 <= 160 * 1024;
     static constexpr int total = (two ? 2 : 1) * one * 16;
     static_assert(total <= 160 * 1024, "LDS of a CU");
 };
 
-template <int DT, int KS, int NW, int CT, int MP> struct ChunkCopy {
+template <int DT, int KS, int NW, int CT, int MP, bool LEAN = false> struct ChunkCopy {
     typedef typename IO<DT>::T T;
-    typedef ScanLds<DT, KS, CT, MP> Lds;
+    typedef ScanLds<DT, KS, CT, MP, LEAN> Lds;
     const uint4 *kq, *rec;   // this key head's and this value head's chunks
     const T *v;              // this value head's row of the first token, at the workgroup's first column
     long vstride;            // elements from token to token
@@ -355,12 +361,18 @@ template <int DT, int KS, int NW, int CT, int MP> struct ChunkCopy {
                      : "v"(off), "s"(__builtin_amdgcn_readfirstlane(to)), "s"(base)
                      : "memory", "m0");
     }
+    // n words from base to word `at` of the buffer
+    template <int N> static __device__ __forceinline__ void copy_words(const uint4 *base, uint32_t to, int w, int lane) {
+#pragma unroll
+        for (int i = 0; i < (N + 64 * NW - 1) / (64 * NW); ++i) {
+            const int at = (i * NW + w) * 64 + lane;
+            if (N % (64 * NW) == 0 || at < N) copy(base, (uint32_t)at * 16, to + (i * NW + w) * 1024);
+        }
+    }
     __device__ __forceinline__ void issue(int n, int w, int lane) const {
         const uint32_t to = lds + (Lds::two ? (uint32_t)(n & 1) * Lds::one * 16 : 0u);
         const uint4 *kn = kq + (long)n * 2 * Lds::kq, *rn = rec + (long)n * Lds::words;
-#pragma unroll
-        for (int i = 0; i < 2 * Lds::kq / (64 * NW); ++i)
-            copy(kn, ((i * NW + w) * 64 + lane) * 16, to + (Lds::k + (i * NW + w) * 64) * 16);
+        copy_words<(LEAN ? 1 : 2) * Lds::kq>(kn, to + Lds::k * 16, w, lane);
         const T *vn = v + (long)n * DC * vstride;
         const int last = min(DC, len - n * DC) - 1;
         constexpr int VP = 16 / (int)sizeof(T), VR = Lds::vrow / VP;   // values, words a row
@@ -369,10 +381,11 @@ template <int DT, int KS, int NW, int CT, int MP> struct ChunkCopy {
             const int at = (i * NW + w) * 64 + lane, t = min(at / VR, last), c = VP * (at % VR);
             copy(vn, (uint32_t)((t * vstride + (c < cols ? c : 0)) * sizeof(T)), to + (Lds::v + (i * NW + w) * 64) * 16);
         }
-#pragma unroll
-        for (int i = 0; i < (Lds::words + 64 * NW - 1) / (64 * NW); ++i) {
-            const int at = (i * NW + w) * 64 + lane;
-            if (at < Lds::words) copy(rn, (uint32_t)at * 16, to + (Lds::rec + (i * NW + w) * 64) * 16);
+        if constexpr (LEAN) {
+            copy_words<Lds::mats>(rn, to + Lds::rec * 16, w, lane);
+            if (w == 0 && lane < GATES) copy(rn + MP * MAT, (uint32_t)lane * 16, to + Lds::gates * 16);
+        } else {
+            copy_words<Lds::words>(rn, to + Lds::rec * 16, w, lane);
         }
     }
     // Chunk n is in LDS, for every wave, and chunk `next` (if `more`) under way.
@@ -399,12 +412,12 @@ constexpr int col_tiles(int cols, int n) { return (cols + 16 * n - 1) / (16 * n)
 // What a workgroup of a scan works on: a (b, h), a segment, its columns.  With MAPS
 // there are the columns of V from a zero state, and then the unit matrix's
 // from no values; no map is needed of the last segment (BACK: of the first).
-template <int NW, int NC, bool MAPS, bool BACK = false> struct ScanPlace {
+template <int NW, bool MAPS, bool BACK = false> struct ScanPlace {
     long bh;
     int b, h, seg, cb, c0, width;   // width: columns there are
     bool unit;
     __device__ __forceinline__ ScanPlace(const DeltaArgs &a, const DeltaSegments &sg, unsigned block, int w) {
-        const int v = col_tiles(a.Dv, NW * NC), tiles = v + (MAPS ? col_tiles(a.Dk, NW * NC) : 0), segs = sg.G - (MAPS ? 1 : 0);
+        const int v = col_tiles(a.Dv, NW), tiles = v + (MAPS ? col_tiles(a.Dk, NW) : 0), segs = sg.G - (MAPS ? 1 : 0);
         const int tile = (int)(block % tiles);
         seg = (int)(block / tiles % segs) + (MAPS && BACK ? 1 : 0);
         bh = block / tiles / segs;
@@ -412,8 +425,8 @@ template <int NW, int NC, bool MAPS, bool BACK = false> struct ScanPlace {
         b = (int)(bh / a.H);
         unit = tile >= v;
         width = unit ? a.Dk : a.Dv;
-        cb = (unit ? tile - v : tile) * 16 * NW * NC;
-        c0 = cb + 16 * NC * w;
+        cb = (unit ? tile - v : tile) * 16 * NW;
+        c0 = cb + 16 * w;
     }
 };
 

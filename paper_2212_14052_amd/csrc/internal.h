@@ -207,13 +207,13 @@ constexpr size_t delta_rec_bytes(int pieces) { return pieces * kDeltaMatBytes + 
 // for all segments at once, joined in order to the states in front of the segments (in:
 // segment, b, h), and then all segments run at once.  exps: scales of F, every 16 columns.
 struct DeltaSegments {
-    int G, Ns, NC;   // NC: columns of 16 a wave
+    int G, Ns, NW;   // NW: waves a workgroup
     float *maps, *in;
     int *exps;
 };
-// segments, and columns of 16 a wave
+// segments, and waves a workgroup
 struct DeltaCut {
-    int G, NC;
+    int G, NW;
 };
 DeltaCut delta_cut(int B, int H, int N, int Dk, int Dv, int dtype);
 constexpr int kDeltaTiles = 16;   // 16 columns each, at most
