@@ -214,10 +214,21 @@ class _Here:
 _HERE = _Here()
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _device(dev: torch.device):
     """A context in which `dev` is current: kernels are launched on the current
     device, whatever device their stream belongs to."""
-    return _HERE if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+    return _HERE if dev.index == _current_device() else torch.cuda.device(dev)
+
+
+def _all_on(idx: int, *ts) -> bool:
+    """Whether all of these (or None) are tensors on GPU `idx`: the usual case, told cheaply."""
+    for t in ts:
+        if t is not None and not (isinstance(t, torch.Tensor) and t.get_device() == idx):
+            return False
+    return True
 
 
 # ----------------------------------------------------------------- ops -----
@@ -493,18 +504,18 @@ def layernorm(x: torch.Tensor, w: Optional[torch.Tensor] = None, b: Optional[tor
     if x.dim() < 1:
         raise ValueError("x must be (..., d)")
     d = x.shape[-1]
-    w, b = _f32(w), _f32(b)
     dt = _dtype(x)
-    _on(dev, w=w, b=b)
+    if not _all_on(dev.index, w, b):
+        _on(dev, w=w, b=b)
+    w, b = _f32(w), _f32(b)
     _shape("w", w, (d,)); _shape("b", b, (d,))
     _out("out", out, x.shape, x.dtype, dev)
     y = out if out is not None else torch.empty_like(x)
-    stats = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=dev)
-    mean, rstd = stats[0], stats[1]
+    mean, rstd = x.new_empty((2,) + x.shape[:-1], dtype=torch.float32).unbind(0)
     with _device(dev):
         _check("h3_layernorm", lib().h3_layernorm(
-            _ptr(x), _ptr(w), _ptr(b), x.numel() // d if d else 0, d, eps, dt, _ptr(y), _ptr(mean), _ptr(rstd),
-            _stream(dev)))
+            x.data_ptr(), _ptr(w), _ptr(b), x.numel() // d if d else 0, d, eps, dt, y.data_ptr(), mean.data_ptr(),
+            rstd.data_ptr(), _stream(dev)))
     return y, mean, rstd
 
 
@@ -539,16 +550,18 @@ def layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, w: Optional[torch.Tensor], 
 def _delta_args(q, k, v, g, beta):
     """Checked (q, k, v, g, beta), contiguous, gates in float32, and their sizes."""
     dev = _gpu("q", q)
-    _on(dev, k=k, v=v, g=g, beta=beta)
-    if q.dim() != 4 or v.dim() != 4:
+    if not _all_on(dev.index, k, v, g, beta):
+        _on(dev, k=k, v=v, g=g, beta=beta)
+    qs, vs = q.shape, v.shape
+    if len(qs) != 4 or len(vs) != 4:
         raise ValueError("q must be (B, L, Hk, Dk) and v (B, L, H, Dv)")
-    Bn, L, Hk, Dk = q.shape
-    H, Dv = v.shape[2], v.shape[3]
+    Bn, L, Hk, Dk = qs
+    H, Dv = vs[2], vs[3]
     dt = _dtype(q)
     if k.dtype != q.dtype or v.dtype != q.dtype:
         raise ValueError("q, k and v must have the same dtype")
-    _shape("k", k, (Bn, L, Hk, Dk)); _shape("v", v, (Bn, L, H, Dv))
-    _shape("g", g, (Bn, L, H)); _shape("beta", beta, (Bn, L, H))
+    gs = (Bn, L, H)
+    _shape("k", k, qs); _shape("v", v, (Bn, L, H, Dv)); _shape("g", g, gs); _shape("beta", beta, gs)
     return dev, q.contiguous(), k.contiguous(), v.contiguous(), _f32(g), _f32(beta), (Bn, L, H, Hk, Dk, Dv, dt)
 
 
@@ -564,8 +577,8 @@ def delta_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, g: torch.Tenso
     o = out if out is not None else torch.empty_like(v)
     with _device(dev):
         _check("h3_delta_step", lib().h3_delta_step(
-            _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), Dk ** -0.5 if scale is None else scale, Bn, T, H, Hk, Dk, Dv,
-            dt, _ptr(S), _ptr(o), _stream(dev)))
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), Dk ** -0.5 if scale is None else scale,
+            Bn, T, H, Hk, Dk, Dv, dt, S.data_ptr(), o.data_ptr(), _stream(dev)))
     return o
 
 

@@ -9,8 +9,11 @@
 // it is read once; the variance is a second sum over the registers (of squared
 // deviations, not of squares, which would cancel where a row sits far from
 // zero).  A row is held by TPR threads, VEC elements (16 bytes where the width
-// and the pointers allow it) at a time, NV times.  The backward pass walks rows
-// with a fixed grid and keeps the column sums of dw and db in registers; each
+// and the pointers allow it) at a time, NV times.  Workgroups walk over rows: the
+// weight and bias, in float32 twice a 16-bit row's bytes each, stay in registers (read again
+// for every row they were most of the traffic: 17 us instead of XX at 16384 x 768 fp16), and the
+// next row is under way while this one is summed.  The backward pass keeps the column
+// sums of dw and db in registers, too; each
 // workgroup writes one float32 partial row of each to the workspace and a
 // second kernel sums those in a fixed order, so results do not depend on timing.
 // Rows too wide for the registers are read again for each sum.
@@ -87,54 +90,70 @@ constexpr int threads_of(int TPR) { return TPR < 256 ? 256 : TPR; }
 
 template <int DT, int VEC, int NV, int TPR>
 __global__ __launch_bounds__(threads_of(TPR)) void layernorm_kernel(
-    const typename IO<DT>::T *__restrict__ x, const float *__restrict__ w, const float *__restrict__ b, int rows, int d,
-    float eps, typename IO<DT>::T *__restrict__ y, float *__restrict__ mean, float *__restrict__ rstd) {
+    const typename IO<DT>::T *x, const float *__restrict__ w, const float *__restrict__ b, int rows, int d,
+    float eps, typename IO<DT>::T *y, float *__restrict__ mean, float *__restrict__ rstd) {
+    constexpr int RPB = threads_of(TPR) / TPR;   // rows at a time
     __shared__ float lds[TPR > 64 ? TPR / 64 : 1];
     const int t = threadIdx.x % TPR;
-    const long row = (long)blockIdx.x * (threads_of(TPR) / TPR) + threadIdx.x / TPR;
-    if (row >= rows) return;   // whole waves; with TPR >= 256 the grid is exact
-    const typename IO<DT>::T *xr = x + row * d;
-    Raw<DT, VEC> v[NV];
+    const long step = (long)gridDim.x * RPB;
+    long row = (long)blockIdx.x * RPB + threadIdx.x / TPR;
+    if (row >= rows) return;   // whole waves; with TPR >= 256 the grid is at most the rows
+    Raw<DT, VEC> v[NV], next[NV];
+    float wf[NV][VEC], bf[NV][VEC];
+    auto fetch = [&](long r) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * TPR + t) * VEC;
+            if (c < d) next[i] = ld_raw<DT, VEC>(x + r * d + c);
+        }
+    };
+    fetch(row);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (i * TPR + t) * VEC;
-        if (c < d) v[i] = ld_raw<DT, VEC>(xr + c);
-    }
-    float s[1] = {0.f};
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if ((i * TPR + t) * VEC < d) {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) s[0] += to_f<DT>(v[i].v[j]);
+        if (c < d) {
+            ld_par<VEC>(w, c, 1.f, wf[i]);
+            ld_par<VEC>(b, c, 0.f, bf[i]);
         }
-    row_sum<TPR>(s, lds);
-    const float mu = s[0] / (float)d;
-    s[0] = 0.f;
+    }
+    for (; row < rows; row += step) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if ((i * TPR + t) * VEC < d) {
+        for (int i = 0; i < NV; ++i) v[i] = next[i];
+        if (row + step < rows) fetch(row + step);
+        float s[1] = {0.f};
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float e = to_f<DT>(v[i].v[j]) - mu;
-                s[0] += e * e;
+        for (int i = 0; i < NV; ++i)
+            if ((i * TPR + t) * VEC < d) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) s[0] += to_f<DT>(v[i].v[j]);
             }
+        row_sum<TPR>(s, lds);
+        const float mu = s[0] / (float)d;
+        s[0] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if ((i * TPR + t) * VEC < d) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float e = to_f<DT>(v[i].v[j]) - mu;
+                    s[0] += e * e;
+                }
+            }
+        row_sum<TPR>(s, lds);
+        const float r = 1.f / sqrtf(s[0] / (float)d + eps);
+        if (t == 0) {
+            if (mean) mean[row] = mu;
+            if (rstd) rstd[row] = r;
         }
-    row_sum<TPR>(s, lds);
-    const float r = 1.f / sqrtf(s[0] / (float)d + eps);
-    if (t == 0) {
-        if (mean) mean[row] = mu;
-        if (rstd) rstd[row] = r;
-    }
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * TPR + t) * VEC;
-        if (c >= d) continue;
-        float wf[VEC], bf[VEC], o[VEC];
-        ld_par<VEC>(w, c, 1.f, wf);
-        ld_par<VEC>(b, c, 0.f, bf);
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * TPR + t) * VEC;
+            if (c >= d) continue;
+            float o[VEC];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) o[j] = (to_f<DT>(v[i].v[j]) - mu) * r * wf[j] + bf[j];
-        st_vec<DT, VEC>(y + row * d + c, o);
+            for (int j = 0; j < VEC; ++j) o[j] = (to_f<DT>(v[i].v[j]) - mu) * r * wf[i][j] + bf[i][j];
+            st_vec<DT, VEC>(y + row * d + c, o);
+        }
     }
 }
 
@@ -169,8 +188,8 @@ __global__ __launch_bounds__(1024) void layernorm_wide_kernel(
 // part: (gridDim.x, 2, d) float32, or null where neither dw nor db is asked
 template <int DT, int VEC, int NV, int TPR>
 __global__ __launch_bounds__(threads_of(TPR)) void layernorm_bwd_kernel(
-    const typename IO<DT>::T *__restrict__ dy, const typename IO<DT>::T *__restrict__ x, const float *__restrict__ w,
-    const float *__restrict__ mean, const float *__restrict__ rstd, int rows, int d, typename IO<DT>::T *__restrict__ dx,
+    const typename IO<DT>::T *dy, const typename IO<DT>::T *x, const float *__restrict__ w,
+    const float *__restrict__ mean, const float *__restrict__ rstd, int rows, int d, typename IO<DT>::T *dx,
     float *__restrict__ part) {
     constexpr int RPB = threads_of(TPR) / TPR;   // rows at a time
     __shared__ float lds[TPR > 64 ? 2 * TPR / 64 : 1];
@@ -185,17 +204,31 @@ __global__ __launch_bounds__(threads_of(TPR)) void layernorm_bwd_kernel(
         if (c < d) ld_par<VEC>(w, c, 1.f, wf[i]);
     }
     const float inv = 1.f / (float)d;
-    for (long row = (long)blockIdx.x * RPB + sub; row < rows; row += (long)gridDim.x * RPB) {
-        Raw<DT, VEC> vx[NV], vy[NV];
+    const long step = (long)gridDim.x * RPB;
+    Raw<DT, VEC> vx[NV], vy[NV], nx[NV], ny[NV];
+    float nmu = 0.f, nr = 0.f;
+    auto fetch = [&](long row) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * TPR + t) * VEC;
             if (c < d) {
-                vx[i] = ld_raw<DT, VEC>(x + row * d + c);
-                vy[i] = ld_raw<DT, VEC>(dy + row * d + c);
+                nx[i] = ld_raw<DT, VEC>(x + row * d + c);
+                ny[i] = ld_raw<DT, VEC>(dy + row * d + c);
             }
         }
-        const float mu = mean[row], r = rstd[row];
+        nmu = mean[row];
+        nr = rstd[row];
+    };
+    long row = (long)blockIdx.x * RPB + sub;
+    if (row < rows) fetch(row);
+    for (; row < rows; row += step) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            vx[i] = nx[i];
+            vy[i] = ny[i];
+        }
+        const float mu = nmu, r = nr;
+        if (row + step < rows) fetch(row + step);
         float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -323,18 +356,19 @@ __global__ __launch_bounds__(1024) void layernorm_reduce_kernel(const float *__r
 }
 
 // How a row is laid over threads: 16-byte vectors where every row starts on 16
-// bytes; a wave for a row up to four vectors a lane (no barrier in its sums),
-// else 256 threads, else 1024; tpr 0 where that does not hold it.
+// bytes; a wave where `most` vectors a lane hold the row (no barrier in its sums), else 256
+// threads, else 1024; tpr 0 where those do not hold it.
 struct Shape {
     int vec, nv, tpr;
 };
-Shape shape_of(int d, int dtype, bool aligned) {
+Shape shape_of(int d, int dtype, bool aligned, int most) {
     const int full = dtype == F32 ? 4 : 8;
     Shape s{aligned && d % full == 0 ? full : 1, 0, 0};
+    if (s.vec == 1) most = 8;
     for (int tpr : {64, 256, 1024}) {
         const int nv = (d + tpr * s.vec - 1) / (tpr * s.vec);
-        if (nv <= 4) {
-            s.nv = nv == 3 ? 4 : nv;
+        if (nv <= most) {
+            s.nv = nv;
             s.tpr = tpr;
             break;
         }
@@ -342,33 +376,47 @@ Shape shape_of(int d, int dtype, bool aligned) {
     return s;
 }
 
+// workgroups that walk over the rows
+int fwd_groups(int rows, int tpr) {
+    const int rpb = threads_of(tpr) / tpr, most = tpr == 1024 ? 512 : 2048, want = (rows + rpb - 1) / rpb;
+    return want < most ? want : most;
+}
 int bwd_groups(int rows, int tpr) {
     const int rpb = tpr == 0 ? 1 : threads_of(tpr) / tpr;
-    const int most = tpr == 64 ? 512 : tpr == 256 ? 1024 : 256;
+    const int most = tpr == 64 ? 512 : tpr == 256 ? 768 : 256;
     const int want = (rows + rpb - 1) / rpb;
     return want < most ? want : most;
 }
 
-template <int DT, int VEC, typename F> hipError_t by_shape(const Shape &s, F f) {
-#define H3_LN(TPRV)                                                           \
-    switch (s.nv) {                                                           \
-        case 1: return f(std::integral_constant<int, 1>(), std::integral_constant<int, TPRV>()); \
-        case 2: return f(std::integral_constant<int, 2>(), std::integral_constant<int, TPRV>()); \
-        default: return f(std::integral_constant<int, 4>(), std::integral_constant<int, TPRV>()); \
-    }
-    if (s.tpr == 64) H3_LN(64)
-    if (s.tpr == 256) H3_LN(256)
-    H3_LN(1024)
-#undef H3_LN
+template <int DT, int VEC, int MOST, typename F> hipError_t by_shape(const Shape &s, F f) {
+    auto nv = [&](auto tpr) {
+        switch (s.nv) {
+            case 1: return f(std::integral_constant<int, 1>(), tpr);
+            case 2: return f(std::integral_constant<int, 2>(), tpr);
+            case 3: return f(std::integral_constant<int, 3>(), tpr);
+            case 4: return f(std::integral_constant<int, 4>(), tpr);
+        }
+        if constexpr (VEC == 1 || MOST > 4) {
+            if (s.nv == 5) return f(std::integral_constant<int, 5>(), tpr);
+            if constexpr (VEC > 1) return f(std::integral_constant<int, 6>(), tpr);
+            else return s.nv == 6 ? f(std::integral_constant<int, 6>(), tpr) : f(std::integral_constant<int, 8>(), tpr);
+        }
+        return hipErrorInvalidValue;
+    };
+    if (s.tpr == 64) return nv(std::integral_constant<int, 64>());
+    if (s.tpr == 256) return nv(std::integral_constant<int, 256>());
+    return nv(std::integral_constant<int, 1024>());
 }
+
+constexpr int kMostFwd = 6, kMostBwd = 4;   // vectors of 16 bytes a lane
 
 template <int DT, int VEC>
 hipError_t ln_fwd(const Shape &s, const void *x, const float *w, const float *b, int rows, int d, float eps, void *y,
                   float *mean, float *rstd, hipStream_t st) {
     typedef typename IO<DT>::T T;
-    return by_shape<DT, VEC>(s, [&](auto nv, auto tpr) {
-        constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value, RPB = threads_of(TPR) / TPR;
-        layernorm_kernel<DT, VEC, NV, TPR><<<(unsigned)((rows + RPB - 1) / RPB), threads_of(TPR), 0, st>>>(
+    return by_shape<DT, VEC, kMostFwd>(s, [&](auto nv, auto tpr) {
+        constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value;
+        layernorm_kernel<DT, VEC, NV, TPR><<<(unsigned)fwd_groups(rows, TPR), threads_of(TPR), 0, st>>>(
             (const T *)x, w, b, rows, d, eps, (T *)y, mean, rstd);
         return hipGetLastError();
     });
@@ -378,7 +426,7 @@ template <int DT, int VEC>
 hipError_t ln_bwd(const Shape &s, const void *dy, const void *x, const float *w, const float *mean, const float *rstd,
                   int rows, int d, void *dx, float *part, int G, hipStream_t st) {
     typedef typename IO<DT>::T T;
-    return by_shape<DT, VEC>(s, [&](auto nv, auto tpr) {
+    return by_shape<DT, VEC, kMostBwd>(s, [&](auto nv, auto tpr) {
         constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value;
         layernorm_bwd_kernel<DT, VEC, NV, TPR><<<(unsigned)G, threads_of(TPR), 0, st>>>(
             (const T *)dy, (const T *)x, w, mean, rstd, rows, d, (T *)dx, part);
@@ -390,7 +438,7 @@ template <int DT>
 hipError_t fwd_of(const void *x, const float *w, const float *b, int rows, int d, float eps, void *y, float *mean,
                   float *rstd, hipStream_t st) {
     typedef typename IO<DT>::T T;
-    const Shape s = shape_of(d, DT, (((uintptr_t)x | (uintptr_t)y) & 15) == 0);
+    const Shape s = shape_of(d, DT, (((uintptr_t)x | (uintptr_t)y) & 15) == 0, kMostFwd);
     if (s.tpr == 0) {
         layernorm_wide_kernel<DT><<<(unsigned)rows, 1024, 0, st>>>((const T *)x, w, b, rows, d, eps, (T *)y, mean, rstd);
         return hipGetLastError();
@@ -403,7 +451,7 @@ template <int DT>
 hipError_t bwd_of(const void *dy, const void *x, const float *w, const float *mean, const float *rstd, int rows, int d,
                   void *dx, float *dw, float *db, float *part, hipStream_t st) {
     typedef typename IO<DT>::T T;
-    const Shape s = shape_of(d, DT, (((uintptr_t)x | (uintptr_t)dy | (uintptr_t)dx) & 15) == 0);
+    const Shape s = shape_of(d, DT, (((uintptr_t)x | (uintptr_t)dy | (uintptr_t)dx) & 15) == 0, kMostBwd);
     if (!dw && !db) part = nullptr;
     int G = bwd_groups(rows, s.tpr);
     hipError_t e = hipSuccess;
