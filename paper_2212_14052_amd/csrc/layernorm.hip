@@ -11,7 +11,7 @@
 // zero).  A row is held by TPR threads, VEC elements (16 bytes where the width
 // and the pointers allow it) at a time, NV times.  Workgroups walk over rows: the
 // weight and bias, in float32 twice a 16-bit row's bytes each, stay in registers (read again
-// for every row they were most of the traffic: 17 us instead of XX at 16384 x 768 fp16), and the
+// for every row they were most of the traffic: forward 17.3 us instead of 8.7 at 16384 x 768 fp16), and the
 // next row is under way while this one is summed.  The backward pass keeps the column
 // sums of dw and db in registers, too; each
 // workgroup writes one float32 partial row of each to the workspace and a
@@ -74,10 +74,10 @@ __device__ __forceinline__ void st_vec(typename IO<DT>::T *p, const float (&f)[V
     if constexpr (VEC == 1) {
         IO<DT>::st(p, 0, f[0]);
     } else if constexpr (DT == F32) {
-        *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
+        store_stream(p, __builtin_bit_cast(uint4, make_float4(f[0], f[1], f[2], f[3])));
     } else {
-        *(uint4 *)p = make_uint4(pack_16x2<DT>(f[0], f[1]), pack_16x2<DT>(f[2], f[3]), pack_16x2<DT>(f[4], f[5]),
-                                 pack_16x2<DT>(f[6], f[7]));
+        store_stream(p, make_uint4(pack_16x2<DT>(f[0], f[1]), pack_16x2<DT>(f[2], f[3]), pack_16x2<DT>(f[4], f[5]),
+                                   pack_16x2<DT>(f[6], f[7])));
     }
 }
 // VEC float32 parameters at p (any alignment of 4), or `other` where p is null
@@ -383,7 +383,7 @@ int fwd_groups(int rows, int tpr) {
 }
 int bwd_groups(int rows, int tpr) {
     const int rpb = tpr == 0 ? 1 : threads_of(tpr) / tpr;
-    const int most = tpr == 64 ? 512 : tpr == 256 ? 768 : 256;
+    const int most = tpr == 64 ? 512 : tpr == 256 ? 512 : 256;
     const int want = (rows + rpb - 1) / rpb;
     return want < most ? want : most;
 }
@@ -408,7 +408,7 @@ template <int DT, int VEC, int MOST, typename F> hipError_t by_shape(const Shape
     return nv(std::integral_constant<int, 1024>());
 }
 
-constexpr int kMostFwd = 6, kMostBwd = 4;   // vectors of 16 bytes a lane
+constexpr int kMostFwd = 4, kMostBwd = 4;   // vectors of 16 bytes a lane
 
 template <int DT, int VEC>
 hipError_t ln_fwd(const Shape &s, const void *x, const float *w, const float *b, int rows, int d, float eps, void *y,
