@@ -300,8 +300,7 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
                                                                int2 *__restrict__ exps) {
     typedef typename IO<DT>::T T;
     constexpr int NT = pieces<DT>(), NX = 2, NO = out_pieces<DT>();
-    constexpr int NC = 1;
-    typedef ChunkCopy<DT, KS, NW, NW, NX + NO, MAPS> Copy;
+    typedef ChunkCopy<DT, KS, NW, NX + NO, MAPS> Copy;
     typedef typename Copy::Lds Lds;
     extern __shared__ uint4 lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
@@ -316,19 +315,17 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
                   (const T *)a.v + ((long)b * a.L * a.H + h) * a.Dv + (at_.unit ? 0 : cb), (long)a.H * a.Dv,
                   a.Dv - (at_.unit ? 0 : cb), len, (uint32_t)(uintptr_t)(dl_lds_void *)lds};
 
-    dl_f4 S[NC][2 * KS];
+    dl_f4 S[2 * KS];
     int E = 0;
     const float *S0 = MAPS ? nullptr : sg.G > 1 ? sg.in + ((long)seg * a.B * a.H) * a.Dk * a.Dv : a.S0;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+    for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-        for (int t = 0; t < 2 * KS; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r, col = c0 + 16 * c + c16;
-                S[c][t][r] = S0 && col < a.Dv && dk < a.Dk ? S0[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
-                if (MAPS && at_.unit && dk < a.Dk && dk == col) S[c][t][r] = 1.f;
-            }
+        for (int r = 0; r < 4; ++r) {
+            const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r, col = c0 + c16;
+            S[t][r] = S0 && col < a.Dv && dk < a.Dk ? S0[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
+            if (MAPS && at_.unit && dk < a.Dk && dk == col) S[t][r] = 1.f;
+        }
     if (Lds::two && first < last) in.issue(first, w, lane);
     for (int n = first; n < last; ++n) {
         const int nt = min(DC, len - n * DC);
@@ -341,15 +338,11 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
         if (!MAPS && states) {
             dl_f4 *p = (dl_f4 *)states + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                if (c0 + 16 * c >= a.Dv) break;
+            for (int t = 0; t < 2 * KS; ++t) {
+                dl_f4 y;
 #pragma unroll
-                for (int t = 0; t < 2 * KS; ++t) {
-                    dl_f4 y;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) y[r] = __builtin_amdgcn_ldexpf(S[c][t][r], E);
-                    p[(c * 2 * KS + t) * 64] = y;
-                }
+                for (int r = 0; r < 4; ++r) y[r] = __builtin_amdgcn_ldexpf(S[t][r], E);
+                p[t * 64] = y;
             }
         }
         const int ek = __builtin_amdgcn_readfirstlane(gt->ek), eq = __builtin_amdgcn_readfirstlane(gt->eq),
@@ -357,11 +350,9 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
                   et = __builtin_amdgcn_readfirstlane(gt->et);
         // K S and, transposed (rows are columns of S, so that a lane will hold four
         // consecutive values of one token), Q S
-        dl_f4 R[NC][4], u[NC][4], x[NC][4];
+        dl_f4 R[4], u[4], x[4];
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int t = 0; t < 4; ++t) R[c][t] = x[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < 4; ++t) R[t] = x[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
         Op<NT> kf[2][4], qf[2][4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) kf[0][t] = lds_rows<NT, KS>(ks, t, 0, lane);
@@ -370,7 +361,7 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
         const int em = max(wave_exp(S), kLeast), eS = em + E;   // of the registers, of S
         const float sc = pow2(-em);
         Op<NX> xo[6];
-        dl_f4 be[4], v[NC][4], f0[4];
+        dl_f4 be[4], v[4], f0[4];
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             if (s + 1 < KS) {
@@ -383,24 +374,19 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
                 for (int t = 0; t < 4; ++t) {
                     f0[t] = *(const dl_f4 *)(gt->from0 + 16 * t + 4 * g4);
                     be[t] = *(const dl_f4 *)(gt->beta + 16 * t + 4 * g4);
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) {
-                        v[c][t] = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * (w * NC + c), lane);
-                        if (MAPS && at_.unit) v[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
-                    }
+                    v[t] = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * w, lane);
+                    if (MAPS && at_.unit) v[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
                 }
 #pragma unroll
                 for (int f = 0; f < 6; ++f) xo[f] = ld_frag<NX>(xs, f, lane);
             }
             in_order<NW == 4>();
-            Op<2> so[NC];
-#pragma unroll
-            for (int c = 0; c < NC; ++c) so[c] = split8<2>(S[c][2 * s], S[c][2 * s + 1], sc);
-            mm_each<NT, 2, 4 * NC>([&](int m) -> const Op<NT> & { return kf[s & 1][m % 4]; }, [&](int m) -> const Op<2> & { return so[m / 4]; },
-                                   [&](int m) -> dl_f4 & { return R[m / 4][m % 4]; });
+            const Op<2> so = split8<2>(S[2 * s], S[2 * s + 1], sc);
+            mm_each<NT, 2, 4>([&](int m) -> const Op<NT> & { return kf[s & 1][m]; }, [&](int) -> const Op<2> & { return so; },
+                                   [&](int m) -> dl_f4 & { return R[m]; });
             if constexpr (!MAPS)
-                mm_each<NO, NT, 4 * NC>([&](int m) -> const Op<2> & { return so[m / 4]; }, [&](int m) -> const Op<NT> & { return qf[s & 1][m % 4]; },
-                                        [&](int m) -> dl_f4 & { return x[m / 4][m % 4]; });
+                mm_each<NO, NT, 4>([&](int) -> const Op<2> & { return so; }, [&](int m) -> const Op<NT> & { return qf[s & 1][m]; },
+                                        [&](int m) -> dl_f4 & { return x[m]; });
             in_order<NW == 4>();
         }
         // R = V - exp(G) K S
@@ -409,8 +395,7 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float f = __builtin_amdgcn_ldexpf(f0[t][r], ek + eS);
-#pragma unroll
-                for (int c = 0; c < NC; ++c) R[c][t][r] = v[c][t][r] - f * R[c][t][r];
+                R[t][r] = v[t][r] - f * R[t][r];
             }
         // e = R - (X diag(beta)) R, u = beta e
         const int er = max(wave_exp(R), kLeast);
@@ -420,41 +405,32 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
         for (int f = 0; f < (MAPS ? 0 : 6); ++f) po[f] = ld_frag<NO>(ps, f, lane);
         in_order<NW == 4>();
         {
-            Op<NX> br[NC][2];
-            dl_f4 y[NC][4];
+            Op<NX> br[2];
+            dl_f4 y[4];
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
+            for (int s = 0; s < 2; ++s) br[s] = split8<NX>(R[2 * s], R[2 * s + 1], sr);
 #pragma unroll
-                for (int s = 0; s < 2; ++s) br[c][s] = split8<NX>(R[c][2 * s], R[c][2 * s + 1], sr);
+            for (int t = 0; t < 4; ++t) y[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+            mm_each<NX, NX, 4>([&](int m) -> const Op<NX> & { return xo[lower_frag(m, 0)]; }, [&](int) -> const Op<NX> & { return br[0]; },
+                                    [&](int m) -> dl_f4 & { return y[m]; });
+            mm_each<NX, NX, 2>([&](int m) -> const Op<NX> & { return xo[lower_frag(2 + m, 1)]; }, [&](int) -> const Op<NX> & { return br[1]; },
+                                    [&](int m) -> dl_f4 & { return y[2 + m]; });
 #pragma unroll
-                for (int t = 0; t < 4; ++t) y[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
-            }
-            mm_each<NX, NX, 4 * NC>([&](int m) -> const Op<NX> & { return xo[lower_frag(m % 4, 0)]; }, [&](int m) -> const Op<NX> & { return br[m / 4][0]; },
-                                    [&](int m) -> dl_f4 & { return y[m / 4][m % 4]; });
-            mm_each<NX, NX, 2 * NC>([&](int m) -> const Op<NX> & { return xo[lower_frag(2 + m % 2, 1)]; }, [&](int m) -> const Op<NX> & { return br[m / 2][1]; },
-                                    [&](int m) -> dl_f4 & { return y[m / 2][2 + m % 2]; });
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        R[c][t][r] -= px * y[c][t][r];
-                        u[c][t][r] = be[t][r] * R[c][t][r];
-                    }
+                for (int r = 0; r < 4; ++r) {
+                    R[t][r] -= px * y[t][r];
+                    u[t][r] = be[t][r] * R[t][r];
+                }
         }
         const int eu = max(wave_exp(u), kLeast);
         if (!MAPS && es) {
             dl_f4 *p = (dl_f4 *)es + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 4 * 64 + lane;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                if (c0 + 16 * c >= a.Dv) break;
-#pragma unroll
-                for (int t = 0; t < 4; ++t) p[(4 * c + t) * 64] = R[c][t];
-                if (lane == 0) exps[ch * kDeltaTiles + c0 / 16 + c] = make_int2(eu, max(min(eS, 114), -126));
-            }
+            for (int t = 0; t < 4; ++t) p[t * 64] = R[t];
+            if (lane == 0) exps[ch * kDeltaTiles + c0 / 16] = make_int2(eu, max(min(eS, 114), -126));
         }
-        constexpr int TG = NC == 1 && KS % 2 == 0 ? 4 : 2;   // state tiles at a time
+        constexpr int TG = KS % 2 == 0 ? 4 : 2;   // state tiles at a time
         Op<NT> kc[2][TG][2];
         dl_f4 te[4];
         float fo[4];
@@ -477,63 +453,50 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
             for (int t = 0; t < 4; ++t) px[t] = __builtin_amdgcn_ldexpf(fo[t] * a.scale, eq + eS);
             T *oc = o + (((long)b * a.L + n * DC) * a.H + h) * a.Dv + c0;
             const int room = a.L - n * DC;
-            Op<NO> uo[NC][2];
-            dl_f4 y[NC][4];
+            Op<NO> uo[2];
+            dl_f4 y[4];
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
+            for (int s = 0; s < 2; ++s) uo[s] = split8<NO>(u[2 * s], u[2 * s + 1], su);
 #pragma unroll
-                for (int s = 0; s < 2; ++s) uo[c][s] = split8<NO>(u[c][2 * s], u[c][2 * s + 1], su);
-#pragma unroll
-                for (int t = 0; t < 4; ++t) y[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
-            }
-            mm_each<NO, NO, 4 * NC>([&](int m) -> const Op<NO> & { return uo[m / 4][0]; }, [&](int m) -> const Op<NO> & { return po[lower_frag(m % 4, 0)]; },
-                                    [&](int m) -> dl_f4 & { return y[m / 4][m % 4]; });
-            mm_each<NO, NO, 2 * NC>([&](int m) -> const Op<NO> & { return uo[m / 2][1]; }, [&](int m) -> const Op<NO> & { return po[lower_frag(2 + m % 2, 1)]; },
-                                    [&](int m) -> dl_f4 & { return y[m / 2][2 + m % 2]; });
-#pragma unroll
-            for (int c = 0; c < NC; ++c)
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) x[c][t][r] = x[c][t][r] * px[t] + y[c][t][r] * py;
-            if (nt < DC) {   // the last chunk: places behind the end are 0
-#pragma unroll
-                for (int c = 0; c < NC; ++c)
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) x[c][t][r] = 16 * t + c16 < nt ? x[c][t][r] : 0.f;
-            }
+            for (int t = 0; t < 4; ++t) y[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+            mm_each<NO, NO, 4>([&](int) -> const Op<NO> & { return uo[0]; }, [&](int m) -> const Op<NO> & { return po[lower_frag(m, 0)]; },
+                                    [&](int m) -> dl_f4 & { return y[m]; });
+            mm_each<NO, NO, 2>([&](int) -> const Op<NO> & { return uo[1]; }, [&](int m) -> const Op<NO> & { return po[lower_frag(2 + m, 1)]; },
+                                    [&](int m) -> dl_f4 & { return y[2 + m]; });
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int c = 0; c < NC; ++c)
-                    if (c0 + 16 * c + 4 * g4 < a.Dv && 16 * t + c16 < room) {
-                        T *op = oc + (uint32_t)((16 * t + c16) * a.H * a.Dv + 16 * c + 4 * g4);
-                        if constexpr (DT == F32) *(float4 *)op = make_float4(x[c][t][0], x[c][t][1], x[c][t][2], x[c][t][3]);
-                        else *(uint2 *)op = make_uint2(pack_16x2<DT>(x[c][t][0], x[c][t][1]), pack_16x2<DT>(x[c][t][2], x[c][t][3]));
-                    }
+                for (int r = 0; r < 4; ++r) x[t][r] = x[t][r] * px[t] + y[t][r] * py;
+            if (nt < DC) {   // the last chunk: places behind the end are 0
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[t][r] = 16 * t + c16 < nt ? x[t][r] : 0.f;
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (c0 + 4 * g4 < a.Dv && 16 * t + c16 < room) {
+                    T *op = oc + (uint32_t)((16 * t + c16) * a.H * a.Dv + 4 * g4);
+                    if constexpr (DT == F32) *(float4 *)op = make_float4(x[t][0], x[t][1], x[t][2], x[t][3]);
+                    else *(uint2 *)op = make_uint2(pack_16x2<DT>(x[t][0], x[t][1]), pack_16x2<DT>(x[t][2], x[t][3]));
+                }
         }
         // S <- exp(G_63) S + K^T (exp(G_63 - G) u), in units of the keys' times the errors' scale;
         // of 2^-60 of S where the errors are smaller than that
         const int En = max(ek + eu + et, max(eS - 60, E - 100)), ew = En - ek;
         const float fs = fl * pow2(max(E - En, -126)), sw = pow2(max(min(-ew, 127), -126));
         E = En;
-        Op<2> wo[NC][2];
+        Op<2> wo[2];
 #pragma unroll
         for (int t = 0; t < 4; ++t) te[t] *= sw;
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) wo[c][s] = split8<2>(u[c][2 * s], u[c][2 * s + 1], te[2 * s], te[2 * s + 1]);
-        dl_f4 y[2][TG][NC];   // summed from zero: added to S step by step, each step would round it
+        for (int s = 0; s < 2; ++s) wo[s] = split8<2>(u[2 * s], u[2 * s + 1], te[2 * s], te[2 * s + 1]);
+        dl_f4 y[2][TG];   // summed from zero: added to S step by step, each step would round it
         auto add = [&](int q) {
 #pragma unroll
             for (int t = 0; t < TG; ++t)
 #pragma unroll
-                for (int c = 0; c < NC; ++c)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) S[c][q * TG + t][r] = S[c][q * TG + t][r] * fs + y[q & 1][t][c][r];
+                for (int r = 0; r < 4; ++r) S[q * TG + t][r] = S[q * TG + t][r] * fs + y[q & 1][t][r];
         };
 #pragma unroll
         for (int q = 0; q < 2 * KS / TG; ++q) {
@@ -546,12 +509,11 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
             in_order<NW == 4>();
 #pragma unroll
             for (int t = 0; t < TG; ++t)
-#pragma unroll
-                for (int c = 0; c < NC; ++c) y[q & 1][t][c] = dl_f4{0.f, 0.f, 0.f, 0.f};
+                y[q & 1][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int s = 0; s < 2; ++s)
-                mm_each<NT, 2, TG * NC>([&](int m) -> const Op<NT> & { return kc[q & 1][m / NC][s]; }, [&](int m) -> const Op<2> & { return wo[m % NC][s]; },
-                                        [&](int m) -> dl_f4 & { return y[q & 1][m / NC][m % NC]; });
+                mm_each<NT, 2, TG>([&](int m) -> const Op<NT> & { return kc[q & 1][m][s]; }, [&](int) -> const Op<2> & { return wo[s]; },
+                                        [&](int m) -> dl_f4 & { return y[q & 1][m]; });
             if (q > 0) add(q - 1);
             in_order<NW == 4>();
         }
@@ -559,35 +521,30 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
     }
     if (!here) return;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+    for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-        for (int t = 0; t < 2 * KS; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[c][t][r] = __builtin_amdgcn_ldexpf(S[c][t][r], E);
+        for (int r = 0; r < 4; ++r) S[t][r] = __builtin_amdgcn_ldexpf(S[t][r], E);
     if constexpr (MAPS) {
         store_map<KS>(a, sg, at_, S, lane);
         return;
     }
     const bool write = S_final && last == nb && (first < last || seg == 0);
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        // tokens of this segment's chunks behind the end
-        if (c0 + 16 * c + 4 * g4 < a.Dv)
-            for (int t = max(first, nb) * DC + c16; t < min(a.L, (first + sg.Ns) * DC); t += 16) {
-                T *op = o + (((long)b * a.L + t) * a.H + h) * a.Dv + c0 + 16 * c + 4 * g4;
-                if constexpr (DT == F32) *(float4 *)op = make_float4(0.f, 0.f, 0.f, 0.f);
-                else *(uint2 *)op = make_uint2(0u, 0u);
-            }
-        const int col = c0 + 16 * c + c16;
-        if (write && col < a.Dv) {
-#pragma unroll
-            for (int t = 0; t < 2 * KS; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
-                    if (dk < a.Dk) S_final[(bh * a.Dk + dk) * a.Dv + col] = S[c][t][r];
-                }
+    // tokens of this segment's chunks behind the end
+    if (c0 + 4 * g4 < a.Dv)
+        for (int t = max(first, nb) * DC + c16; t < min(a.L, (first + sg.Ns) * DC); t += 16) {
+            T *op = o + (((long)b * a.L + t) * a.H + h) * a.Dv + c0 + 4 * g4;
+            if constexpr (DT == F32) *(float4 *)op = make_float4(0.f, 0.f, 0.f, 0.f);
+            else *(uint2 *)op = make_uint2(0u, 0u);
         }
+    const int col = c0 + c16;
+    if (write && col < a.Dv) {
+#pragma unroll
+        for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
+                if (dk < a.Dk) S_final[(bh * a.Dk + dk) * a.Dv + col] = S[t][r];
+            }
     }
 }
 
@@ -649,13 +606,13 @@ __global__ __launch_bounds__(256, 1) void delta_join_kernel(DeltaArgs a, DeltaSe
     for (int i = 0; i + 1 < segs; ++i) {
         const int seg = back ? segs - 1 - i : i;
         __syncthreads();
-        dl_f4 S[1][2 * KS], y[TW];
+        dl_f4 S[2 * KS], y[TW];
 #pragma unroll
-        for (int t = 0; t < 2 * KS; ++t) S[0][t] = st[t][lane];
+        for (int t = 0; t < 2 * KS; ++t) S[t] = st[t][lane];
         const int es = wave_exp(S), e = es + ef;
         Op<2> so[KS];
 #pragma unroll
-        for (int s = 0; s < KS; ++s) so[s] = split8<2>(S[0][2 * s], S[0][2 * s + 1], pow2(-es));
+        for (int s = 0; s < KS; ++s) so[s] = split8<2>(S[2 * s], S[2 * s + 1], pow2(-es));
 #pragma unroll
         for (int j = 0; j < TW; ++j) {
             y[j] = dl_f4{0.f, 0.f, 0.f, 0.f};

@@ -23,8 +23,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
                                                                    const uint4 *__restrict__ kq, DeltaGrads d) {
     typedef typename IO<DT>::T T;
     constexpr int NT = pieces<DT>(), NM = 2;
-    constexpr int NC = 1;
-    typedef ChunkCopy<DT, KS, NW, NW, 2 * NM> Copy;
+    typedef ChunkCopy<DT, KS, NW, 2 * NM> Copy;
     typedef typename Copy::Lds Lds;
     extern __shared__ uint4 lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
@@ -39,19 +38,17 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
                   (const T *)d.dout + ((long)b * a.L * a.H + h) * a.Dv + (at_.unit ? 0 : cb), (long)a.H * a.Dv,
                   a.Dv - (at_.unit ? 0 : cb), len, (uint32_t)(uintptr_t)(dl_lds_void *)lds};
 
-    dl_f4 S[NC][2 * KS];   // dS' 2^-E
+    dl_f4 S[2 * KS];   // dS' 2^-E
     int E = 0;
     const float *dS = MAPS ? nullptr : sg.G > 1 ? sg.in + ((long)seg * a.B * a.H) * a.Dk * a.Dv : d.dS;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+    for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-        for (int t = 0; t < 2 * KS; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r, col = c0 + 16 * c + c16;
-                S[c][t][r] = dS && col < a.Dv && dk < a.Dk ? dS[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
-                if (MAPS && at_.unit && dk < a.Dk && dk == col) S[c][t][r] = 1.f;
-            }
+        for (int r = 0; r < 4; ++r) {
+            const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r, col = c0 + c16;
+            S[t][r] = dS && col < a.Dv && dk < a.Dk ? dS[(bh * a.Dk + dk) * a.Dv + col] : 0.f;
+            if (MAPS && at_.unit && dk < a.Dk && dk == col) S[t][r] = 1.f;
+        }
     if (Lds::two && first < last) in.issue(last - 1, w, lane);
     for (int n = last - 1; n >= first; --n) {
         const long ch = bh * a.N + n;
@@ -64,34 +61,28 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
         if constexpr (!MAPS) {
             dl_f4 *p = (dl_f4 *)d.dends + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                if (c0 + 16 * c >= a.Dv) break;
+            for (int t = 0; t < 2 * KS; ++t) {
+                dl_f4 y;
 #pragma unroll
-                for (int t = 0; t < 2 * KS; ++t) {
-                    dl_f4 y;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) y[r] = __builtin_amdgcn_ldexpf(S[c][t][r], E);
-                    p[(c * 2 * KS + t) * 64] = y;
-                }
+                for (int r = 0; r < 4; ++r) y[r] = __builtin_amdgcn_ldexpf(S[t][r], E);
+                p[t * 64] = y;
             }
         }
         const int ek = __builtin_amdgcn_readfirstlane(gt->ek), eq = __builtin_amdgcn_readfirstlane(gt->eq),
                   ex = __builtin_amdgcn_readfirstlane(gt->ex), ep = __builtin_amdgcn_readfirstlane(gt->ep),
                   ef = __builtin_amdgcn_readfirstlane(gt->ef);
         // du = t (K dS') + P^T do
-        dl_f4 u[NC][4], dd[NC][4], te[4], be[4];
+        dl_f4 u[4], dd[4], te[4], be[4];
         Op<NM> pf[6], xf[6];
         Op<NT> kf[2][4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) kf[0][t] = lds_rows<NT, KS>(ks, t, 0, lane);
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                u[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
-                dd[c][t] = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * (w * NC + c), lane);
-                if (MAPS && at_.unit) dd[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
-            }
+        for (int t = 0; t < 4; ++t) {
+            u[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+            dd[t] = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * w, lane);
+            if (MAPS && at_.unit) dd[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+        }
         const int em = max(wave_exp(S), kLeast), eS = em + E;   // of the registers, of dS'
         const float sc = pow2(-em);
 #pragma unroll
@@ -109,26 +100,22 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
                 }
             }
             in_order<NW == 4>();
-            Op<2> so[NC];
-#pragma unroll
-            for (int c = 0; c < NC; ++c) so[c] = split8<2>(S[c][2 * s], S[c][2 * s + 1], sc);
-            mm_each<NT, 2, 4 * NC>([&](int m) -> const Op<NT> & { return kf[s & 1][m % 4]; }, [&](int m) -> const Op<2> & { return so[m / 4]; },
-                                   [&](int m) -> dl_f4 & { return u[m / 4][m % 4]; });
+            const Op<2> so = split8<2>(S[2 * s], S[2 * s + 1], sc);
+            mm_each<NT, 2, 4>([&](int m) -> const Op<NT> & { return kf[s & 1][m]; }, [&](int) -> const Op<2> & { return so; },
+                                   [&](int m) -> dl_f4 & { return u[m]; });
             in_order<NW == 4>();
         }
         if (nt < DC) {   // the last chunk: nothing comes from behind the end
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) dd[c][t][r] = 16 * t + 4 * g4 + r < nt ? dd[c][t][r] : 0.f;
+                for (int r = 0; r < 4; ++r) dd[t][r] = 16 * t + 4 * g4 + r < nt ? dd[t][r] : 0.f;
         }
         const int ed = max(wave_exp(dd), kLeast);
 #pragma unroll
         for (int f = 0; f < 6; ++f) xf[f] = ld_frag<NM>(xs, f, lane);
         in_order<NW == 4>();
-        dl_f4 y[NC][4];
+        dl_f4 y[4];
         {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -136,25 +123,20 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
                 for (int r = 0; r < 4; ++r) te[t][r] = __builtin_amdgcn_ldexpf(te[t][r], ek + eS);
             const int e = DT == F16 ? 0 : ed;
             const float py = __builtin_amdgcn_ldexpf(a.scale, ep + e);
-            Op<NT> od[NC][2];   // do as it came
-            dl_f4 x[NC][4];
+            Op<NT> od[2];   // do as it came
+            dl_f4 x[4];
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
+            for (int s = 0; s < 2; ++s) od[s] = split8<NT>(dd[2 * s], dd[2 * s + 1], pow2(-e));
 #pragma unroll
-                for (int s = 0; s < 2; ++s) od[c][s] = split8<NT>(dd[c][2 * s], dd[c][2 * s + 1], pow2(-e));
+            for (int t = 0; t < 4; ++t) x[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+            mm_each<NM, NT, 4>([&](int m) -> const Op<NM> & { return pf[upper_frag(m, 1)]; }, [&](int) -> const Op<NT> & { return od[1]; },
+                                    [&](int m) -> dl_f4 & { return x[m]; });
+            mm_each<NM, NT, 2>([&](int m) -> const Op<NM> & { return pf[upper_frag(m, 0)]; }, [&](int) -> const Op<NT> & { return od[0]; },
+                                    [&](int m) -> dl_f4 & { return x[m]; });
 #pragma unroll
-                for (int t = 0; t < 4; ++t) x[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
-            }
-            mm_each<NM, NT, 4 * NC>([&](int m) -> const Op<NM> & { return pf[upper_frag(m % 4, 1)]; }, [&](int m) -> const Op<NT> & { return od[m / 4][1]; },
-                                    [&](int m) -> dl_f4 & { return x[m / 4][m % 4]; });
-            mm_each<NM, NT, 2 * NC>([&](int m) -> const Op<NM> & { return pf[upper_frag(m % 2, 0)]; }, [&](int m) -> const Op<NT> & { return od[m / 2][0]; },
-                                    [&](int m) -> dl_f4 & { return x[m / 2][m % 2]; });
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) u[c][t][r] = te[t][r] * u[c][t][r] + py * x[c][t][r];
+                for (int r = 0; r < 4; ++r) u[t][r] = te[t][r] * u[t][r] + py * x[t][r];
         }
         // z = du - (diag(beta) X)^T du; then y for the state
         const int eu = max(wave_exp(u), kLeast);
@@ -173,43 +155,36 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
             }
         in_order<NW == 4>();
         {
-            Op<NM> bu[NC][2];
-            dl_f4 x[NC][4];
+            Op<NM> bu[2];
+            dl_f4 x[4];
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
+            for (int s = 0; s < 2; ++s) bu[s] = split8<NM>(u[2 * s], u[2 * s + 1], su);
 #pragma unroll
-                for (int s = 0; s < 2; ++s) bu[c][s] = split8<NM>(u[c][2 * s], u[c][2 * s + 1], su);
+            for (int t = 0; t < 4; ++t) x[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+            mm_each<NM, NM, 4>([&](int m) -> const Op<NM> & { return xf[upper_frag(m, 1)]; }, [&](int) -> const Op<NM> & { return bu[1]; },
+                                    [&](int m) -> dl_f4 & { return x[m]; });
+            mm_each<NM, NM, 2>([&](int m) -> const Op<NM> & { return xf[upper_frag(m, 0)]; }, [&](int) -> const Op<NM> & { return bu[0]; },
+                                    [&](int m) -> dl_f4 & { return x[m]; });
+            dl_f4 *p = (dl_f4 *)d.zs + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 4 * 64 + lane;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) x[c][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
-            }
-            mm_each<NM, NM, 4 * NC>([&](int m) -> const Op<NM> & { return xf[upper_frag(m % 4, 1)]; }, [&](int m) -> const Op<NM> & { return bu[m / 4][1]; },
-                                    [&](int m) -> dl_f4 & { return x[m / 4][m % 4]; });
-            mm_each<NM, NM, 2 * NC>([&](int m) -> const Op<NM> & { return xf[upper_frag(m % 2, 0)]; }, [&](int m) -> const Op<NM> & { return bu[m / 2][0]; },
-                                    [&](int m) -> dl_f4 & { return x[m / 2][m % 2]; });
+            for (int t = 0; t < 4; ++t) {
+                dl_f4 z;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                dl_f4 *p = (dl_f4 *)d.zs + (ch * col_tiles(a.Dv, 1) + c0 / 16 + c) * 4 * 64 + lane;
-                const bool keep = !MAPS && c0 + 16 * c < a.Dv;
+                for (int r = 0; r < 4; ++r) z[r] = u[t][r] - px * x[t][r];
+                if (!MAPS) p[t * 64] = z;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    dl_f4 z;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) z[r] = u[c][t][r] - px * x[c][t][r];
-                    if (keep) p[t * 64] = z;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) y[c][t][r] = be[t][r] * z[r];
-                }
+                for (int r = 0; r < 4; ++r) y[t][r] = be[t][r] * z[r];
             }
         }
         const int ez = max(wave_exp(y), kLeast), esc = scale_exp(mag(a.scale)) + 13;   // 2^esc: at most the scale
-        if (!MAPS && lane < NC && c0 + 16 * lane < a.Dv)
-            d.exps[ch * kDeltaTiles + c0 / 16 + lane] = make_int4(ez, max(min(eS, 114), -126), ed, 0);
+        if (!MAPS && lane == 0)
+            d.exps[ch * kDeltaTiles + c0 / 16] = make_int4(ez, max(min(eS, 114), -126), ed, 0);
         // dS <- exp(G_63) dS' + Q^T (f do) - K^T (f y), both in units of the larger one's scale; of
         // 2^-60 of dS' where both are smaller than that
         const int En = max(max(ek + ez + ef, eq + ed + ef + esc + 1), max(eS - 60, E - 100));
         const float fs = fl * pow2(max(E - En, -126)), sy = pow2(max(min(ek - En, 127), -126)), so_ = pow2(max(min(eq - En, 127), -126));
         E = En;
-        Op<2> yo[NC][2], qo[NC][2];
+        Op<2> yo[2], qo[2];
         dl_f4 fy[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -217,20 +192,16 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
             f0[t] *= a.scale * so_;
         }
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                yo[c][s] = split8<2>(y[c][2 * s], y[c][2 * s + 1], fy[2 * s], fy[2 * s + 1]);
-                qo[c][s] = split8<2>(dd[c][2 * s], dd[c][2 * s + 1], f0[2 * s], f0[2 * s + 1]);
-            }
-        dl_f4 x[2][2][NC];
+        for (int s = 0; s < 2; ++s) {
+            yo[s] = split8<2>(y[2 * s], y[2 * s + 1], fy[2 * s], fy[2 * s + 1]);
+            qo[s] = split8<2>(dd[2 * s], dd[2 * s + 1], f0[2 * s], f0[2 * s + 1]);
+        }
+        dl_f4 x[2][2];
         auto add = [&](int q) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int c = 0; c < NC; ++c)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) S[c][2 * q + t][r] = S[c][2 * q + t][r] * fs + x[q & 1][t][c][r];
+                for (int r = 0; r < 4; ++r) S[2 * q + t][r] = S[2 * q + t][r] * fs + x[q & 1][t][r];
         };
 #pragma unroll
         for (int q = 0; q < KS; ++q) {
@@ -246,14 +217,13 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
             in_order<NW == 4>();
 #pragma unroll
             for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int c = 0; c < NC; ++c) x[q & 1][t][c] = dl_f4{0.f, 0.f, 0.f, 0.f};
+                x[q & 1][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                mm_each<NT, 2, 2 * NC>([&](int m) -> const Op<NT> & { return kc[q & 1][m / NC][s]; }, [&](int m) -> const Op<2> & { return yo[m % NC][s]; },
-                                       [&](int m) -> dl_f4 & { return x[q & 1][m / NC][m % NC]; });
-                mm_each<NT, 2, 2 * NC>([&](int m) -> const Op<NT> & { return qc[q & 1][m / NC][s]; }, [&](int m) -> const Op<2> & { return qo[m % NC][s]; },
-                                       [&](int m) -> dl_f4 & { return x[q & 1][m / NC][m % NC]; });
+                mm_each<NT, 2, 2>([&](int m) -> const Op<NT> & { return kc[q & 1][m][s]; }, [&](int) -> const Op<2> & { return yo[s]; },
+                                       [&](int m) -> dl_f4 & { return x[q & 1][m]; });
+                mm_each<NT, 2, 2>([&](int m) -> const Op<NT> & { return qc[q & 1][m][s]; }, [&](int) -> const Op<2> & { return qo[s]; },
+                                       [&](int m) -> dl_f4 & { return x[q & 1][m]; });
             }
             if (q > 0) add(q - 1);
             in_order<NW == 4>();
@@ -262,26 +232,21 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
     }
     if (!here) return;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+    for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-        for (int t = 0; t < 2 * KS; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[c][t][r] = __builtin_amdgcn_ldexpf(S[c][t][r], E);
+        for (int r = 0; r < 4; ++r) S[t][r] = __builtin_amdgcn_ldexpf(S[t][r], E);
     if constexpr (MAPS) {
         store_map<KS>(a, sg, at_, S, lane);
     } else if (d.dS0 && seg == 0) {
+        const int col = c0 + c16;
+        if (col >= a.Dv) return;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int col = c0 + 16 * c + c16;
-            if (col >= a.Dv) continue;
+        for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-            for (int t = 0; t < 2 * KS; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
-                    if (dk < a.Dk) d.dS0[(bh * a.Dk + dk) * a.Dv + col] = S[c][t][r];
-                }
-        }
+            for (int r = 0; r < 4; ++r) {
+                const int dk = 32 * (t >> 1) + 8 * g4 + 4 * (t & 1) + r;
+                if (dk < a.Dk) d.dS0[(bh * a.Dk + dk) * a.Dv + col] = S[t][r];
+            }
     }
 }
 

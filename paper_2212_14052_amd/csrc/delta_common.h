@@ -132,15 +132,13 @@ __device__ __forceinline__ float max3_abs(float m, float x, float y) {
     return m;
 }
 // the exponent for x of the whole wave
-template <int M, int N> __device__ __forceinline__ int wave_exp(const dl_f4 (&x)[M][N]) {
+template <int N> __device__ __forceinline__ int wave_exp(const dl_f4 (&x)[N]) {
     float m = 0.f;
 #pragma unroll
-    for (int c = 0; c < M; ++c)
-#pragma unroll
-        for (int t = 0; t < N; ++t) {
-            m = max3_abs(m, x[c][t][0], x[c][t][1]);
-            m = max3_abs(m, x[c][t][2], x[c][t][3]);
-        }
+    for (int t = 0; t < N; ++t) {
+        m = max3_abs(m, x[t][0], x[t][1]);
+        m = max3_abs(m, x[t][2], x[t][3]);
+    }
     return scale_exp(__builtin_amdgcn_readfirstlane(group_max<64>(__float_as_uint(m))));
 }
 
@@ -326,7 +324,7 @@ __device__ __forceinline__ int tokens_of(const DeltaArgs &a, int b) {
 }
 
 // ---------------------------------------------- bringing in a scan's chunk ---
-// A workgroup of NW waves, CT columns of 16, keeps in LDS a chunk's keys and
+// A workgroup of NW waves of 16 columns keeps in LDS a chunk's keys and
 // queries, its record (MP pieces of triangular matrices and the gates) and the
 // workgroup's columns of V or do.  All of it is copied from memory as it lies there,
 // 1 KB an instruction, without passing through registers, and, where two fit, while the
@@ -335,9 +333,9 @@ __device__ __forceinline__ int tokens_of(const DeltaArgs &a, int b) {
 // stored), columns behind Dv copies of the first ones (not stored either).
 // LEAN: no queries and no P (the first half of a forward record), one chunk at a
 // time, small enough that two workgroups share a CU and wait for each other's turn.
-template <int DT, int KS, int CT, int MP, bool LEAN = false> struct ScanLds {
+template <int DT, int KS, int NW, int MP, bool LEAN = false> struct ScanLds {
     static constexpr int words = MP * MAT + GATES, kq = kq_words<KS>(pieces<DT>());   // uint4
-    static constexpr int vrow = 16 * CT, v16 = DC * vrow * (int)sizeof(typename IO<DT>::T) / 16;
+    static constexpr int vrow = 16 * NW, v16 = DC * vrow * (int)sizeof(typename IO<DT>::T) / 16;
     static constexpr int k = 0, q = kq, v = LEAN ? kq : 2 * kq, rec = v + v16, mats = LEAN ? 2 * MAT : MP * MAT, gates = rec + mats,
                          one = gates + GATES;
     static constexpr bool two = !LEAN && 2 * one * 16 <= 160 * 1024;
@@ -345,9 +343,9 @@ template <int DT, int KS, int CT, int MP, bool LEAN = false> struct ScanLds {
     static_assert(total <= 160 * 1024, "LDS of a CU");
 };
 
-template <int DT, int KS, int NW, int CT, int MP, bool LEAN = false> struct ChunkCopy {
+template <int DT, int KS, int NW, int MP, bool LEAN = false> struct ChunkCopy {
     typedef typename IO<DT>::T T;
-    typedef ScanLds<DT, KS, CT, MP, LEAN> Lds;
+    typedef ScanLds<DT, KS, NW, MP, LEAN> Lds;
     const uint4 *kq, *rec;   // this key head's and this value head's chunks
     const T *v;              // this value head's row of the first token, at the workgroup's first column
     long vstride;            // elements from token to token
@@ -432,20 +430,15 @@ template <int NW, bool MAPS, bool BACK = false> struct ScanPlace {
 
 // S as columns of a segment's map: (32 KS, dvp + 32 KS) row-major, its
 // second part with the exponent of its scale for every 16 columns.
-template <int KS, int NC, typename P>
-__device__ __forceinline__ void store_map(const DeltaArgs &a, const DeltaSegments &sg, const P &at, const dl_f4 (&S)[NC][2 * KS],
-                                          int lane) {
+template <int KS, typename P>
+__device__ __forceinline__ void store_map(const DeltaArgs &a, const DeltaSegments &sg, const P &at, const dl_f4 (&S)[2 * KS], int lane) {
     const int dvp = (a.Dv + 15) & ~15, row = dvp + 32 * KS, e = wave_exp(S);
     float *p = sg.maps + ((at.bh * sg.G + at.seg) * 32 * KS + 8 * (lane >> 4)) * row + (at.unit ? dvp : 0) + at.c0 + (lane & 15);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        if (at.c0 + 16 * c >= at.width) break;
+    for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-        for (int t = 0; t < 2 * KS; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) p[(32 * (t >> 1) + 4 * (t & 1) + r) * row + 16 * c] = S[c][t][r];
-        if (at.unit && lane == 0) sg.exps[(at.bh * sg.G + at.seg) * 8 + at.c0 / 16 + c] = e;
-    }
+        for (int r = 0; r < 4; ++r) p[(32 * (t >> 1) + 4 * (t & 1) + r) * row] = S[t][r];
+    if (at.unit && lane == 0) sg.exps[(at.bh * sg.G + at.seg) * 8 + at.c0 / 16] = e;
 }
 
 // dynamic LDS above 64 KB has to be asked for
