@@ -275,9 +275,9 @@ int h3_layer_fwd_heads(const void *x, const void *Wq, const void *Wk, const void
  *   w, b        (d) float32, or NULL for 1 and 0.
  *   eps         >= 0.
  *   mean, rstd  (rows) float32, written, or NULL.  They overlap nothing.
- * Arithmetic in float32.  Any d >= 1; rows and row sizes that are multiples of
+ * Arithmetic in float32.  d up to 2^22; rows and row sizes that are multiples of
  * 16 bytes are read 16 bytes at a time.
- * Errors: EINVAL, EUNSUPPORTED (dtype), EDEVICE.
+ * Errors: EINVAL, EUNSUPPORTED (dtype, d), EDEVICE.
  */
 int h3_layernorm(const void *x, const float *w, const float *b, int rows, int d, float eps, int dtype, void *y,
                  float *mean, float *rstd, void *stream);
@@ -293,7 +293,7 @@ int h3_layernorm(const void *x, const float *w, const float *b, int rows, int d,
  *   dw, db      (d) float32.  Each of dx, dw, db may be NULL, not all three.
  *   workspace   >= h3_workspace_size(H3_OP_LAYERNORM_BWD, rows, d, 1, 0, 0, dtype)
  *               (partial sums of dw and db, added in a fixed order).
- * Errors: EINVAL, EUNSUPPORTED (dtype), EWORKSPACE, EDEVICE.
+ * Errors: EINVAL, EUNSUPPORTED (dtype, d), EWORKSPACE, EDEVICE.
  */
 int h3_layernorm_bwd(const void *dy, const void *x, const float *w, const float *mean, const float *rstd, int rows,
                      int d, int dtype, void *dx, float *dw, float *db, void *workspace, size_t ws_bytes, void *stream);
@@ -311,7 +311,7 @@ int h3_layernorm_bwd(const void *dy, const void *x, const float *w, const float 
  *   S           (B, H, Dk, Dv) float32, 16-byte aligned, read and overwritten.
  *   Dk a multiple of 8 up to H3_DELTA_MAX_DK, Dv one up to H3_DELTA_MAX_DV;
  *   Hk divides H.  Outputs overlap nothing.  Arithmetic in float32.
- * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype), EDEVICE.
+ * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, B H ceil(Dv / 32) >= 2^26), EDEVICE.
  */
 int h3_delta_step(const void *q, const void *k, const void *v, const float *g, const float *beta, float scale, int B,
                   int T, int H, int Hk, int Dk, int Dv, int dtype, float *S, void *o, void *stream);

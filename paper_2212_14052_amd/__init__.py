@@ -223,6 +223,14 @@ def _device(dev: torch.device):
     return _HERE if dev.index == _current_device() else torch.cuda.device(dev)
 
 
+def _rows(t: torch.Tensor) -> int:
+    """Rows of t (..., d): a count that the C entries take as an int."""
+    rows = t.numel() // t.shape[-1] if t.shape[-1] else 0
+    if rows > 2 ** 31 - 1:
+        raise ValueError(f"at most 2^31 - 1 rows a call (got {rows})")
+    return rows
+
+
 def _all_on(idx: int, *ts) -> bool:
     """Whether all of these (or None) are tensors on GPU `idx`: the usual case, told cheaply."""
     for t in ts:
@@ -514,7 +522,7 @@ def layernorm(x: torch.Tensor, w: Optional[torch.Tensor] = None, b: Optional[tor
     mean, rstd = x.new_empty((2,) + x.shape[:-1], dtype=torch.float32).unbind(0)
     with _device(dev):
         _check("h3_layernorm", lib().h3_layernorm(
-            x.data_ptr(), _ptr(w), _ptr(b), x.numel() // d if d else 0, d, eps, dt, y.data_ptr(), mean.data_ptr(),
+            x.data_ptr(), _ptr(w), _ptr(b), _rows(x), d, eps, dt, y.data_ptr(), mean.data_ptr(),
             rstd.data_ptr(), _stream(dev)))
     return y, mean, rstd
 
@@ -532,7 +540,7 @@ def layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, w: Optional[torch.Tensor], 
     if x.shape != dy.shape or x.dtype != dy.dtype:
         raise ValueError("x must match dy in shape and dtype")
     d = dy.shape[-1]
-    rows = dy.numel() // d if d else 0
+    rows = _rows(dy)
     dt = _dtype(dy)
     w, mean, rstd = _f32(w), _f32(mean), _f32(rstd)
     _shape("w", w, (d,)); _shape("mean", mean, dy.shape[:-1]); _shape("rstd", rstd, dy.shape[:-1])
@@ -589,7 +597,7 @@ def _lengths(lengths: Optional[torch.Tensor], Bn: int, dev: torch.device) -> Opt
     _shape("lengths", lengths, (Bn,))
     if lengths.dtype not in (torch.int32, torch.int64):
         raise ValueError(f"lengths must be int32 or int64 (got {lengths.dtype})")
-    return lengths.to(torch.int32).contiguous()
+    return (lengths if lengths.dtype == torch.int32 else lengths.clamp(0, 2 ** 31 - 1).to(torch.int32)).contiguous()
 
 
 def _aligned(t: torch.Tensor) -> torch.Tensor:

@@ -36,11 +36,15 @@ int launched(hipError_t e) { return e == hipSuccess ? H3_OK : H3_EDEVICE; }
 bool delta_sizes_ok(int Dk, int Dv) {
     return Dk >= 8 && Dk % 8 == 0 && Dk <= H3_DELTA_MAX_DK && Dv >= 8 && Dv % 8 == 0 && Dv <= H3_DELTA_MAX_DV;
 }
+int delta_chunks(int L) { return (L - 1) / kDeltaChunk + 1; }
 // its launches hold one workgroup a chunk: at most 2^31 - 1; offsets inside a
 // chunk are 32 bits
 bool delta_chunks_ok(int B, int L, int H, int Dv) {
-    return (double)H * Dv <= 4194304.0 && (double)B * H * ((L + kDeltaChunk - 1) / kDeltaChunk) < 2147483647.0 && (double)B * H * ((Dv + 15) / 16) < 2147483647.0;
+    return (double)H * Dv <= 4194304.0 && (double)B * H * delta_chunks(L) < 2147483647.0 && (double)B * H * ((Dv + 15) / 16) < 2147483647.0;
 }
+bool delta_ok(int B, int L, int H, int Dk, int Dv) { return delta_sizes_ok(Dk, Dv) && delta_chunks_ok(B, L, H, Dv); }
+// width of a normalised row: its launches over columns stay under 2^32 threads
+bool norm_width_ok(int d) { return d <= 1 << 22; }
 // bytes of its tensors: q or k, v or o, g or beta, a state for each head
 struct DeltaBytes {
     size_t qk, v, gate, state;
@@ -61,12 +65,12 @@ struct DeltaWs {
     size_t kq, seg, es, states, exps, kept_kq, dends, bexps, bseg, fwd, saved, bwd, maps, ins;
     int G, Ns, NW;
     DeltaWs(int B, int H, int L, int Dk, int Dv, int dtype) {
-        const size_t ch = (size_t)B * H * ((L + kDeltaChunk - 1) / kDeltaChunk);
+        const size_t ch = (size_t)B * H * delta_chunks(L);
         const size_t dkp = (Dk + 31) / 32 * 32, dvp = (Dv + 15) / 16 * 16;
         const size_t rows = align_up(ch * kDeltaChunk * dvp * 4), state = align_up(ch * dkp * dvp * 4);
         const size_t keys = align_up(ch * 2 * (dtype == H3_F32 ? 2 : 1) * kDeltaChunk * dkp * 2);
         kq = align_up(ch * delta_rec_bytes(dtype == H3_BF16 ? 3 : 4));
-        const int N = (L + kDeltaChunk - 1) / kDeltaChunk;
+        const int N = delta_chunks(L);
         const DeltaCut cut = delta_cut(B, H, N, Dk, Dv, dtype);
         G = cut.G;
         NW = cut.NW;
@@ -297,13 +301,13 @@ size_t h3_workspace_size(int op, int B, int H, int L, int m, int chunk, int dtyp
             if (chunk != 2 && chunk != 4 && chunk != 8) return 0;
             return heads_ws(B, H, L, chunk).total;
         case H3_OP_DELTA:   // m = Dk, chunk = Dv
-            return delta_sizes_ok(m, chunk) ? DeltaWs(B, H, L, m, chunk, dtype).fwd : 0;
+            return delta_ok(B, L, H, m, chunk) ? DeltaWs(B, H, L, m, chunk, dtype).fwd : 0;
         case H3_OP_DELTA_SAVED:
-            return delta_sizes_ok(m, chunk) ? DeltaWs(B, H, L, m, chunk, dtype).saved : 0;
+            return delta_ok(B, L, H, m, chunk) ? DeltaWs(B, H, L, m, chunk, dtype).saved : 0;
         case H3_OP_DELTA_BWD:
-            return delta_sizes_ok(m, chunk) ? DeltaWs(B, H, L, m, chunk, dtype).bwd : 0;
+            return delta_ok(B, L, H, m, chunk) ? DeltaWs(B, H, L, m, chunk, dtype).bwd : 0;
         case H3_OP_LAYERNORM_BWD:   // B = rows, H = d
-            return align_up(layernorm_bwd_workspace(B, H));
+            return norm_width_ok(H) ? align_up(layernorm_bwd_workspace(B, H)) : 0;
         case H3_OP_FFTCONV_BWD: {
             // the spectrum of the du pass; at L = 2048 (16-bit) also room for
             // kernel-gradient partial sums per eight rows, which no kernel
@@ -607,7 +611,7 @@ int h3_layer_fwd_heads(const void *x, const void *Wq, const void *Wk, const void
 int h3_layernorm(const void *x, const float *w, const float *b, int rows, int d, float eps, int dtype, void *y,
                  float *mean, float *rstd, void *stream) {
     if (!x || !y || rows < 1 || d < 1 || !(eps >= 0.f)) return H3_EINVAL;
-    if (!dtype_ok(dtype)) return H3_EUNSUPPORTED;
+    if (!dtype_ok(dtype) || !norm_width_ok(d)) return H3_EUNSUPPORTED;
     const size_t io = (size_t)rows * d * esize(dtype), ps = (size_t)d * 4, rs = (size_t)rows * 4;
     const uintptr_t ea = esize(dtype) - 1;
     if (((uintptr_t)x & ea) || ((uintptr_t)y & ea) || ((uintptr_t)w & 3) || ((uintptr_t)b & 3) || ((uintptr_t)mean & 3) ||
@@ -626,7 +630,7 @@ int h3_layernorm(const void *x, const float *w, const float *b, int rows, int d,
 int h3_layernorm_bwd(const void *dy, const void *x, const float *w, const float *mean, const float *rstd, int rows,
                      int d, int dtype, void *dx, float *dw, float *db, void *workspace, size_t ws_bytes, void *stream) {
     if (!dy || !x || !mean || !rstd || rows < 1 || d < 1 || (!dx && !dw && !db)) return H3_EINVAL;
-    if (!dtype_ok(dtype)) return H3_EUNSUPPORTED;
+    if (!dtype_ok(dtype) || !norm_width_ok(d)) return H3_EUNSUPPORTED;
     const size_t need = h3_workspace_size(H3_OP_LAYERNORM_BWD, rows, d, 1, 0, 0, dtype);
     if (!workspace || ws_bytes < need) return H3_EWORKSPACE;
     const size_t io = (size_t)rows * d * esize(dtype), ps = (size_t)d * 4, rs = (size_t)rows * 4;
@@ -654,7 +658,8 @@ int h3_delta_step(const void *q, const void *k, const void *v, const float *g, c
                   int T, int H, int Hk, int Dk, int Dv, int dtype, float *S, void *o, void *stream) {
     if (!q || !k || !v || !g || !beta || !S || !o || B < 1 || T < 1 || H < 1 || Hk < 1 || Dk < 1 || Dv < 1 || H % Hk)
         return H3_EINVAL;
-    if (!dtype_ok(dtype) || !delta_sizes_ok(Dk, Dv)) return H3_EUNSUPPORTED;
+    if (!dtype_ok(dtype) || !delta_sizes_ok(Dk, Dv) || (double)B * H * ((Dv + 31) / 32) >= 67108864.0)   // 2^26 waves
+        return H3_EUNSUPPORTED;
     const DeltaBytes n(B, T, H, Hk, Dk, Dv, dtype);
     const uintptr_t ea = esize(dtype) - 1;
     if (((uintptr_t)q & ea) || ((uintptr_t)k & ea) || ((uintptr_t)v & ea) || ((uintptr_t)o & ea) || ((uintptr_t)g & 3) ||
@@ -673,7 +678,7 @@ int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, c
                   float *S_final, void *saved, size_t saved_bytes, void *workspace, size_t ws_bytes, void *stream) {
     if (!q || !k || !v || !g || !beta || !o || B < 1 || L < 1 || H < 1 || Hk < 1 || Dk < 1 || Dv < 1 || H % Hk)
         return H3_EINVAL;
-    if (!dtype_ok(dtype) || !delta_sizes_ok(Dk, Dv) || !delta_chunks_ok(B, L, H, Dv)) return H3_EUNSUPPORTED;
+    if (!dtype_ok(dtype) || !delta_ok(B, L, H, Dk, Dv)) return H3_EUNSUPPORTED;
     const DeltaWs w(B, H, L, Dk, Dv, dtype);
     if (!workspace || ws_bytes < w.fwd || (saved && saved_bytes < w.saved)) return H3_EWORKSPACE;
     const DeltaBytes n(B, L, H, Hk, Dk, Dv, dtype);
@@ -691,7 +696,7 @@ int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, c
         for (int j = i + 1; j < 4; ++j)
             if (overlap(outs[i], osz[i], outs[j], osz[j])) return H3_EINVAL;
     }
-    DeltaArgs a{q, k, v, g, beta, lengths, S0, scale, B, L, H, Hk, Dk, Dv, (L + kDeltaChunk - 1) / kDeltaChunk};
+    DeltaArgs a{q, k, v, g, beta, lengths, S0, scale, B, L, H, Hk, Dk, Dv, delta_chunks(L)};
     char *ws = (char *)workspace, *sv = (char *)saved;
     DeltaBuffers d{};
     d.rec = (uint4 *)ws;
@@ -713,7 +718,7 @@ int h3_delta_rule_bwd(const void *q, const void *k, const void *v, const float *
     if (!q || !k || !v || !g || !beta || !dout || !saved || !dq || !dk || !dv || !dg || !dbeta || B < 1 || L < 1 || H < 1 ||
         Hk < 1 || Dk < 1 || Dv < 1 || H % Hk)
         return H3_EINVAL;
-    if (!dtype_ok(dtype) || !delta_sizes_ok(Dk, Dv) || !delta_chunks_ok(B, L, H, Dv)) return H3_EUNSUPPORTED;
+    if (!dtype_ok(dtype) || !delta_ok(B, L, H, Dk, Dv)) return H3_EUNSUPPORTED;
     const DeltaWs w(B, H, L, Dk, Dv, dtype);
     if (!workspace || ws_bytes < w.bwd || saved_bytes < w.saved) return H3_EWORKSPACE;
     const DeltaBytes n(B, L, H, Hk, Dk, Dv, dtype);
@@ -732,7 +737,7 @@ int h3_delta_rule_bwd(const void *q, const void *k, const void *v, const float *
         for (int j = i + 1; j < 7; ++j)
             if (overlap(outs[i], osz[i], outs[j], osz[j])) return H3_EINVAL;
     }
-    DeltaArgs a{q, k, v, g, beta, lengths, nullptr, scale, B, L, H, Hk, Dk, Dv, (L + kDeltaChunk - 1) / kDeltaChunk};
+    DeltaArgs a{q, k, v, g, beta, lengths, nullptr, scale, B, L, H, Hk, Dk, Dv, delta_chunks(L)};
     char *ws = (char *)workspace, *sv = (char *)saved;
     DeltaBuffers d{};
     d.back = (uint4 *)sv;

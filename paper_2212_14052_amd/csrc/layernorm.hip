@@ -409,6 +409,7 @@ template <int DT, int VEC, int MOST, typename F> hipError_t by_shape(const Shape
 }
 
 constexpr int kMostFwd = 4, kMostBwd = 4;   // vectors of 16 bytes a lane
+constexpr int kWideRows = 1 << 21;          // rows a launch with a workgroup of 1024 for each (under 2^32 threads)
 
 template <int DT, int VEC>
 hipError_t ln_fwd(const Shape &s, const void *x, const float *w, const float *b, int rows, int d, float eps, void *y,
@@ -440,7 +441,12 @@ hipError_t fwd_of(const void *x, const float *w, const float *b, int rows, int d
     typedef typename IO<DT>::T T;
     const Shape s = shape_of(d, DT, (((uintptr_t)x | (uintptr_t)y) & 15) == 0, kMostFwd);
     if (s.tpr == 0) {
-        layernorm_wide_kernel<DT><<<(unsigned)rows, 1024, 0, st>>>((const T *)x, w, b, rows, d, eps, (T *)y, mean, rstd);
+        for (int r = 0; r < rows; r += kWideRows) {
+            const int n = rows - r < kWideRows ? rows - r : kWideRows;
+            layernorm_wide_kernel<DT><<<(unsigned)n, 1024, 0, st>>>((const T *)x + (long)r * d, w, b, n, d, eps, (T *)y + (long)r * d,
+                                                                   mean ? mean + r : nullptr, rstd ? rstd + r : nullptr);
+            if (rows - r <= kWideRows) break;
+        }
         return hipGetLastError();
     }
     if (s.vec == 1) return ln_fwd<DT, 1>(s, x, w, b, rows, d, eps, y, mean, rstd, st);
@@ -456,7 +462,12 @@ hipError_t bwd_of(const void *dy, const void *x, const float *w, const float *me
     int G = bwd_groups(rows, s.tpr);
     hipError_t e = hipSuccess;
     if (s.tpr == 0) {
-        if (dx) layernorm_bwd_wide_dx_kernel<DT><<<(unsigned)rows, 1024, 0, st>>>((const T *)dy, (const T *)x, w, mean, rstd, rows, d, (T *)dx);
+        for (int r = 0; dx && r < rows; r += kWideRows) {
+            const int n = rows - r < kWideRows ? rows - r : kWideRows;
+            layernorm_bwd_wide_dx_kernel<DT><<<(unsigned)n, 1024, 0, st>>>((const T *)dy + (long)r * d, (const T *)x + (long)r * d, w,
+                                                                          mean + r, rstd + r, n, d, (T *)dx + (long)r * d);
+            if (rows - r <= kWideRows) break;
+        }
         if (part)
             layernorm_bwd_wide_dw_kernel<DT><<<(unsigned)(((d + 255) / 256) * G), 256, 0, st>>>(
                 (const T *)dy, (const T *)x, mean, rstd, rows, d, part, G);

@@ -34,6 +34,15 @@ def test_layernorm_refusals():
     assert norm(w=Y + 128) == EINVAL                # y over the weight
 
 
+def test_layernorm_widths():
+    assert norm(d=(1 << 22) + 1) == EUNSUP
+    assert norm_bwd(d=(1 << 22) + 1) == EUNSUP
+    assert h3.workspace_size(h3.OP_LAYERNORM_BWD, 4, (1 << 22) + 1, 1, 0, 0, 2) == 0
+    with pytest.raises(ValueError):
+        h3._rows(torch.empty(1, dtype=torch.float16).expand(2 ** 31, 1))
+    assert h3._rows(torch.empty(3, 0)) == 0 and h3._rows(torch.empty(2, 3, 4)) == 6
+
+
 def norm_bwd(dy=V, x=X, w=K, mean=G, rstd=BE, rows=4, d=64, dt=2, dx=Y, dw=S, db=S + 65536, ws=W, wsb=1 << 20):
     return h3.lib().h3_layernorm_bwd(P(dy), P(x), P(w), P(mean), P(rstd), rows, d, dt, P(dx), P(dw), P(db), P(ws), wsb, None)
 
@@ -77,6 +86,7 @@ def test_delta_step_refusals():
     assert step(o=V) == EINVAL                      # output over v
     assert step(o=S + 256) == EINVAL                # output inside the state
     assert step(S=K) == EINVAL
+    assert step(B=1 << 23, H=8, Hk=8, Dk=8, Dv=8, o=O << 8) == EUNSUP      # 2^26 waves
 
 
 def test_binding_refusals():
@@ -111,6 +121,8 @@ def test_delta_rule_refusals():
     for name, bad in (("Dk", 12), ("Dk", 136), ("Dv", 20), ("Dv", 264), ("dt", 4)):
         assert rule(**{name: bad}) == EUNSUP
     assert rule(B=1 << 20, L=1 << 24, H=2, Hk=2, Dk=8, Dv=8) == EUNSUP     # 2^31 chunks and more
+    assert rule(H=65536, Hk=1, Dv=72) == EUNSUP                            # H Dv beyond 2^22
+    assert rule(L=2 ** 31 - 1) == EWS
     assert rule(ws=0) == EWS
     assert rule(wsb=size(h3.OP_DELTA) - 1) == EWS
     assert rule(saved=X, savedb=size(h3.OP_DELTA_SAVED) - 1) == EWS
@@ -154,6 +166,7 @@ def test_delta_rule_bwd_refusals():
 
 
 def test_delta_sizes():
+    assert size(h3.OP_DELTA, H=65536, Dv=72) == 0 and size(h3.OP_DELTA, B=1 << 20, L=1 << 24, H=2) == 0
     assert size(h3.OP_DELTA, Dk=12) == 0 and size(h3.OP_DELTA_SAVED, Dv=0) == 0 and size(h3.OP_DELTA_BWD, L=0) == 0
     # a chunk's state and errors in float32 for every 64 tokens
     assert size(h3.OP_DELTA_SAVED) >= 2 * 4 * 2 * (64 * 64 * 4 + 64 * 64 * 4)
