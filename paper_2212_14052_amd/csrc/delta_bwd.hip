@@ -252,42 +252,47 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
 
 constexpr int AROW = DC + 4;   // floats a row of a 64 x 64 matrix in LDS
 
+template <int KS> constexpr int grad_waves = KS > 2 ? 8 : 4;   // one for each of the key channels' tiles
+
 // LDS of delta_bwd_chunk_kernel, in 16-byte words: first 32 columns at a time of the states, of y and u, and of do,
 // then keys, queries, D and E in the same place.
 template <int DT, int KS> struct GradLds {
-    static constexpr int NT = pieces<DT>();
+    static constexpr int NT = pieces<DT>(), NW = grad_waves<KS>;
     static constexpr int S = 0, dS = S + 4 * KS * 64, y = dS + 4 * KS * 64, u = y + 8 * 64, o = u + 8 * 64, stage = o + NT * 4 * 64;
     static constexpr int kq = kq_words<KS>(NT), k = 0, q = kq, D = 2 * kq, E = D + DC * AROW / 4, after = E + DC * AROW / 4;
     static constexpr int rest = stage > after ? stage : after;
-    static constexpr int gd = rest, gates = gd + DC / 2, red = gates + GATES, rin = red + DC, big = rin + 2, total = (big + 2) * 16;
+    static constexpr int gd = rest, gates = gd + DC / 2, red = gates + GATES, dot = red + NW * DC / 4, rin = dot + DC / 4, big = rin + NW / 2,
+                         total = (big + 2) * 16;
     static_assert(total <= 160 * 1024, "LDS of a CU");
 };
 
-// A workgroup of four waves takes a chunk of a key head and goes through the
+// A workgroup of NW waves takes a chunk of a key head and goes through the
 // value heads that share it (ONE: there is one).  It brings in, 32 columns at a time, the
 // states, z and e of a chunk as the scans left them, cuts them into pieces once for all
 // waves, and reads operands whose summands are columns with transposing reads.  Every wave
-// has KS / 2 (rounded up) of the key channels' tiles for all tokens: results are transposed
+// has one of the key channels' tiles for all tokens: results are transposed
 // (rows are channels), so that a lane holds four consecutive channels of one token; and a row tile
-// of D and E.
+// of D and E, of eight waves the first four of D, the others of E.
 //
 // Bound by HBM: the states alone are as many bytes as the chunk's inputs and
 // gradients together.
 template <int DT, int KS, bool ONE>
-__global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
+__global__ __launch_bounds__(64 * grad_waves<KS>, (KS > 2 || ONE ? 2 : 1)) void delta_bwd_chunk_kernel(
     DeltaArgs a, const uint4 *__restrict__ rec, const uint4 *__restrict__ kq, const float *__restrict__ es,
     const float *__restrict__ states, const int2 *__restrict__ exps, DeltaGrads d) {
     typedef typename IO<DT>::T T;
-    constexpr int NT = pieces<DT>(), TT = (KS + 1) / 2;
     typedef GradLds<DT, KS> Lds;
+    constexpr int NT = pieces<DT>(), NW = Lds::NW, NS = (4 * KS + NW - 1) / NW, NI = 8 / NW;   // tiles of states, of e and z, a wave
     extern __shared__ uint4 lds[];
     float *D = (float *)(lds + Lds::D), *E = (float *)(lds + Lds::E);
     double *gd = (double *)(lds + Lds::gd);
     ChunkGates *gt = (ChunkGates *)(lds + Lds::gates);
     float *red = (float *)(lds + Lds::red);        // the waves' sums of dG
+    float *dots = (float *)(lds + Lds::dot);       // z . e over the later columns
     double *rin = (double *)(lds + Lds::rin);      // and of <S', dS'>
     uint32_t *big = (uint32_t *)(lds + Lds::big);  // the waves' largest magnitudes of D and of E
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
+    const int wt = w & 3, half = w >> 2;   // token tile; which columns of 32, which of D and E
     // chunks from the front first: the scan wrote theirs last
     const int hk = (int)(blockIdx.x % a.Hk), b = (int)(blockIdx.x / a.Hk % a.B), n = (int)(blockIdx.x / a.Hk / a.B);
     const int per = ONE ? 1 : a.H / a.Hk, ct16 = col_tiles(a.Dv, 1);
@@ -295,13 +300,11 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
     const long tok0 = (long)b * a.L + n * DC;
     const T *op = (const T *)d.dout;
     T *dqp = (T *)d.dq, *dkp = (T *)d.dk, *dvo = (T *)d.dv;
-    dl_f4 tq[ONE ? 1 : 4][TT], tk[ONE ? 1 : 4][TT];   // sums over the value heads
+    dl_f4 tq[ONE ? 1 : 4], tk[ONE ? 1 : 4];   // sums over the value heads
 #pragma unroll
-    for (int t = 0; t < (ONE ? 1 : 4); ++t)
-#pragma unroll
-        for (int j = 0; j < TT; ++j) tq[t][j] = tk[t][j] = dl_f4{0.f, 0.f, 0.f, 0.f};
-    auto store = [&](int t, int j, dl_f4 x, dl_f4 y) {   // dq and dk of this wave's channel tile j, token tile t
-        const int row = 16 * t + c16, dk = 16 * (w * TT + j) + 4 * g4;
+    for (int t = 0; t < (ONE ? 1 : 4); ++t) tq[t] = tk[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+    auto store = [&](int t, dl_f4 x, dl_f4 y) {   // dq and dk of this wave's channel tile, token tile t
+        const int row = 16 * t + c16, dk = 16 * w + 4 * g4;
         if (row >= room || dk >= a.Dk) return;
         const bool real = row < nt;
 #pragma unroll
@@ -322,30 +325,34 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
     for (int hh = 0; hh < per; ++hh) {
         const int h = hk * per + hh;
         const long ch = ((long)b * a.H + h) * a.N + n;
+        // (offsets into LDS are formed where they are used: kept over the loop they take more registers than there are)
+        int lane = tid & 63;
+        asm volatile("" : "+v"(lane));
+        int g4 = lane >> 4, c16 = lane & 15;
         __syncthreads();   // the last head's matrices are read
         if (nt <= 0) {     // nothing behind a sequence's end has a gradient
-            for (int it = tid; it < room * a.Dv; it += 256) IO<DT>::st(dvo + ((tok0 + it / a.Dv) * a.H + h) * a.Dv, it % a.Dv, 0.f);
+            for (int it = tid; it < room * a.Dv; it += 64 * NW) IO<DT>::st(dvo + ((tok0 + it / a.Dv) * a.H + h) * a.Dv, it % a.Dv, 0.f);
             if (tid < room) d.dg[(tok0 + tid) * a.H + h] = d.dbeta[(tok0 + tid) * a.H + h] = 0.f;
             continue;
         }
         const dl_f4 *Sp = (const dl_f4 *)states + ch * ct16 * 2 * KS * 64, *Ep = (const dl_f4 *)d.dends + ch * ct16 * 2 * KS * 64;
         const dl_f4 *ep = (const dl_f4 *)es + ch * ct16 * 4 * 64, *zp = (const dl_f4 *)d.zs + ch * ct16 * 4 * 64;
-        // 32 columns: states of KS (column tile, row tile)s a wave, e and z of token tile w, do of token tile w
-        dl_f4 xs[KS], xe[KS], x_e[2], x_z[2], xo[2];
+        // 32 columns: states of NS (column tile, row tile)s a wave, e, z and do of token tile wt
+        dl_f4 xs[NS], xe[NS], x_e[NI], x_z[NI], xo[NI];
         auto fetch = [&](int c2) {
 #pragma unroll
-            for (int i = 0; i < KS; ++i) {
-                const int at = i * 4 + w, ct = min(c2 + at / (2 * KS), ct16 - 1);
+            for (int i = 0; i < NS; ++i) {
+                const int at = min(i * NW + w, 4 * KS - 1), ct = min(c2 + at / (2 * KS), ct16 - 1);
                 xs[i] = Sp[(ct * 2 * KS + at % (2 * KS)) * 64 + lane];
                 xe[i] = Ep[(ct * 2 * KS + at % (2 * KS)) * 64 + lane];
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int ct = min(c2 + i, ct16 - 1);
-                x_e[i] = ep[(ct * 4 + w) * 64 + lane];
-                x_z[i] = zp[(ct * 4 + w) * 64 + lane];
-                const int c = 16 * (c2 + i) + 4 * g4;
-                const T *p = op + ((tok0 + min(16 * w + c16, nt - 1)) * a.H + h) * a.Dv + (c < a.Dv ? c : 0);
+            for (int i = 0; i < NI; ++i) {
+                const int ct = min(c2 + half + i, ct16 - 1);
+                x_e[i] = ep[(ct * 4 + wt) * 64 + lane];
+                x_z[i] = zp[(ct * 4 + wt) * 64 + lane];
+                const int c = 16 * (c2 + half + i) + 4 * g4;
+                const T *p = op + ((tok0 + min(16 * wt + c16, nt - 1)) * a.H + h) * a.Dv + (c < a.Dv ? c : 0);
                 if constexpr (DT == F32) {
                     xo[i] = *(const dl_f4 *)p;
                 } else {
@@ -366,21 +373,22 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
             ey = max(ey, g.x); eE = max(eE, g.y); eo = max(eo, DT == F16 ? 0 : g.z);   // fp16 goes in as it is
         }
         const float su = pow2(-eu), sS = pow2(-eS), sy = pow2(-ey), sE = pow2(-eE), sd = pow2(-eo);
-        dl_f4 dq[4][TT], kr[4][TT], kw[4][TT], ad[4], ae[4];
+        dl_f4 dq[4], kr[4], kw[4], ad[NI][4];   // ad: a row tile of D (of E), or of both
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            ad[t] = ae[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
+            dq[t] = kr[t] = kw[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < TT; ++j) dq[t][j] = kr[t][j] = kw[t][j] = dl_f4{0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < NI; ++i) ad[i][t] = dl_f4{0.f, 0.f, 0.f, 0.f};
         }
         float inner[4] = {0.f, 0.f, 0.f, 0.f}, dot[4] = {0.f, 0.f, 0.f, 0.f};   // short sums: <S, dS'> cancels
         __syncthreads();
-        const dl_f4 be = *(const dl_f4 *)(gt->beta + 16 * w + 4 * g4);
+        const dl_f4 be = *(const dl_f4 *)(gt->beta + 16 * wt + 4 * g4);
         for (int c2 = 0; c2 < ct16; c2 += 2) {
             if (c2) __syncthreads();   // the columns before are read
 #pragma unroll
-            for (int i = 0; i < KS; ++i) {
-                const int at = i * 4 + w, ct = at / (2 * KS), t = at % (2 * KS);
+            for (int i = 0; i < NS; ++i) {
+                const bool once = 4 * KS % NW == 0 || i * NW + w < 4 * KS;   // else the last tile again
+                const int at = min(i * NW + w, 4 * KS - 1), ct = at / (2 * KS), t = at % (2 * KS);
                 const bool on = 16 * (c2 + ct) + c16 < a.Dv;
                 const int to = (kq_block<KS, 2>(0, ct, t >> 1) * 64 + kq_place(c16, g4)) * 2 + (t & 1);
                 dl_f4 x, y;
@@ -388,7 +396,7 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
                 for (int r = 0; r < 4; ++r) {
                     x[r] = on ? xs[i][r] : 0.f;
                     y[r] = on ? xe[i][r] : 0.f;
-                    inner[r] += x[r] * y[r];
+                    inner[r] += once ? x[r] * y[r] : 0.f;
                 }
                 uint32_t p[2][2], q[2][2];
                 split2<2>(x[0], sS, x[1], sS, p[0]); split2<2>(x[2], sS, x[3], sS, p[1]);
@@ -400,18 +408,18 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int c = 16 * (c2 + i) + c16;
+            for (int i = 0; i < NI; ++i) {
+                const int c = 16 * (c2 + half + i) + c16;
                 const bool on = c < a.Dv;
-                const int to = (kq_block<2, 2>(0, i, w >> 1) * 64 + kq_place(c16, 2 * (w & 1) + (g4 >> 1))) * 2 + (g4 & 1);
+                const int to = (kq_block<2, 2>(0, half + i, wt >> 1) * 64 + kq_place(c16, 2 * (wt & 1) + (g4 >> 1))) * 2 + (g4 & 1);
                 dl_f4 x, y;
-                T *p = dvo + ((tok0 + 16 * w + 4 * g4) * a.H + h) * a.Dv + c;
+                T *p = dvo + ((tok0 + 16 * wt + 4 * g4) * a.H + h) * a.Dv + c;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     dot[r] += on ? x_z[i][r] * x_e[i][r] : 0.f;
                     x[r] = on ? be[r] * x_z[i][r] : 0.f;
                     y[r] = on ? be[r] * x_e[i][r] : 0.f;
-                    const int row = 16 * w + 4 * g4 + r;
+                    const int row = 16 * wt + 4 * g4 + r;
                     if (on && row < room) IO<DT>::st(p, (long)r * a.H * a.Dv, row < nt ? x[r] : 0.f);
                 }
                 uint32_t f[2][2], q[2][2];
@@ -423,61 +431,44 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
                     ((uint2 *)(lds + Lds::u))[to + m * 4 * 128] = make_uint2(q[0][m], q[1][m]);
                 }
             }
-            {
-                Raw8<DT> v;
-                if constexpr (DT == F32) {
-                    v.a[0] = __builtin_bit_cast(uint4, xo[0]);
-                    v.a[1] = __builtin_bit_cast(uint4, xo[1]);
-                } else {
-                    v.a[0] = make_uint4(__float_as_uint(xo[0][0]), __float_as_uint(xo[0][1]), __float_as_uint(xo[1][0]), __float_as_uint(xo[1][1]));
-                }
-                const bool row = 16 * w + c16 < nt, lo = 16 * c2 + 4 * g4 < a.Dv, hi = 16 * c2 + 16 + 4 * g4 < a.Dv;
-                if constexpr (DT == F32) {
-                    v.a[0] = or_zero(v.a[0], row && lo);
-                    v.a[1] = or_zero(v.a[1], row && hi);
-                } else {
-                    if (!(row && lo)) v.a[0].x = v.a[0].y = 0u;
-                    if (!(row && hi)) v.a[0].z = v.a[0].w = 0u;
-                }
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {   // four columns of a token as the first half of an operand
+                Raw8<DT> v{};
+                v.a[0] = or_zero(__builtin_bit_cast(uint4, xo[i]), 16 * wt + c16 < nt && 16 * (c2 + half + i) + 4 * g4 < a.Dv);
                 const Op<NT> oo = op_of<DT>(v, sd);
 #pragma unroll
-                for (int m = 0; m < NT; ++m) lds[Lds::o + (m * 4 + w) * 64 + lane] = oo.p[m];
+                for (int m = 0; m < NT; ++m)
+                    ((uint2 *)(lds + Lds::o + (m * 4 + wt) * 64 + lane))[half + i] = make_uint2(__builtin_bit_cast(uint4, oo.p[m]).x, __builtin_bit_cast(uint4, oo.p[m]).y);
             }
             if (c2 + 2 < ct16) fetch(c2 + 2);
             __syncthreads();
-            Op<2> so[TT], to[TT];
-#pragma unroll
-            for (int j = 0; j < TT; ++j) {
-                const int ct = min(w * TT + j, 2 * KS - 1);   // a tile too many is not stored
-                so[j] = lds_cols<2, KS, false, 2>(lds + Lds::S, ct, 0, lane);
-                to[j] = lds_cols<2, KS, false, 2>(lds + Lds::dS, ct, 0, lane);
-            }
+            const int ct = min(w, 2 * KS - 1);   // a tile too many is not stored
+            const Op<2> so = lds_cols<2, KS, false, 2>(lds + Lds::S, ct, 0, lane), to = lds_cols<2, KS, false, 2>(lds + Lds::dS, ct, 0, lane);
             Op<NT> ow;
-            const Op<2> yw = lds_cols<2, 2, false, 2>(lds + Lds::y, w, 0, lane);
+            const Op<2> yw = lds_cols<2, 2, false, 2>(lds + Lds::y, wt, 0, lane);
 #pragma unroll
-            for (int m = 0; m < NT; ++m) ow.p[m] = lds[Lds::o + (m * 4 + w) * 64 + lane];
+            for (int m = 0; m < NT; ++m) ow.p[m] = lds[Lds::o + (m * 4 + wt) * 64 + lane];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const Op<2> yo = lds_cols<2, 2, false, 2>(lds + Lds::y, t, 0, lane), uo = lds_cols<2, 2, false, 2>(lds + Lds::u, t, 0, lane);
                 Op<NT> oo;
 #pragma unroll
                 for (int m = 0; m < NT; ++m) oo.p[m] = lds[Lds::o + (m * 4 + t) * 64 + lane];
-                mm_each<2, NT, TT>([&](int j) -> const Op<2> & { return so[j]; }, [&](int) -> const Op<NT> & { return oo; }, [&](int j) -> dl_f4 & { return dq[t][j]; });
-                mm_each<2, 2, 2 * TT>([&](int j) -> const Op<2> & { return j < TT ? so[j % TT] : to[j % TT]; }, [&](int j) -> const Op<2> & { return j < TT ? yo : uo; },
-                                      [&](int j) -> dl_f4 & { return j < TT ? kr[t][j % TT] : kw[t][j % TT]; });
-                if (t <= w) {
-                    ad[t] = mm(ow, uo, ad[t]);
-                    ae[t] = mm(yw, uo, ae[t]);
+                dq[t] = mm(so, oo, dq[t]);
+                mm_each<2, 2, 2>([&](int j) -> const Op<2> & { return j ? to : so; }, [&](int j) -> const Op<2> & { return j ? uo : yo; },
+                                 [&](int j) -> dl_f4 & { return j ? kw[t] : kr[t]; });
+                if (t <= wt) {
+                    if (NW == 4 || half == 0) ad[0][t] = mm(ow, uo, ad[0][t]);
+                    if (NW == 4 || half == 1) ad[NI - 1][t] = mm(yw, uo, ad[NI - 1][t]);
                 }
             }
         }
-        // dbeta of token tile w: the sum over a row's 16 lanes
+        // dbeta of token tile wt: the sum over a row's 16 lanes
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
 #pragma unroll
             for (int m = 1; m < 16; m *= 2) dot[r] += __shfl_xor(dot[r], m);
-            const int row = 16 * w + 4 * g4 + r;
-            if (c16 == 0 && row < room) d.dbeta[(tok0 + row) * a.H + h] = row < nt ? dot[r] : 0.f;
+            if (half == 1 && c16 == 0) dots[16 * wt + 4 * g4 + r] = dot[r];
         }
         double in64 = 0.0;
 #pragma unroll
@@ -487,33 +478,43 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
         {
             const uint4 *in = kq + (((long)b * a.Hk + hk) * a.N + n) * 2 * Lds::kq;
 #pragma unroll
-            for (int i = 0; i < 2 * Lds::kq / 256; ++i) lds[i * 256 + tid] = in[i * 256 + tid];
+            for (int i = 0; i < 2 * Lds::kq / (64 * NW); ++i) lds[i * 64 * NW + tid] = in[i * 64 * NW + tid];
         }
+        if (half == 0 && c16 == 0)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = 16 * wt + 4 * g4 + r;
+                if (row < room) d.dbeta[(tok0 + row) * a.H + h] = row < nt ? dot[r] + (NW == 8 ? dots[row] : 0.f) : 0.f;
+            }
+        asm volatile("" : "+v"(lane));
+        g4 = lane >> 4;
+        c16 = lane & 15;
         const uint4 *ks = lds + Lds::k, *qs = lds + Lds::q;
         const int ek = gt->ek, eq = gt->eq;
-        uint32_t md = 0, me = 0;
+        uint32_t md[NI] = {};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int col = 16 * j + c16;
             const double gj = gd[col];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int i = 16 * w + 4 * g4 + r;
+                const int i = 16 * wt + 4 * g4 + r;
                 float f = 0.f;
                 if (i >= col) f = __builtin_amdgcn_exp2f((float)(gd[i] - gj));
-                const float x = i >= col ? a.scale * __builtin_amdgcn_ldexpf(ad[j][r], eo + eu) * f : 0.f;
-                const float y = i > col ? -__builtin_amdgcn_ldexpf(ae[j][r], ey + eu) * f : 0.f;
-                D[i * AROW + col] = x;
-                E[i * AROW + col] = y;
-                md = umax(md, mag(x));
-                me = umax(me, mag(y));
+#pragma unroll
+                for (int m = 0; m < NI; ++m) {
+                    const bool of_d = NW == 4 ? m == 0 : half == 0;
+                    const float x = __builtin_amdgcn_ldexpf(ad[m][j][r], eu + (of_d ? eo : ey)) * f * (of_d ? a.scale : -1.f);
+                    const float y = i > col || (of_d && i == col) ? x : 0.f;
+                    (of_d ? D : E)[i * AROW + col] = y;
+                    md[m] = umax(md[m], mag(y));
+                }
             }
         }
-        md = group_max<64>(md);
-        me = group_max<64>(me);
-        if (lane == 0) {
-            big[w] = md;
-            big[4 + w] = me;
+#pragma unroll
+        for (int m = 0; m < NI; ++m) {
+            md[m] = group_max<64>(md[m]);
+            if (lane == 0) big[4 * (NW == 4 ? m : half) + wt] = md[m];
         }
         float kx = 0.f;   // sum of k . t (u dS'^T)
         __syncthreads();  // D and E are there
@@ -521,6 +522,7 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
         const int eF = scale_exp(umax(umax(big[4], big[5]), umax(big[6], big[7])));
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
+            __builtin_amdgcn_sched_barrier(0);   // a token tile's operands at a time: the registers
             const int row = 16 * t + c16;
             const float f = gt->from0[row], e = gt->toend[row];
             Op<2> dr[2], er[2], dc[2], ec[2];   // rows and columns `row` of D and E
@@ -543,10 +545,8 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
                 }
             }
             float dG = 0.f;
-#pragma unroll
-            for (int j = 0; j < TT; ++j) {
-                const int ct = w * TT + j;   // this wave's channel tile
-                if (ct >= 2 * KS) break;
+            const int ct = w;   // this wave's channel tile
+            if (ct < 2 * KS) {
                 float kv[4] = {0.f, 0.f, 0.f, 0.f}, qv[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int p = NT - 1; p >= 0; --p) {
@@ -560,10 +560,10 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
                 for (int r = 0; r < 4; ++r) {
                     kv[r] = __builtin_amdgcn_ldexpf(kv[r], ek);
                     qv[r] = __builtin_amdgcn_ldexpf(qv[r], eq);
-                    dq[t][j][r] = __builtin_amdgcn_ldexpf(dq[t][j][r], eS + eo) * (f * a.scale);
-                    kr[t][j][r] = __builtin_amdgcn_ldexpf(kr[t][j][r], eS + ey) * -f;
-                    kw[t][j][r] = __builtin_amdgcn_ldexpf(kw[t][j][r], eE + eu) * e;
-                    kx += kv[r] * kw[t][j][r];
+                    dq[t][r] = __builtin_amdgcn_ldexpf(dq[t][r], eS + eo) * (f * a.scale);
+                    kr[t][r] = __builtin_amdgcn_ldexpf(kr[t][r], eS + ey) * -f;
+                    kw[t][r] = __builtin_amdgcn_ldexpf(kw[t][r], eE + eu) * e;
+                    kx += kv[r] * kw[t][r];
                 }
                 dl_f4 p = {0.f, 0.f, 0.f, 0.f}, q = p, x = p, y = p;
 #pragma unroll
@@ -580,20 +580,20 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
                 }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    dq[t][j][r] += __builtin_amdgcn_ldexpf(p[r], ek + eD);
-                    kr[t][j][r] += __builtin_amdgcn_ldexpf(q[r], ek + eF);
-                    kw[t][j][r] += __builtin_amdgcn_ldexpf(x[r], eq + eD) + __builtin_amdgcn_ldexpf(y[r], ek + eF);
+                    dq[t][r] += __builtin_amdgcn_ldexpf(p[r], ek + eD);
+                    kr[t][r] += __builtin_amdgcn_ldexpf(q[r], ek + eF);
+                    kw[t][r] += __builtin_amdgcn_ldexpf(x[r], eq + eD) + __builtin_amdgcn_ldexpf(y[r], ek + eF);
                 }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    dG += qv[r] * dq[t][j][r] + kv[r] * (kr[t][j][r] - kw[t][j][r]);
-                    kr[t][j][r] += kw[t][j][r];
+                    dG += qv[r] * dq[t][r] + kv[r] * (kr[t][r] - kw[t][r]);
+                    kr[t][r] += kw[t][r];
                 }
                 if constexpr (ONE) {
-                    store(t, j, dq[t][j], kr[t][j]);
+                    store(t, dq[t], kr[t]);
                 } else {
-                    tq[t][j] += dq[t][j];
-                    tk[t][j] += kr[t][j];
+                    tq[t] += dq[t];
+                    tk[t] += kr[t];
                 }
             }
             dG += __shfl_xor(dG, 16);
@@ -607,22 +607,25 @@ __global__ __launch_bounds__(256, 1) void delta_bwd_chunk_kernel(
         __syncthreads();
         if (w == 0) {
             // suffix sums in float64: many terms, of both signs
-            double x = (double)red[lane] + red[DC + lane] + red[2 * DC + lane] + red[3 * DC + lane];
+            double x = 0.0, y = 0.0;
+#pragma unroll
+            for (int i = 0; i < NW; ++i) {
+                x += (double)red[i * DC + lane];
+                y += rin[i];
+            }
 #pragma unroll
             for (int m = 1; m < 64; m *= 2) {
-                const double y = __shfl_down(x, m);
-                if (lane + m < 64) x += y;
+                const double z = __shfl_down(x, m);
+                if (lane + m < 64) x += z;
             }
-            x += (rin[0] + rin[1]) + (rin[2] + rin[3]);
+            x += y;
             if (lane < room) d.dg[(tok0 + lane) * a.H + h] = lane < nt ? (float)x : 0.f;
         }
     }
     if (ONE && nt > 0) return;
     const dl_f4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int j = 0; j < TT; ++j) store(t, j, ONE ? zero : tq[ONE ? 0 : t][j], ONE ? zero : tk[ONE ? 0 : t][j]);
+    for (int t = 0; t < 4; ++t) store(t, ONE ? zero : tq[ONE ? 0 : t], ONE ? zero : tk[ONE ? 0 : t]);
 }
 
 template <int DT, int KS, int NW>
@@ -653,10 +656,10 @@ template <int DT, int KS> hipError_t bwd_of(const DeltaArgs &a, const DeltaBuffe
     const unsigned grid = (unsigned)((long)a.B * a.Hk * a.N);
     if (a.H == a.Hk) {
         if ((e = lds_room(delta_bwd_chunk_kernel<DT, KS, true>, lds2)) != hipSuccess) return e;
-        delta_bwd_chunk_kernel<DT, KS, true><<<grid, 256, lds2, st>>>(a, w.back, w.kq, w.es, w.states, w.exps, d);
+        delta_bwd_chunk_kernel<DT, KS, true><<<grid, 64 * grad_waves<KS>, lds2, st>>>(a, w.back, w.kq, w.es, w.states, w.exps, d);
     } else {
         if ((e = lds_room(delta_bwd_chunk_kernel<DT, KS, false>, lds2)) != hipSuccess) return e;
-        delta_bwd_chunk_kernel<DT, KS, false><<<grid, 256, lds2, st>>>(a, w.back, w.kq, w.es, w.states, w.exps, d);
+        delta_bwd_chunk_kernel<DT, KS, false><<<grid, 64 * grad_waves<KS>, lds2, st>>>(a, w.back, w.kq, w.es, w.states, w.exps, d);
     }
     return hipGetLastError();
 }
