@@ -250,8 +250,6 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
     }
 }
 
-constexpr int AROW = DC + 4;   // floats a row of a 64 x 64 matrix in LDS
-
 template <int KS> constexpr int grad_waves = KS > 2 ? 8 : 4;   // one for each of the key channels' tiles
 
 // LDS of delta_bwd_chunk_kernel, in 16-byte words: first 32 columns at a time of the states, of y and u, and of do,
@@ -259,7 +257,7 @@ template <int KS> constexpr int grad_waves = KS > 2 ? 8 : 4;   // one for each o
 template <int DT, int KS> struct GradLds {
     static constexpr int NT = pieces<DT>(), NW = grad_waves<KS>;
     static constexpr int S = 0, dS = S + 4 * KS * 64, y = dS + 4 * KS * 64, u = y + 8 * 64, o = u + 8 * 64, stage = o + NT * 4 * 64;
-    static constexpr int kq = kq_words<KS>(NT), k = 0, q = kq, D = 2 * kq, E = D + DC * AROW / 4, after = E + DC * AROW / 4;
+    static constexpr int kq = kq_words<KS>(NT), k = 0, q = kq, D = 2 * kq, E = D + kq_words<2>(2), after = E + kq_words<2>(2);
     static constexpr int rest = stage > after ? stage : after;
     static constexpr int gd = rest, gates = gd + DC / 2, red = gates + GATES, dot = red + NW * DC / 4, rin = dot + DC / 4, big = rin + NW / 2,
                          total = (big + 2) * 16;
@@ -284,7 +282,6 @@ __global__ __launch_bounds__(64 * grad_waves<KS>, (KS > 2 || ONE ? 2 : 1)) void 
     typedef GradLds<DT, KS> Lds;
     constexpr int NT = pieces<DT>(), NW = Lds::NW, NS = (4 * KS + NW - 1) / NW, NI = 8 / NW;   // tiles of states, of e and z, a wave
     extern __shared__ uint4 lds[];
-    float *D = (float *)(lds + Lds::D), *E = (float *)(lds + Lds::E);
     double *gd = (double *)(lds + Lds::gd);
     ChunkGates *gt = (ChunkGates *)(lds + Lds::gates);
     float *red = (float *)(lds + Lds::red);        // the waves' sums of dG
@@ -474,74 +471,92 @@ __global__ __launch_bounds__(64 * grad_waves<KS>, (KS > 2 || ONE ? 2 : 1)) void 
 #pragma unroll
         for (int i = 0; i < 4; ++i) in64 += inner[i];
         in64 *= gt->from0[DC - 1];
-        __syncthreads();   // the columns are read: keys, queries, D and E take their place
+        // keys and queries are under way while D and E are formed
+        constexpr int NQ = 2 * Lds::kq / (64 * NW);
+        dl_f4 x_k[NQ];
         {
-            const uint4 *in = kq + (((long)b * a.Hk + hk) * a.N + n) * 2 * Lds::kq;
+            const dl_f4 *in = (const dl_f4 *)kq + (((long)b * a.Hk + hk) * a.N + n) * 2 * Lds::kq;
 #pragma unroll
-            for (int i = 0; i < 2 * Lds::kq / (64 * NW); ++i) lds[i * 64 * NW + tid] = in[i * 64 * NW + tid];
+            for (int i = 0; i < NQ; ++i) x_k[i] = in[i * 64 * NW + tid];
         }
+        asm volatile("" : "+v"(lane));
+        g4 = lane >> 4;
+        c16 = lane & 15;
+#pragma unroll
+        for (int m = 0; m < NI; ++m) {
+            const bool of_d = NW == 4 ? m == 0 : half == 0;
+            const float f = of_d ? a.scale : -1.f;
+            const int e = eu + (of_d ? eo : ey);
+            uint32_t md = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int col = 16 * j + c16;
+                const double gj = gd[col];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 16 * wt + 4 * g4 + r;
+                    const float x = __builtin_amdgcn_ldexpf(ad[m][j][r], e) * f * __builtin_amdgcn_exp2f((float)(gd[i] - gj));
+                    ad[m][j][r] = i > col || (of_d && i == col) ? x : 0.f;
+                    md = umax(md, mag(ad[m][j][r]));
+                }
+            }
+            md = group_max<64>(md);
+            if (lane == 0) big[4 * (NW == 4 ? m : half) + wt] = md;
+        }
+        __syncthreads();   // the columns are read: keys, queries, D and E take their place
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) ((dl_f4 *)lds)[i * 64 * NW + tid] = x_k[i];
         if (half == 0 && c16 == 0)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int row = 16 * wt + 4 * g4 + r;
                 if (row < room) d.dbeta[(tok0 + row) * a.H + h] = row < nt ? dot[r] + (NW == 8 ? dots[row] : 0.f) : 0.f;
             }
-        asm volatile("" : "+v"(lane));
-        g4 = lane >> 4;
-        c16 = lane & 15;
-        const uint4 *ks = lds + Lds::k, *qs = lds + Lds::q;
+        const uint4 *ks = lds + Lds::k, *qs = lds + Lds::q, *Ds = lds + Lds::D, *Es = lds + Lds::E;
         const int ek = gt->ek, eq = gt->eq;
-        uint32_t md[NI] = {};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int col = 16 * j + c16;
-            const double gj = gd[col];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * wt + 4 * g4 + r;
-                float f = 0.f;
-                if (i >= col) f = __builtin_amdgcn_exp2f((float)(gd[i] - gj));
-#pragma unroll
-                for (int m = 0; m < NI; ++m) {
-                    const bool of_d = NW == 4 ? m == 0 : half == 0;
-                    const float x = __builtin_amdgcn_ldexpf(ad[m][j][r], eu + (of_d ? eo : ey)) * f * (of_d ? a.scale : -1.f);
-                    const float y = i > col || (of_d && i == col) ? x : 0.f;
-                    (of_d ? D : E)[i * AROW + col] = y;
-                    md[m] = umax(md[m], mag(y));
-                }
-            }
-        }
+        const int eD = scale_exp(umax(umax(big[0], big[1]), umax(big[2], big[3])));
+        const int eF = scale_exp(umax(umax(big[4], big[5]), umax(big[6], big[7])));
 #pragma unroll
         for (int m = 0; m < NI; ++m) {
-            md[m] = group_max<64>(md[m]);
-            if (lane == 0) big[4 * (NW == 4 ? m : half) + wt] = md[m];
+            const bool of_d = NW == 4 ? m == 0 : half == 0;
+            const float f = pow2(-(of_d ? eD : eF));
+            uint2 *to = (uint2 *)(lds + (of_d ? Lds::D : Lds::E)) + (kq_block<2>(0, 0, wt >> 1) * 64 + kq_place(c16, 2 * (wt & 1) + (g4 >> 1))) * 2 + (g4 & 1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t x[2][2];
+                split2<2>(ad[m][j][0], f, ad[m][j][1], f, x[0]);
+                split2<2>(ad[m][j][2], f, ad[m][j][3], f, x[1]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) to[kq_block<2>(i, j, 0) * 128] = make_uint2(x[0][i], x[1][i]);
+            }
         }
         float kx = 0.f;   // sum of k . t (u dS'^T)
         __syncthreads();  // D and E are there
-        const int eD = scale_exp(umax(umax(big[0], big[1]), umax(big[2], big[3])));
-        const int eF = scale_exp(umax(umax(big[4], big[5]), umax(big[6], big[7])));
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             __builtin_amdgcn_sched_barrier(0);   // a token tile's operands at a time: the registers
             const int row = 16 * t + c16;
             const float f = gt->from0[row], e = gt->toend[row];
             Op<2> dr[2], er[2], dc[2], ec[2];   // rows and columns `row` of D and E
+            const int at = (kq_place(c16, g4 >> 1) * 2 + (g4 & 1)), at2 = kq_place(c16, 2 + (g4 >> 1)) * 2 + (g4 & 1);
+            auto column = [&](const uint4 *M, int s) {
+                Op<2> x;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint2 *p = (const uint2 *)(M + kq_block<2>(i, t, s) * 64), lo = p[at], hi = p[at2];
+                    x.p[i] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+                }
+                return x;
+            };
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                const int o = 32 * s + 4 * g4;
                 if (s <= t / 2) {
-                    dr[s] = split8<2>(*(const dl_f4 *)(D + row * AROW + o), *(const dl_f4 *)(D + row * AROW + o + 16), pow2(-eD));
-                    er[s] = split8<2>(*(const dl_f4 *)(E + row * AROW + o), *(const dl_f4 *)(E + row * AROW + o + 16), pow2(-eF));
+                    dr[s] = lds_cols<2, 2, false>(Ds, t, s, lane);
+                    er[s] = lds_cols<2, 2, false>(Es, t, s, lane);
                 }
                 if (s >= t / 2) {
-                    float x[8], y[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        x[i] = D[(o + (i & 3) + 16 * (i >> 2)) * AROW + row];
-                        y[i] = E[(o + (i & 3) + 16 * (i >> 2)) * AROW + row];
-                    }
-                    dc[s] = split8<2>(x, pow2(-eD));
-                    ec[s] = split8<2>(y, pow2(-eF));
+                    dc[s] = column(Ds, s);
+                    ec[s] = column(Es, s);
                 }
             }
             float dG = 0.f;
