@@ -28,7 +28,9 @@ typedef __attribute__((address_space(3))) void dl_lds_void;
 
 // pieces of the inputs by type
 template <int DT> constexpr int pieces() { return DT == F32 ? 2 : 1; }
-// pieces of what only a 16-bit output is made of: bf16 has 8 bits
+// Pieces of what only a 16-bit output is made of (P, u and the state where they meet queries): a bf16
+// output is rounded to 2^-8 at the end, so one piece of 2^-11 for each factor is an eighth of that, of each
+// term; fp16's 2^-11 needs two.  Nothing of it enters the state.
 template <int DT> constexpr int out_pieces() { return DT == BF16 ? 1 : 2; }
 
 // an operand of eight values a lane in N pieces

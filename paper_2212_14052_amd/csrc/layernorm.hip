@@ -16,7 +16,12 @@
 // sums of dw and db in registers, too; each
 // workgroup writes one float32 partial row of each to the workspace and a
 // second kernel sums those in a fixed order, so results do not depend on timing.
-// Rows too wide for the registers are read again for each sum.
+// Rows too wide for the registers are read again for each sum.  Outputs are streamed
+// past the caches (8192 x 2560 bf16: 17.7 us with ordinary stores, 16.7 so).
+//
+// Forward at 8192 x 2560 bf16: 16.9 us, 4.97 TB/s, what a large copy reaches (4.99).
+// At 16384 x 768 fp16: forward 8.4 us (6.0 TB/s: part of it stays in the last cache),
+// backward 19.8, the second kernel 6.2.
 #include <type_traits>
 
 #include "common.h"
@@ -357,14 +362,17 @@ __global__ __launch_bounds__(1024) void layernorm_reduce_kernel(const float *__r
 
 // How a row is laid over threads: 16-byte vectors where every row starts on 16
 // bytes; a wave where `most` vectors a lane hold the row (no barrier in its sums), else 256
-// threads, else 1024; tpr 0 where those do not hold it.
+// threads, else 1024; tpr 0 where those do not hold it.  With up to eight vectors a lane a
+// wave also takes rows of 2560 16-bit values, with too few rows under way: 19.6 us instead of
+// 16.9 at 8192 x 2560; with one the rows of 768 go to workgroups and their barriers: 66.7 us
+// instead of 34.0 at 16384 x 768, forward and backward.
 struct Shape {
     int vec, nv, tpr;
 };
-Shape shape_of(int d, int dtype, bool aligned, int most) {
+Shape shape_of(int d, int dtype, bool aligned) {
     const int full = dtype == F32 ? 4 : 8;
     Shape s{aligned && d % full == 0 ? full : 1, 0, 0};
-    if (s.vec == 1) most = 8;
+    const int most = s.vec == 1 ? 8 : 4;
     for (int tpr : {64, 256, 1024}) {
         const int nv = (d + tpr * s.vec - 1) / (tpr * s.vec);
         if (nv <= most) {
@@ -376,7 +384,11 @@ Shape shape_of(int d, int dtype, bool aligned, int most) {
     return s;
 }
 
-// workgroups that walk over the rows
+// Workgroups that walk over the rows: fewer leave the card empty, more read the weights (and
+// write partial sums) once more each.  8192 x 2560 bf16 forward: 23.5 us with a quarter of
+// them, 19.1 with four times as many, 16.9 so; forward and backward of 16384 x 768 fp16 with 512
+// and 256 (of 2048 and 512): 37.7, with 8192 and 1024: 40.6, so 34.0; of 4999 x 1031 float32
+// 42.3, 35.2 and 31.5.
 int fwd_groups(int rows, int tpr) {
     const int rpb = threads_of(tpr) / tpr, most = tpr == 1024 ? 512 : 2048, want = (rows + rpb - 1) / rpb;
     return want < most ? want : most;
@@ -388,7 +400,7 @@ int bwd_groups(int rows, int tpr) {
     return want < most ? want : most;
 }
 
-template <int DT, int VEC, int MOST, typename F> hipError_t by_shape(const Shape &s, F f) {
+template <int DT, int VEC, typename F> hipError_t by_shape(const Shape &s, F f) {
     auto nv = [&](auto tpr) {
         switch (s.nv) {
             case 1: return f(std::integral_constant<int, 1>(), tpr);
@@ -396,10 +408,9 @@ template <int DT, int VEC, int MOST, typename F> hipError_t by_shape(const Shape
             case 3: return f(std::integral_constant<int, 3>(), tpr);
             case 4: return f(std::integral_constant<int, 4>(), tpr);
         }
-        if constexpr (VEC == 1 || MOST > 4) {
+        if constexpr (VEC == 1) {
             if (s.nv == 5) return f(std::integral_constant<int, 5>(), tpr);
-            if constexpr (VEC > 1) return f(std::integral_constant<int, 6>(), tpr);
-            else return s.nv == 6 ? f(std::integral_constant<int, 6>(), tpr) : f(std::integral_constant<int, 8>(), tpr);
+            return s.nv == 6 ? f(std::integral_constant<int, 6>(), tpr) : f(std::integral_constant<int, 8>(), tpr);
         }
         return hipErrorInvalidValue;
     };
@@ -408,14 +419,13 @@ template <int DT, int VEC, int MOST, typename F> hipError_t by_shape(const Shape
     return nv(std::integral_constant<int, 1024>());
 }
 
-constexpr int kMostFwd = 4, kMostBwd = 4;   // vectors of 16 bytes a lane
 constexpr int kWideRows = 1 << 21;          // rows a launch with a workgroup of 1024 for each (under 2^32 threads)
 
 template <int DT, int VEC>
 hipError_t ln_fwd(const Shape &s, const void *x, const float *w, const float *b, int rows, int d, float eps, void *y,
                   float *mean, float *rstd, hipStream_t st) {
     typedef typename IO<DT>::T T;
-    return by_shape<DT, VEC, kMostFwd>(s, [&](auto nv, auto tpr) {
+    return by_shape<DT, VEC>(s, [&](auto nv, auto tpr) {
         constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value;
         layernorm_kernel<DT, VEC, NV, TPR><<<(unsigned)fwd_groups(rows, TPR), threads_of(TPR), 0, st>>>(
             (const T *)x, w, b, rows, d, eps, (T *)y, mean, rstd);
@@ -427,7 +437,7 @@ template <int DT, int VEC>
 hipError_t ln_bwd(const Shape &s, const void *dy, const void *x, const float *w, const float *mean, const float *rstd,
                   int rows, int d, void *dx, float *part, int G, hipStream_t st) {
     typedef typename IO<DT>::T T;
-    return by_shape<DT, VEC, kMostBwd>(s, [&](auto nv, auto tpr) {
+    return by_shape<DT, VEC>(s, [&](auto nv, auto tpr) {
         constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value;
         layernorm_bwd_kernel<DT, VEC, NV, TPR><<<(unsigned)G, threads_of(TPR), 0, st>>>(
             (const T *)dy, (const T *)x, w, mean, rstd, rows, d, (T *)dx, part);
@@ -439,7 +449,7 @@ template <int DT>
 hipError_t fwd_of(const void *x, const float *w, const float *b, int rows, int d, float eps, void *y, float *mean,
                   float *rstd, hipStream_t st) {
     typedef typename IO<DT>::T T;
-    const Shape s = shape_of(d, DT, (((uintptr_t)x | (uintptr_t)y) & 15) == 0, kMostFwd);
+    const Shape s = shape_of(d, DT, (((uintptr_t)x | (uintptr_t)y) & 15) == 0);
     if (s.tpr == 0) {
         for (int r = 0; r < rows; r += kWideRows) {
             const int n = rows - r < kWideRows ? rows - r : kWideRows;
@@ -457,7 +467,7 @@ template <int DT>
 hipError_t bwd_of(const void *dy, const void *x, const float *w, const float *mean, const float *rstd, int rows, int d,
                   void *dx, float *dw, float *db, float *part, hipStream_t st) {
     typedef typename IO<DT>::T T;
-    const Shape s = shape_of(d, DT, (((uintptr_t)x | (uintptr_t)dy | (uintptr_t)dx) & 15) == 0, kMostBwd);
+    const Shape s = shape_of(d, DT, (((uintptr_t)x | (uintptr_t)dy | (uintptr_t)dx) & 15) == 0);
     if (!dw && !db) part = nullptr;
     int G = bwd_groups(rows, s.tpr);
     hipError_t e = hipSuccess;

@@ -5,9 +5,8 @@ Tolerances.  Keys of unit length, beta in (0, 1) and decays at most 1: neither t
 recurrence nor its reverse stretches an error, so the chunks' errors add up.  Every
 gradient is a sum of products of a state S, a state's gradient dS, an error e or
 an output's gradient, so what a chunk rounds away is bounded by C times the product of the
-largest norms of its two factors: C = 2^-15 where two bf16 pieces take part (the
-forward pass's X, for 16-bit inputs), 2^-20 in float32 (sums of up to 128 + 64 terms, 2^-24
-each, at a sixteenth by their signs).  16-bit results are rounded once more: half a step."""
+largest norms of its two factors: C = 2^-20 in float32 (operands in two fp16 pieces, 2^-22; sums of
+up to 128 + 64 terms, 2^-24 each, at a sixteenth by their signs), 2^-15 for 16-bit inputs.  16-bit results are rounded once more: half a step."""
 import pytest
 import torch
 
@@ -73,7 +72,7 @@ def run_and_check(dtype, q, k, v, g, beta, S0, do, dS, scale=None, lengths=None)
         half = torch.finfo(x.dtype).eps / 2 if x.dtype != torch.float32 else 0.0
         far = (x.double() - ref).abs()
         assert (far <= half * ref.abs() + C * bound + (2.0 ** -25 if x.dtype == torch.float16 else 0.0)).all(), (name, far.max().item(), C * bound)
-        # In the 2-norm the pieces' roundings average out over their signs: a sixteenth of C for two pieces.  It cannot be under
+        # In the 2-norm the roundings average out over their signs: a sixteenth of C.  It cannot be under
         # eight float32 roundings of 2^-24 (half of C in float32): with a single token dk = dS u - S dv already rounds exp(g) S,
         # S^T k, e, u, dS's two terms, dv and the difference once each.  dg is a difference of sums: half of C.
         near = max(C / (2 if name == "dg" else 16), 2.0 ** -21 * -(-v.shape[1] // 64))

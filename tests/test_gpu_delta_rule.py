@@ -4,9 +4,12 @@ Tolerances.  Keys of unit length, beta in (0, 1) and decays at most 1 make each
 token's map of the state a contraction: what a chunk of 64 rounds away adds up
 over the chunks at most.  With M the largest state column's length plus the
 largest error e, a chunk's float32 sums are off by (Dk + 64) 2^-24 M.  Matrices
-and vectors of 16-bit inputs enter the solved product X (beta R) and the
-output's P u in two bf16 pieces each (2^-15 of the terms' sizes at most), float32
-inputs in three (2^-22): the terms' sizes are the row sums of |X| and |P|."""
+and vectors enter the products in two fp16 pieces each (2^-22 of the terms' sizes, which are
+the row sums of |X| and |P|); 16-bit inputs are allowed 2^-15.  That covers what makes a bf16
+output alone, P, u and the state in one piece (2^-11 a factor): the at least 8 and mostly 64 to
+192 terms of an output round independently, each with a root mean square of 2^-11 / sqrt(3) / 2 of its
+own size, and their sum's length, 2^-12.8 over the root of the number of terms, is at most 2^-14.3 (8) to
+2^-16.6 (192) of the columns', against 2^-15 (1 + the sum of |P|) of the longest column and 2^-8 of the output."""
 import pytest
 import torch
 
