@@ -296,16 +296,19 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
 // E for the wave, that of the last chunk's keys times errors, so that a chunk is
 // added in the same instruction that decays them.
 //
-// Sequences may be cut into segments (see DeltaSegments).  With MAPS a workgroup
+// Sequences may be cut into segments (see DeltaSegments).  In mode MAP a workgroup
 // does not produce outputs but its segment's map from state to state.
-template <int DT, int KS, int NW, bool MAPS>
-__global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_kernel(DeltaArgs a, DeltaSegments sg, const uint4 *__restrict__ rec,
+enum ScanMode { OUT, OUT_SAVE, MAP };   // outputs; outputs and what the backward pass reads; a segment's map
+
+template <int DT, int KS, int NW, ScanMode MODE>
+__global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_scan_kernel(DeltaArgs a, DeltaSegments sg, const uint4 *__restrict__ rec,
                                                                const uint4 *__restrict__ kq,
                                                                typename IO<DT>::T *__restrict__ o, float *S_final,
                                                                float *__restrict__ es, float *__restrict__ states,
                                                                int2 *__restrict__ exps) {
     typedef typename IO<DT>::T T;
     constexpr int NT = pieces<DT>(), NX = 2, NO = out_pieces<DT>();
+    constexpr bool MAPS = MODE == MAP, SAVE = MODE == OUT_SAVE;
     typedef ChunkCopy<DT, KS, NW, NX + NO, MAPS> Copy;
     typedef typename Copy::Lds Lds;
     extern __shared__ uint4 lds[];
@@ -341,16 +344,7 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
         const uint4 *ks = at + Lds::k, *qs = at + Lds::q, *xs = at + Lds::rec, *ps = xs + NX * MAT;
         const T *vs = (const T *)(at + Lds::v);
         const ChunkGates *gt = (const ChunkGates *)(at + Lds::gates);
-        if (!MAPS && states) {
-            dl_f4 *p = (dl_f4 *)states + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;
-#pragma unroll
-            for (int t = 0; t < 2 * KS; ++t) {
-                dl_f4 y;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) y[r] = __builtin_amdgcn_ldexpf(S[t][r], E);
-                p[t * 64] = y;
-            }
-        }
+        dl_f4 *kept = (dl_f4 *)states + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;   // where this state is left
         const int ek = __builtin_amdgcn_readfirstlane(gt->ek), eq = __builtin_amdgcn_readfirstlane(gt->eq),
                   ex = __builtin_amdgcn_readfirstlane(gt->ex), ep = __builtin_amdgcn_readfirstlane(gt->ep),
                   et = __builtin_amdgcn_readfirstlane(gt->et);
@@ -430,10 +424,10 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
                 }
         }
         const int eu = max(wave_exp(u), kLeast);
-        if (!MAPS && es) {
+        if constexpr (SAVE) {
             dl_f4 *p = (dl_f4 *)es + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 4 * 64 + lane;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) p[t * 64] = R[t];
+            for (int t = 0; t < 4; ++t) store_stream(p + t * 64, __builtin_bit_cast(uint4, R[t]));
             if (lane == 0) exps[ch * kDeltaTiles + c0 / 16] = make_int2(eu, max(min(eS, 114), -126));
         }
         constexpr int TG = KS % 2 == 0 ? 4 : 2;   // state tiles at a time
@@ -491,6 +485,7 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
         // of 2^-60 of S where the errors are smaller than that
         const int En = max(ek + eu + et, max(eS - 60, E - 100)), ew = En - ek;
         const float fs = fl * pow2(max(E - En, -126)), sw = pow2(max(min(-ew, 127), -126));
+        const int Eo = E;
         E = En;
         Op<2> wo[2];
 #pragma unroll
@@ -521,6 +516,15 @@ __global__ __launch_bounds__(64 * NW, MAPS ? NW / 2 : NW / 4) void delta_scan_ke
                 mm_each<NT, 2, TG>([&](int m) -> const Op<NT> & { return kc[q & 1][m][s]; }, [&](int) -> const Op<2> & { return wo[s]; },
                                         [&](int m) -> dl_f4 & { return y[q & 1][m]; });
             if (q > 0) add(q - 1);
+            if constexpr (SAVE) {
+#pragma unroll
+                for (int t = q * TG; t < q * TG + TG; ++t) {
+                    dl_f4 y;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) y[r] = __builtin_amdgcn_ldexpf(S[t][r], Eo);
+                    store_stream(kept + t * 64, __builtin_bit_cast(uint4, y));
+                }
+            }
             in_order<NW == 4>();
         }
         add(2 * KS / TG - 1);
@@ -666,13 +670,13 @@ DeltaCut delta_cut(int B, int H, int N, int Dk, int Dv, int dtype) {
 
 namespace {
 
-template <int DT, int KS, int NW>
+template <int DT, int KS, int NW, ScanMode MODE>
 hipError_t scan_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_final, hipStream_t st) {
     typedef typename IO<DT>::T T;
     constexpr int lds = ScanLds<DT, KS, NW, 2 + out_pieces<DT>()>::total;
-    const hipError_t e = lds_room(delta_scan_kernel<DT, KS, NW, false>, lds);
+    const hipError_t e = lds_room(delta_scan_kernel<DT, KS, NW, MODE>, lds);
     if (e != hipSuccess) return e;
-    delta_scan_kernel<DT, KS, NW, false><<<(unsigned)((long)a.B * a.H * w.seg.G * col_tiles(a.Dv, NW)), 64 * NW, lds, st>>>(
+    delta_scan_kernel<DT, KS, NW, MODE><<<(unsigned)((long)a.B * a.H * w.seg.G * col_tiles(a.Dv, NW)), 64 * NW, lds, st>>>(
         a, w.seg, w.rec, w.kq, (T *)o, S_final, w.es, w.states, w.exps);
     return hipGetLastError();
 }
@@ -686,14 +690,14 @@ hipError_t fwd_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_f
     const DeltaSegments sg = w.seg;
     if (sg.G > 1) {
         constexpr int NW = 8, lds = ScanLds<DT, KS, NW, 2 + out_pieces<DT>(), true>::total;
-        if ((e = lds_room(delta_scan_kernel<DT, KS, NW, true>, lds)) != hipSuccess) return e;
-        delta_scan_kernel<DT, KS, NW, true><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW) + col_tiles(a.Dk, NW))), 64 * NW, lds, st>>>(
+        if ((e = lds_room(delta_scan_kernel<DT, KS, NW, MAP>, lds)) != hipSuccess) return e;
+        delta_scan_kernel<DT, KS, NW, MAP><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW) + col_tiles(a.Dk, NW))), 64 * NW, lds, st>>>(
             a, sg, w.rec, w.kq, nullptr, nullptr, nullptr, nullptr, nullptr);
         if ((e = launch_delta_join(a, sg, a.S0, false, st)) != hipSuccess) return e;
     }
     if constexpr (DT != F32)
-        if (sg.NW == 8) return scan_of<DT, KS, 8>(a, w, o, S_final, st);
-    return scan_of<DT, KS, 4>(a, w, o, S_final, st);
+        if (sg.NW == 8) return w.es ? scan_of<DT, KS, 8, OUT_SAVE>(a, w, o, S_final, st) : scan_of<DT, KS, 8, OUT>(a, w, o, S_final, st);
+    return w.es ? scan_of<DT, KS, 4, OUT_SAVE>(a, w, o, S_final, st) : scan_of<DT, KS, 4, OUT>(a, w, o, S_final, st);
 }
 
 template <int DT> hipError_t fwd_by(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_final, hipStream_t st) {

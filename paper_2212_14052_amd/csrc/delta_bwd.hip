@@ -59,16 +59,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
         const T *vs = (const T *)(at + Lds::v);
         const ChunkGates *gt = (const ChunkGates *)(at + Lds::gates);
         const int nt = min(DC, len - n * DC);
-        if constexpr (!MAPS) {
-            dl_f4 *p = (dl_f4 *)d.dends + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;
-#pragma unroll
-            for (int t = 0; t < 2 * KS; ++t) {
-                dl_f4 y;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) y[r] = __builtin_amdgcn_ldexpf(S[t][r], E);
-                p[t * 64] = y;
-            }
-        }
+        dl_f4 *kept = (dl_f4 *)d.dends + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;   // where this state is left
         const int ek = __builtin_amdgcn_readfirstlane(gt->ek), eq = __builtin_amdgcn_readfirstlane(gt->eq),
                   ex = __builtin_amdgcn_readfirstlane(gt->ex), ep = __builtin_amdgcn_readfirstlane(gt->ep),
                   ef = __builtin_amdgcn_readfirstlane(gt->ef);
@@ -172,7 +163,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
                 dl_f4 z;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) z[r] = u[t][r] - px * x[t][r];
-                if (!MAPS) p[t * 64] = z;
+                if (!MAPS) store_stream(p + t * 64, __builtin_bit_cast(uint4, z));
 #pragma unroll
                 for (int r = 0; r < 4; ++r) y[t][r] = be[t][r] * z[r];
             }
@@ -184,6 +175,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
         // 2^-60 of dS' where both are smaller than that
         const int En = max(max(ek + ez + ef, eq + ed + ef + esc + 1), max(eS - 60, E - 100));
         const float fs = fl * pow2(max(E - En, -126)), sy = pow2(max(min(ek - En, 127), -126)), so_ = pow2(max(min(eq - En, 127), -126));
+        const int Eo = E;
         E = En;
         Op<2> yo[2], qo[2];
         dl_f4 fy[4];
@@ -227,6 +219,15 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
                                        [&](int m) -> dl_f4 & { return x[q & 1][m]; });
             }
             if (q > 0) add(q - 1);
+            if constexpr (!MAPS) {
+#pragma unroll
+                for (int t = q * 2; t < q * 2 + 2; ++t) {
+                    dl_f4 y;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) y[r] = __builtin_amdgcn_ldexpf(S[t][r], Eo);
+                    store_stream(kept + t * 64, __builtin_bit_cast(uint4, y));
+                }
+            }
             in_order<NW == 4>();
         }
         add(KS - 1);
