@@ -6,8 +6,8 @@
 //     du = P^T do + t (K dS'),   z = du - (diag(beta) X)^T du,   y = beta z = dv,
 //     dS = exp(G_63) dS' + Q^T (f do) - K^T (f y)
 // is again a scan whose columns do not meet, in the order from the end
-// (delta_bwd_scan_kernel, bound by the same chain inside a chunk as the forward pass's: 182 us for 4 x 2048
-// tokens of 20 heads of 128 bf16); it leaves z and dS' of every chunk.  Then every chunk for itself
+// (delta_bwd_scan_kernel, bound by the same chain inside a chunk as the forward pass's: 142 us for 4 x 2048
+// tokens of 20 heads of 128 bf16; 186 with dS' stored at a chunk's start); it leaves z and dS' of every chunk.  Then every chunk for itself
 // (delta_bwd_chunk_kernel), with
 //     D = lower part of (do u^T) exp(G_i - G_j),  E = -(strictly lower part of (y u^T) exp(G_i - G_j)):
 //     dq = f (do S^T) + D K,   dk = reads + writes,  reads = E K - f (y S^T),
