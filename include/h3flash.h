@@ -334,7 +334,9 @@ int h3_delta_step(const void *q, const void *k, const void *v, const float *g, c
  *   Dk, Dv, Hk as for h3_delta_step; any L >= 1.  Other than S_final and S0
  *   nothing that is written overlaps anything.
  * States, gates and sums are float32, differences of summed log decays
- * float64; a NaN or Inf may reach every token of its chunk of 64.
+ * float64; a NaN or Inf may reach every token of its chunk of 64.  Where no token
+ * stretches the state (g <= 0, 0 <= beta |k|^2 <= 2) a chunk is off by a few 2^-22 of the state's size;
+ * where tokens do, a chunk's solved matrix grows with what its 64 tokens stretch, and its errors with it.
  * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, 2^31 chunks, H Dv > 2^22), EWORKSPACE, EDEVICE.
  */
 int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, const float *beta, const float *S0,

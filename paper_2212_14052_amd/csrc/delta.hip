@@ -298,8 +298,8 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
 //
 // What the backward pass reads is stored between the last products, and past the caches: a CU takes
 // 1 KB of stores or copies every 16 cycles, and a wave waits where it asks for many at once, as for
-// the state at a chunk's start, behind the next chunk's copies (4 x 2048 tokens of 20 heads of
-// 128 bf16: 182 us so, 171 past the caches, 160 as it is; 115 with nothing kept).
+// the state at a chunk's start, behind the next chunk's copies (both kernels for 4 x 2048
+// tokens of 20 heads of 128 bf16: 244 us so, 234 past the caches, 204 as it is; 166 with nothing kept).
 //
 // Sequences may be cut into segments (see DeltaSegments).  In mode MAP a workgroup
 // does not produce outputs but its segment's map from state to state.

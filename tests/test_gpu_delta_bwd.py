@@ -11,7 +11,7 @@ import pytest
 import torch
 
 import paper_2212_14052_amd as h3
-from tests.test_gpu_delta_rule import DTYPES, inputs
+from tests.test_gpu_delta_rule import DTYPES, MANY, inputs
 
 pytestmark = pytest.mark.gpu
 NAMES = ("dq", "dk", "dv", "dg", "dbeta", "dS0")
@@ -123,6 +123,13 @@ def test_few_heads_long(B, L, H, Hk, Dk, Dv, dtype):
     run_and_check(dtype, *args)
     for n in (0, 60, L // 2):
         run_and_check(dtype, *args, None, torch.tensor([n, L][:B], device="cuda", dtype=torch.int32))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,L,H,Hk,Dk,Dv", MANY)
+def test_many_heads(B, L, H, Hk, Dk, Dv, dtype):
+    """Heads that fill the card: workgroups of eight waves for 16-bit inputs, some without columns."""
+    run_and_check(dtype, *full_inputs(B, L, H, Hk, Dk, Dv, dtype, 11))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

@@ -173,6 +173,23 @@ def test_few_heads_long(B, L, H, Hk, Dk, Dv, dtype):
         run_and_check(dtype, *args, S0, None, lengths)
 
 
+MANY = [(16, 70, 16, 8, 72, 72), (8, 130, 16, 16, 24, 200), (16, 65, 16, 16, 128, 128)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,L,H,Hk,Dk,Dv", MANY)
+def test_many_heads(B, L, H, Hk, Dk, Dv, dtype):
+    """Heads that fill the card: workgroups of eight waves for 16-bit inputs, some without columns."""
+    run_and_check(dtype, *inputs(B, L, H, Hk, Dk, Dv, dtype, 11))
+
+
+def test_lengths_beyond_32_bits():
+    q, k, v, g, beta, S0 = inputs(2, 70, 2, 2, 32, 32, "f16", 12)
+    want = h3.delta_rule(q, k, v, g, beta, S0=S0)
+    got = h3.delta_rule(q, k, v, g, beta, S0=S0, lengths=torch.tensor([2 ** 32 + 3, 2 ** 40], device="cuda"))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_final_state_over_the_first_one():
     """The C entry point's S_final may be S0's buffer, also where segments read and write it."""
     q, k, v, g, beta, S0 = inputs(1, 2600, 2, 2, 64, 64, "bf16", 10)
