@@ -57,6 +57,17 @@ __device__ __forceinline__ void store_stream(void *p, uint4 v) {
     __builtin_nontemporal_store(__builtin_bit_cast(u4, v), (u4 *)p);
 }
 
+// 64 lanes of 16 bytes from memory to LDS past the registers: lane i from base + off
+// to the LDS address `to` + 16 i (`to` and `base` the same in every lane).  The hardware wants one wait state
+// between the write of m0 and the load that takes its LDS address from it, which the
+// compiler does not put into inline code; without it the load may use the copy before's address.
+__device__ __forceinline__ void copy_to_lds(const void *base, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2"
+                 :
+                 : "v"(off), "s"(to), "s"(base)
+                 : "memory", "m0");
+}
+
 // Exponent e with m = f 2^e, f in [1/2, 1) (frexp); 0 for 0, NaN and inf, so
 // that such rows pass through unscaled.
 __device__ __forceinline__ int pow2_exp(float m) {

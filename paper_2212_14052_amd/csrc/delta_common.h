@@ -354,12 +354,8 @@ template <int DT, int KS, int NW, int MP, bool LEAN = false> struct ChunkCopy {
     int cols, len;           // columns from there, tokens
     uint32_t lds;
 
-    // 64 lanes of 16 bytes, lane i from base + off to the LDS address `to` + 16 i
     static __device__ __forceinline__ void copy(const void *base, uint32_t off, uint32_t to) {
-        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, %2"
-                     :
-                     : "v"(off), "s"(__builtin_amdgcn_readfirstlane(to)), "s"(base)
-                     : "memory", "m0");
+        copy_to_lds(base, off, __builtin_amdgcn_readfirstlane(to));
     }
     // n words from base to word `at` of the buffer
     template <int N> static __device__ __forceinline__ void copy_words(const uint4 *base, uint32_t to, int w, int lane) {

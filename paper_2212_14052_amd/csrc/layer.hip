@@ -288,10 +288,7 @@ __global__ __launch_bounds__(GW_T) __attribute__((amdgpu_waves_per_eu(NS == 3 ? 
             const int q = wvu + 8 * sl;
             const bool real = q < S::SLICES;
             const uint32_t la = real ? st + (uint32_t)q * 1024 : lds0 + (uint32_t)(NS * S::STAGE_B);
-            asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, %2"
-                         :
-                         : "v"(soff[sl] + ks * step[sl]), "s"(la), "s"(src[sl])
-                         : "memory", "m0");
+            copy_to_lds(src[sl], soff[sl] + ks * step[sl], la);
         }
     };
     f32x16_t acc[S::TI][2];

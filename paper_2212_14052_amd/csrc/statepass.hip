@@ -253,10 +253,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void c
             const bool real = q < slices;
             const uint32_t vo = 2u * (uint32_t)src_elem(real ? q : w);
             const uint32_t la = __builtin_amdgcn_readfirstlane(real ? st + (uint32_t)q * 1024 : dummy);
-            asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, %2"
-                         :
-                         : "v"(vo), "s"(la), "s"(src)
-                         : "memory", "m0");
+            copy_to_lds(src, vo, la);
         }
     };
     auto store_row = [&](int rr) {   // wave 0: the 64 sums of row rr from res[(rr - r0) & 1]
