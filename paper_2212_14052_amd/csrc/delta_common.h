@@ -70,20 +70,13 @@ __device__ __forceinline__ void mm_each(A a, B b, C c) {
 __device__ __forceinline__ float low_half(uint32_t w) { return f16_to_f32((uint16_t)(w & 0xffffu)); }
 __device__ __forceinline__ float high_half(uint32_t w) { return f16_to_f32((uint16_t)(w >> 16)); }
 
-// x s and y t as N pieces, a word each: mixed-precision instructions take the
-// product, its rounding to half a word and the remainder, which is exact to
-// float32's rounding, in one step each (written in C the compiler forms the halves twice).
+// x s and y t as N pieces, a word each: the products rounded to half words, and what that leaves, which is exact
+// to float32's rounding, from a mixed-precision instruction each.  (Six instructions a pair; five in inline assembly, but
+// the compiler does not see assembly among the matrix instructions, whose operands must not be
+// written for some cycles before and after.)
 template <int N> __device__ __forceinline__ void split2(float x, float s, float y, float t, uint32_t (&w)[N]) {
-    uint32_t h;
-    asm("v_fma_mixlo_f16 %0, %1, %2, 0" : "=v"(h) : "v"(x), "v"(s));
-    asm("v_fma_mixhi_f16 %0, %1, %2, 0" : "+v"(h) : "v"(y), "v"(t));
-    w[0] = h;
-    if constexpr (N == 2) {
-        float p, q;
-        asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel_hi:[0,0,1]" : "=v"(p) : "v"(x), "v"(s), "v"(h));
-        asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel:[0,0,1] op_sel_hi:[0,0,1]" : "=v"(q) : "v"(y), "v"(t), "v"(h));
-        w[1] = pack_16x2<F16>(p, q);
-    }
+    w[0] = pack_16x2<F16>(x * s, y * t);
+    if constexpr (N == 2) w[1] = pack_16x2<F16>(__builtin_fmaf(x, s, -low_half(w[0])), __builtin_fmaf(y, t, -high_half(w[0])));
 }
 template <int N> __device__ __forceinline__ Op<N> split8(const float (&x)[8], float s) {
     Op<N> o;

@@ -14,6 +14,9 @@ import paper_2212_14052_amd as h3
 
 OBJDUMP = "/opt/rocm/llvm/bin/llvm-objdump"
 BUNDLE = b"__CLANG_OFFLOAD_BUNDLE__"
+# of a matrix instruction: states before its summand's registers may be written, before its result may be read or written
+MATRIX = {"v_mfma_f32_16x16x32_f16": (3, 8), "v_mfma_f32_16x16x32_bf16": (3, 8), "v_mfma_f32_32x32x16_f16": (7, 12),
+          "v_mfma_f32_32x32x16_bf16": (7, 12), "v_mfma_f32_16x16x4_f32": (7, 10)}
 REG = re.compile(r"\b([vsa])(\d+)\b|\b([vsa])\[(\d+):(\d+)\]|\b(m0|vcc)\b")
 
 
@@ -58,6 +61,7 @@ class Instruction:
         self.into_lds = into_lds
         self.writes = ops[0] if ops and not keeps else set()
         self.reads = set().union(set(), *(ops if keeps else ops[1:]))
+        self.summand = ops[3] if self.matrix else set()
         if self.name.startswith(("v_fmac", "v_fma_mixhi")):
             self.reads |= self.writes
 
@@ -68,6 +72,14 @@ def missing(before, states, now):
         return "a write of m0, then a copy into LDS"
     if now.memory and before.vector and states < 5 and any(r[0] == "s" or r == "vcc" for r in before.writes & now.reads):
         return "a scalar register written by a vector instruction, then an address in it"
+    if now.matrix and before.vector and states < 2 and before.writes & now.reads:
+        return "a vector instruction's result into a matrix instruction"
+    if before.matrix and (now.vector or now.memory or now.name.startswith("ds_")):
+        summand, result = MATRIX[before.name]
+        if states < summand and before.summand & now.writes:
+            return "a matrix instruction's summand, overwritten"
+        if states < result and before.writes & (now.reads | now.writes):
+            return "a matrix instruction's result, read or overwritten"
     return None
 
 
@@ -105,6 +117,13 @@ def disassemble_and_read(args):
     ("s_mov_b32 m0, s4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 v1, s[2:3]", 0),
     ("v_readfirstlane_b32 s3, v0\n\ts_nop 3\n\tglobal_load_dword v1, v2, s[2:3]", 1),
     ("v_readfirstlane_b32 s3, v0\n\ts_nop 4\n\tglobal_load_dword v1, v2, s[2:3]", 0),
+    ("v_add_f32_e32 v1, v2, v3\n\tv_mfma_f32_16x16x32_f16 v[4:7], v[0:3], v[8:11], 0", 1),
+    ("v_add_f32_e32 v1, v2, v3\n\ts_nop 1\n\tv_mfma_f32_16x16x32_f16 v[4:7], v[0:3], v[8:11], 0", 0),
+    ("v_mfma_f32_16x16x32_f16 v[4:7], v[0:3], v[8:11], v[12:15]\n\ts_nop 1\n\tv_fma_mixlo_f16 v14, v20, v21, 0", 1),
+    ("v_mfma_f32_16x16x32_f16 v[4:7], v[0:3], v[8:11], v[12:15]\n\ts_nop 2\n\tv_fma_mixlo_f16 v14, v20, v21, 0", 0),
+    ("v_mfma_f32_16x16x32_f16 v[4:7], v[0:3], v[8:11], 0\n\ts_nop 6\n\tv_add_f32_e32 v20, v20, v4", 1),
+    ("v_mfma_f32_16x16x32_f16 v[4:7], v[0:3], v[8:11], 0\n\ts_nop 7\n\tv_add_f32_e32 v20, v20, v4", 0),
+    ("v_mfma_f32_16x16x32_f16 v[4:7], v[0:3], v[8:11], 0\n\ts_branch 9\n\tv_add_f32_e32 v20, v20, v4", 0),
 ])
 def test_the_reader(text, count):
     assert len(faults("0 <k>:\n\t" + text + "\n")) == count
