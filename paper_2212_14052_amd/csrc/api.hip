@@ -69,7 +69,7 @@ struct DeltaWs {
         const size_t dkp = (Dk + 31) / 32 * 32, dvp = (Dv + 15) / 16 * 16;
         const size_t rows = align_up(ch * kDeltaChunk * dvp * 4), state = align_up(ch * dkp * dvp * 4);
         const size_t keys = align_up(ch * 2 * (dtype == H3_F32 ? 2 : 1) * kDeltaChunk * dkp * 2);
-        kq = align_up(ch * delta_rec_bytes(dtype == H3_BF16 ? 3 : 4));
+        kq = align_up(ch * kDeltaRecBytes);
         const int N = delta_chunks(L);
         const DeltaCut cut = delta_cut(B, H, N, Dk, Dv, dtype);
         G = cut.G;
@@ -80,7 +80,7 @@ struct DeltaWs {
         ins = align_up(sgs * Dk * Dv * 4);
         seg = kq + keys;
         fwd = seg + maps + ins + align_up(sgs * 8 * 4);
-        es = align_up(ch * delta_rec_bytes(4));
+        es = align_up(ch * kDeltaRecBytes);
         states = es + rows;
         exps = states + state;
         kept_kq = exps + align_up(ch * kDeltaTiles * sizeof(int2));

@@ -35,7 +35,7 @@ template <int DT, int KS>
 __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__restrict__ rec, uint4 *__restrict__ back,
                                                           uint4 *__restrict__ kq) {
     typedef typename IO<DT>::T T;
-    constexpr int NT = pieces<DT>(), NM = out_pieces<DT>(), NX = 2;
+    constexpr int NT = pieces<DT>(), NX = 2;
     constexpr int KQ = kq_words<KS>(NT);
     // the keys, then A and P in their place; the inverses of the diagonal blocks
     __shared__ uint4 ks[KQ > 2 * DC * AROW / 4 ? KQ : 2 * DC * AROW / 4];
@@ -51,9 +51,9 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g4 = lane >> 4, c16 = lane & 15;
     const long tok0 = (long)b * a.L + n * DC;
     const int hk = h / (a.H / a.Hk);
-    uint4 *xf = rec + ch * ((NX + NM) * MAT + GATES), *pf = xf + NX * MAT;
+    uint4 *xf = rec + ch * (2 * NX * MAT + GATES), *pf = xf + NX * MAT;
     uint4 *xt = back + ch * (2 * NX * MAT + GATES), *pt = xt + NX * MAT;
-    ChunkGates *gf = (ChunkGates *)(pf + NM * MAT), *gb = (ChunkGates *)(pt + NX * MAT);
+    ChunkGates *gf = (ChunkGates *)(pf + NX * MAT), *gb = (ChunkGates *)(pt + NX * MAT);
     const T *kp = (const T *)a.k + (tok0 * a.Hk + hk) * a.Dk, *qp = (const T *)a.q + (tok0 * a.Hk + hk) * a.Dk;
     Raw8<DT> kr[KS], qr[KS];
 #pragma unroll
@@ -251,11 +251,12 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
         if (s <= w / 2) {
             const int f = lower_frag(w, s) * FRAG + lane;
             const Op<NX> x = split8<NX>(xv[s], sx);
-            const Op<NM> p = split8<NM>(pv[s], sp);
+            const Op<NX> p = split8<NX>(pv[s], sp);
 #pragma unroll
-            for (int i = 0; i < NX; ++i) xf[i * MAT + f] = x.p[i];
-#pragma unroll
-            for (int i = 0; i < NM; ++i) pf[i * MAT + f] = p.p[i];
+            for (int i = 0; i < NX; ++i) {
+                xf[i * MAT + f] = x.p[i];
+                pf[i * MAT + f] = p.p[i];
+            }
         }
         if (back && s >= w / 2) {
             const int f = upper_frag(w, s) * FRAG + lane;
@@ -312,9 +313,9 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
                                                                float *__restrict__ es, float *__restrict__ states,
                                                                int2 *__restrict__ exps) {
     typedef typename IO<DT>::T T;
-    constexpr int NT = pieces<DT>(), NX = 2, NO = out_pieces<DT>();
+    constexpr int NT = pieces<DT>(), NX = 2;
     constexpr bool MAPS = MODE == MAP, SAVE = MODE == OUT_SAVE;
-    typedef ChunkCopy<DT, KS, NW, NX + NO, MAPS> Copy;
+    typedef ChunkCopy<DT, KS, NW, MAPS> Copy;
     typedef typename Copy::Lds Lds;
     extern __shared__ uint4 lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
@@ -390,7 +391,7 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
             mm_each<NT, 2, 4>([&](int m) -> const Op<NT> & { return kf[s & 1][m]; }, [&](int) -> const Op<2> & { return so; },
                                    [&](int m) -> dl_f4 & { return R[m]; });
             if constexpr (!MAPS)
-                mm_each<NO, NT, 4>([&](int) -> const Op<2> & { return so; }, [&](int m) -> const Op<NT> & { return qf[s & 1][m]; },
+                mm_each<NX, NT, 4>([&](int) -> const Op<2> & { return so; }, [&](int m) -> const Op<NT> & { return qf[s & 1][m]; },
                                         [&](int m) -> dl_f4 & { return x[m]; });
             in_order<NW == 4>();
         }
@@ -405,9 +406,9 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
         // e = R - (X diag(beta)) R, u = beta e
         const int er = max(wave_exp(R), kLeast);
         const float px = pow2_sum(er + ex), sr = pow2(-er);
-        Op<NO> po[6];
+        Op<NX> po[6];
 #pragma unroll
-        for (int f = 0; f < (MAPS ? 0 : 6); ++f) po[f] = ld_frag<NO>(ps, f, lane);
+        for (int f = 0; f < (MAPS ? 0 : 6); ++f) po[f] = ld_frag<NX>(ps, f, lane);
         in_order<NW == 4>();
         {
             Op<NX> br[2];
@@ -458,15 +459,15 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
             for (int t = 0; t < 4; ++t) px[t] = __builtin_amdgcn_ldexpf(fo[t] * a.scale, eq + eS);
             T *oc = o + (((long)b * a.L + n * DC) * a.H + h) * a.Dv + c0;
             const int room = a.L - n * DC;
-            Op<NO> uo[2];
+            Op<NX> uo[2];
             dl_f4 y[4];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) uo[s] = split8<NO>(u[2 * s], u[2 * s + 1], su);
+            for (int s = 0; s < 2; ++s) uo[s] = split8<NX>(u[2 * s], u[2 * s + 1], su);
 #pragma unroll
             for (int t = 0; t < 4; ++t) y[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
-            mm_each<NO, NO, 4>([&](int) -> const Op<NO> & { return uo[0]; }, [&](int m) -> const Op<NO> & { return po[lower_frag(m, 0)]; },
+            mm_each<NX, NX, 4>([&](int) -> const Op<NX> & { return uo[0]; }, [&](int m) -> const Op<NX> & { return po[lower_frag(m, 0)]; },
                                     [&](int m) -> dl_f4 & { return y[m]; });
-            mm_each<NO, NO, 2>([&](int) -> const Op<NO> & { return uo[1]; }, [&](int m) -> const Op<NO> & { return po[lower_frag(2 + m, 1)]; },
+            mm_each<NX, NX, 2>([&](int) -> const Op<NX> & { return uo[1]; }, [&](int m) -> const Op<NX> & { return po[lower_frag(2 + m, 1)]; },
                                     [&](int m) -> dl_f4 & { return y[2 + m]; });
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -678,7 +679,7 @@ namespace {
 template <int DT, int KS, int NW, ScanMode MODE>
 hipError_t scan_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_final, hipStream_t st) {
     typedef typename IO<DT>::T T;
-    constexpr int lds = ScanLds<DT, KS, NW, 2 + out_pieces<DT>()>::total;
+    constexpr int lds = ScanLds<DT, KS, NW>::total;
     const hipError_t e = lds_room(delta_scan_kernel<DT, KS, NW, MODE>, lds);
     if (e != hipSuccess) return e;
     delta_scan_kernel<DT, KS, NW, MODE><<<(unsigned)((long)a.B * a.H * w.seg.G * col_tiles(a.Dv, NW)), 64 * NW, lds, st>>>(
@@ -694,7 +695,7 @@ hipError_t fwd_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_f
     if (e != hipSuccess) return e;
     const DeltaSegments sg = w.seg;
     if (sg.G > 1) {
-        constexpr int NW = 8, lds = ScanLds<DT, KS, NW, 2 + out_pieces<DT>(), true>::total;
+        constexpr int NW = 8, lds = ScanLds<DT, KS, NW, true>::total;
         if ((e = lds_room(delta_scan_kernel<DT, KS, NW, MAP>, lds)) != hipSuccess) return e;
         delta_scan_kernel<DT, KS, NW, MAP><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW) + col_tiles(a.Dk, NW))), 64 * NW, lds, st>>>(
             a, sg, w.rec, w.kq, nullptr, nullptr, nullptr, nullptr, nullptr);

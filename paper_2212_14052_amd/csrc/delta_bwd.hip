@@ -24,7 +24,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
                                                                    const uint4 *__restrict__ kq, DeltaGrads d) {
     typedef typename IO<DT>::T T;
     constexpr int NT = pieces<DT>(), NM = 2;
-    typedef ChunkCopy<DT, KS, NW, 2 * NM> Copy;
+    typedef ChunkCopy<DT, KS, NW> Copy;
     typedef typename Copy::Lds Lds;
     extern __shared__ uint4 lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
@@ -650,7 +650,7 @@ __global__ __launch_bounds__(64 * grad_waves<KS>, (KS > 2 || ONE ? 2 : 1)) void 
 
 template <int DT, int KS, int NW>
 hipError_t scans_of(const DeltaArgs &a, const DeltaBuffers &w, const DeltaGrads &d, hipStream_t st) {
-    constexpr int lds = ScanLds<DT, KS, NW, 4>::total;
+    constexpr int lds = ScanLds<DT, KS, NW>::total;
     const DeltaSegments sg = w.seg;
     const long bh = (long)a.B * a.H;
     hipError_t e;

@@ -28,10 +28,8 @@ typedef __attribute__((address_space(3))) void dl_lds_void;
 
 // pieces of the inputs by type
 template <int DT> constexpr int pieces() { return DT == F32 ? 2 : 1; }
-// Pieces of what only a 16-bit output is made of (P, u and the state where they meet queries): a bf16
-// output is rounded to 2^-8 at the end, so one piece of 2^-11 for each factor is an eighth of that, of each
-// term; fp16's 2^-11 needs two.  Nothing of it enters the state.
-template <int DT> constexpr int out_pieces() { return DT == BF16 ? 1 : 2; }
+// Everything else is two, also what only a 16-bit output is made of: a value written under a key that held
+// another makes terms cancel, and what one piece rounds away of the old value can be all of the new one.
 
 // an operand of eight values a lane in N pieces
 template <int N> struct Op {
@@ -320,7 +318,7 @@ __device__ __forceinline__ int tokens_of(const DeltaArgs &a, int b) {
 
 // ---------------------------------------------- bringing in a scan's chunk ---
 // A workgroup of NW waves of 16 columns keeps in LDS a chunk's keys and
-// queries, its record (MP pieces of triangular matrices and the gates) and the
+// queries, its record (two triangular matrices in two pieces each, the gates) and the
 // workgroup's columns of V or do.  All of it is copied from memory as it lies there,
 // 1 KB an instruction, without passing through registers, and, where two fit, while the
 // chunk before is worked on.  Nothing is cleared: rows behind the end are copies of the
@@ -328,19 +326,19 @@ __device__ __forceinline__ int tokens_of(const DeltaArgs &a, int b) {
 // stored), columns behind Dv copies of the first ones (not stored either).
 // LEAN: no queries and no P (the first half of a forward record), one chunk at a
 // time, small enough that two workgroups share a CU and wait for each other's turn.
-template <int DT, int KS, int NW, int MP, bool LEAN = false> struct ScanLds {
-    static constexpr int words = MP * MAT + GATES, kq = kq_words<KS>(pieces<DT>());   // uint4
+template <int DT, int KS, int NW, bool LEAN = false> struct ScanLds {
+    static constexpr int words = 4 * MAT + GATES, kq = kq_words<KS>(pieces<DT>());   // uint4
     static constexpr int vrow = 16 * NW, v16 = DC * vrow * (int)sizeof(typename IO<DT>::T) / 16;
-    static constexpr int k = 0, q = kq, v = LEAN ? kq : 2 * kq, rec = v + v16, mats = LEAN ? 2 * MAT : MP * MAT, gates = rec + mats,
+    static constexpr int k = 0, q = kq, v = LEAN ? kq : 2 * kq, rec = v + v16, mats = (LEAN ? 2 : 4) * MAT, gates = rec + mats,
                          one = gates + GATES;
     static constexpr bool two = !LEAN && 2 * one * 16 <= 160 * 1024;
     static constexpr int total = (two ? 2 : 1) * one * 16;
     static_assert(total <= 160 * 1024, "LDS of a CU");
 };
 
-template <int DT, int KS, int NW, int MP, bool LEAN = false> struct ChunkCopy {
+template <int DT, int KS, int NW, bool LEAN = false> struct ChunkCopy {
     typedef typename IO<DT>::T T;
-    typedef ScanLds<DT, KS, NW, MP, LEAN> Lds;
+    typedef ScanLds<DT, KS, NW, LEAN> Lds;
     const uint4 *kq, *rec;   // this key head's and this value head's chunks
     const T *v;              // this value head's row of the first token, at the workgroup's first column
     long vstride;            // elements from token to token
@@ -372,7 +370,7 @@ template <int DT, int KS, int NW, int MP, bool LEAN = false> struct ChunkCopy {
         }
         if constexpr (LEAN) {
             copy_words<Lds::mats>(rn, to + Lds::rec * 16, w, lane);
-            if (w == 0 && lane < GATES) copy(rn + MP * MAT, (uint32_t)lane * 16, to + Lds::gates * 16);
+            if (w == 0 && lane < GATES) copy(rn + 4 * MAT, (uint32_t)lane * 16, to + Lds::gates * 16);
         } else {
             copy_words<Lds::words>(rn, to + Lds::rec * 16, w, lane);
         }

@@ -191,13 +191,13 @@ struct ChunkGates {
     int ek, eq, ex, ep, et, ef, unused[2];
 };
 // Buffers of the chunks of every (b, h).  rec: what a scan of the chunks reads
-// of each, delta_rec_bytes: operand fragments of X (64 x 64, two fp16 pieces)
-// and P (two, one for bf16), the gates.  back: the same of the transposes
+// of each, kDeltaRecBytes: operand fragments of X and P (64 x 64, two fp16 pieces each),
+// the gates.  back: the same of the transposes
 // (two pieces each) for the backward pass.  es (64, Dv padded to 16): the errors e;
 // states (Dk padded to 32, Dv padded to 16): the chunks' first states, both as they lie in a
 // scan's registers: 16 columns, tile, lane, four rows.  The forward pass
 // writes back, es, states and exps where they are given (all or none).
-constexpr size_t delta_rec_bytes(int pieces) { return pieces * kDeltaMatBytes + sizeof(ChunkGates); }
+constexpr size_t kDeltaRecBytes = 4 * kDeltaMatBytes + sizeof(ChunkGates);
 // kq: the keys and queries of every chunk and key head (room for H heads) in the
 // layout that the matrix cores read.  exps: the exponents of the scales of beta e and of the first state, for every 16
 // columns.
