@@ -364,7 +364,7 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
         for (int t = 0; t < 4; ++t) kf[0][t] = lds_rows<NT, KS>(ks, t, 0, lane);
 #pragma unroll
         for (int t = 0; t < (MAPS ? 0 : 4); ++t) qf[0][t] = lds_rows<NT, KS>(qs, t, 0, lane);
-        const int em = max(wave_exp(S), kLeast), eS = em + E;   // of the registers, of S
+        const int e0 = wave_exp(S), em = max(e0, kLeast), eS = em + E;   // of the registers, of S
         const float sc = pow2(-em);
         Op<NX> xo[6];
         dl_f4 be[4], v[4], f0[4];
@@ -434,7 +434,7 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
             dl_f4 *p = (dl_f4 *)es + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 4 * 64 + lane;
 #pragma unroll
             for (int t = 0; t < 4; ++t) store_stream(p + t * 64, __builtin_bit_cast(uint4, R[t]));
-            if (lane == 0) exps[ch * kDeltaTiles + c0 / 16] = make_int2(eu, max(min(eS, 114), -126));
+            if (lane == 0) exps[ch * kDeltaTiles + c0 / 16] = make_int2(eu, kept_exp(e0, E));
         }
         constexpr int TG = KS % 2 == 0 ? 4 : 2;   // state tiles at a time
         Op<NT> kc[2][TG][2];

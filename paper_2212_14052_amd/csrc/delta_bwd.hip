@@ -75,7 +75,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
             dd[t] = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * w, lane);
             if (MAPS && at_.unit) dd[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
         }
-        const int em = max(wave_exp(S), kLeast), eS = em + E;   // of the registers, of dS'
+        const int e0 = wave_exp(S), em = max(e0, kLeast), eS = em + E;   // of the registers, of dS'
         const float sc = pow2(-em);
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
         }
         const int ez = max(wave_exp(y), kLeast), esc = scale_exp(mag(a.scale)) + 13;   // 2^esc: at most the scale
         if (!MAPS && lane == 0)
-            d.exps[ch * kDeltaTiles + c0 / 16] = make_int4(ez, max(min(eS, 114), -126), ed, 0);
+            d.exps[ch * kDeltaTiles + c0 / 16] = make_int4(ez, kept_exp(e0, E), ed, 0);
         // dS <- exp(G_63) dS' + Q^T (f do) - K^T (f y), both in units of the larger one's scale; of
         // 2^-60 of dS' where both are smaller than that
         const int En = max(max(ek + ez + ef, eq + ed + ef + esc + 1), max(eS - 60, E - 100));

@@ -105,9 +105,10 @@ template <int N> __device__ __forceinline__ Op<N> split8(dl_f4 a, dl_f4 b, dl_f4
 
 // -------------------------------------------------------------- scales -----
 // The exponent e with largest 2^-e in 2^13 .. 2^14, from the largest magnitude's
-// bits; 0 for zero, Inf and NaN, -126 where 2^-e would leave float32.
+// bits; 0 for Inf and NaN, -126 where 2^-e would leave float32 and for zero: a tile of
+// zeros must not raise the exponent of what it is added to.
 __device__ __forceinline__ int scale_exp(uint32_t bits) {
-    if (bits == 0 || bits >= 0x7f800000u) return 0;
+    if (bits >= 0x7f800000u) return 0;
     const int e = (int)(bits >> 23) - 127 - 13;
     return e < -126 ? -126 : e;
 }
@@ -117,6 +118,8 @@ __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)
 // (of a value of 2^-67 or less fewer bits go in).
 constexpr int kLeast = -80;
 __device__ __forceinline__ float pow2_sum(int e) { return e < -126 ? 0.f : pow2(e > 127 ? 127 : e); }
+// what the backward pass is told of a state: its exponent e in the registers and E of the registers
+__device__ __forceinline__ int kept_exp(int e, int E) { return e <= -126 ? -126 : max(min(max(e, kLeast) + E, 114), -126); }
 __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
 // the larger of m and the magnitudes of two values

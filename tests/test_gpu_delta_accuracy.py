@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import paper_2212_14052_amd as h3
+from tests.test_gpu_delta_bwd import NAMES, full_inputs, grads_of, reverse
 from tests.test_gpu_delta_rule import DTYPES, inputs, reference
 
 pytestmark = pytest.mark.gpu
@@ -37,3 +38,49 @@ def test_rewritten_keys(dtype, ratio, carried):
     off = (o.double() - ro)[:, first + 32:].norm() / new.norm()
     assert off <= (half(v.dtype) if dtype != "f32" else 0.0) + 2.0 ** -17 * (old.norm() / new.norm()), off.item()
     assert (S.double() - rS).norm() <= 2.0 ** -17 * old.norm()
+
+
+def check_gradients(args, do, dS, lengths=None):
+    """All gradients in the 2-norm: a chunk's roundings of 2^-22 (operands) and 2^-24 (sums) are independent, under
+    2^-21 together; dg is a difference of sums about four times its size.  Not the 16-bit ones that fp16 holds with
+    fewer bits."""
+    q, k, v, g, beta, S0 = args
+    refs = reverse(q, k, v, g, beta, S0, do, dS, q.shape[-1] ** -0.5, lengths)[0]
+    got = grads_of(q, k, v, g, beta, S0, do, dS, None, lengths)
+    for name, x, ref in zip(NAMES, got, refs):
+        if x.dtype == torch.float16:
+            continue
+        tol = (half(x.dtype) if x.dtype != torch.float32 else 0.0) + 2.0 ** (-19 if name == "dg" else -21) * -(-v.shape[1] // 64)
+        assert (x.double() - ref).norm() <= tol * ref.norm(), (name, ((x.double() - ref).norm() / ref.norm()).item())
+
+
+GRAD_SIZES = [(2, 192, 2, 2, 128, 128), (1, 150, 4, 2, 64, 40), (2, 130, 2, 2, 32, 72), (1, 2700, 1, 1, 64, 64)]
+
+
+@pytest.mark.parametrize("size", [2.0 ** -20, 2.0 ** -30])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,L,H,Hk,Dk,Dv", GRAD_SIZES)
+def test_only_the_final_state_has_a_small_gradient(B, L, H, Hk, Dk, Dv, dtype, size):
+    q, k, v, g, beta, S0, do, dS = full_inputs(B, L, H, Hk, Dk, Dv, dtype, 21)
+    check_gradients((q, k, v, g * 0.01, beta, S0), torch.zeros_like(do), dS * size)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,L,H,Hk,Dk,Dv", GRAD_SIZES)
+def test_no_gradient_from_a_prompt(B, L, H, Hk, Dk, Dv, dtype):
+    """The outputs of the first tokens have no gradient, those of the last ones a small one."""
+    q, k, v, g, beta, S0, do, dS = full_inputs(B, L, H, Hk, Dk, Dv, dtype, 22)
+    do *= 2.0 ** -14 if dtype == "f16" else 2.0 ** -30
+    do[:, :L - 40] = 0.0
+    check_gradients((q, k, v, g * 0.01, beta, S0), do, None)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,L,H,Hk,Dk,Dv", GRAD_SIZES)
+def test_columns_of_zeros(B, L, H, Hk, Dk, Dv, dtype):
+    """Sixteen columns of zeros beside small ones, in the values, the states and the gradients."""
+    q, k, v, g, beta, S0, do, dS = full_inputs(B, L, H, Hk, Dk, Dv, dtype, 23)
+    for t, size in ((v, 2.0 ** -10), (S0, 2.0 ** -26), (do, 2.0 ** -12), (dS, 2.0 ** -28)):
+        t *= size if dtype == "f16" else size * size
+        t[..., 16:32] = 0.0
+    check_gradients((q, k, v, g, beta, S0), do, dS)
