@@ -292,9 +292,9 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
 // NW waves of 16 columns.  es, states, exps: for the backward pass, or null.
 //
 // A wave's vector instructions take longer than its matrix instructions here,
-// so scales cost nothing of their own: they ride on the rounding to pieces, on the
-// decays, or on a sum's multiplication.  The registers hold S 2^-E with one exponent
-// E for the wave, that of the last chunk's keys times errors, so that a chunk is
+// so scales cost next to nothing of their own: they ride on the rounding to pieces, on the
+// decays, or on a sum's multiplication.  The registers hold S 2^-E with an exponent
+// E for each column, that of the last chunk's keys times errors, so that a chunk is
 // added in the same instruction that decays them.
 //
 // What the backward pass reads is stored between the last products, and past the caches: a CU takes
@@ -364,7 +364,7 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
         for (int t = 0; t < 4; ++t) kf[0][t] = lds_rows<NT, KS>(ks, t, 0, lane);
 #pragma unroll
         for (int t = 0; t < (MAPS ? 0 : 4); ++t) qf[0][t] = lds_rows<NT, KS>(qs, t, 0, lane);
-        const int e0 = wave_exp(S), em = max(e0, kLeast), eS = em + E;   // of the registers, of S
+        const int e0 = col_exp(S), em = max(e0, kLeast), eS = em + E;   // of the registers, of S
         const float sc = pow2(-em);
         Op<NX> xo[6];
         dl_f4 be[4], v[4], f0[4];
@@ -404,7 +404,7 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
                 R[t][r] = v[t][r] - f * R[t][r];
             }
         // e = R - (X diag(beta)) R, u = beta e
-        const int er = max(wave_exp(R), kLeast);
+        const int er = max(col_exp(R), kLeast);
         const float px = pow2_sum(er + ex), sr = pow2(-er);
         Op<NX> po[6];
 #pragma unroll
@@ -429,12 +429,13 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
                     u[t][r] = be[t][r] * R[t][r];
                 }
         }
-        const int eu = max(wave_exp(u), kLeast);
+        const int eu = max(col_exp(u), kLeast);
         if constexpr (SAVE) {
             dl_f4 *p = (dl_f4 *)es + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 4 * 64 + lane;
 #pragma unroll
             for (int t = 0; t < 4; ++t) store_stream(p + t * 64, __builtin_bit_cast(uint4, R[t]));
-            if (lane == 0) exps[ch * kDeltaTiles + c0 / 16] = make_int2(eu, kept_exp(e0, E));
+            const int2 e = make_int2(tile_exp(eu), tile_exp(kept_exp(e0, E)));
+            if (lane == 0) exps[ch * kDeltaTiles + c0 / 16] = e;
         }
         constexpr int TG = KS % 2 == 0 ? 4 : 2;   // state tiles at a time
         Op<NT> kc[2][TG][2];
@@ -453,10 +454,14 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
         in_order<NW == 4>();
         // o = scale (exp(G) Q S + P u)
         if constexpr (!MAPS) {
-            const float py = __builtin_amdgcn_ldexpf(a.scale, ep + eu), su = pow2(-eu);
-            float px[4];
+            const float su = pow2(-eu);
+            float px[4], py[4];   // rows are columns of S and u here: their exponents come from those columns' lanes
 #pragma unroll
-            for (int t = 0; t < 4; ++t) px[t] = __builtin_amdgcn_ldexpf(fo[t] * a.scale, eq + eS);
+            for (int r = 0; r < 4; ++r) {
+                const int e = __shfl(eS * 65536 + eu, 4 * g4 + r);   // |eu| < 2^15
+                px[r] = __builtin_amdgcn_ldexpf(a.scale, eq + ((e + 32768) >> 16));
+                py[r] = __builtin_amdgcn_ldexpf(a.scale, ep + (int)(int16_t)e);
+            }
             T *oc = o + (((long)b * a.L + n * DC) * a.H + h) * a.Dv + c0;
             const int room = a.L - n * DC;
             Op<NX> uo[2];
@@ -472,7 +477,7 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[t][r] = x[t][r] * px[t] + y[t][r] * py;
+                for (int r = 0; r < 4; ++r) x[t][r] = x[t][r] * fo[t] * px[r] + y[t][r] * py[r];
             if (nt < DC) {   // the last chunk: places behind the end are 0
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
@@ -626,7 +631,7 @@ __global__ __launch_bounds__(256, 1) void delta_join_kernel(DeltaArgs a, DeltaSe
         dl_f4 S[2 * KS], y[TW];
 #pragma unroll
         for (int t = 0; t < 2 * KS; ++t) S[t] = st[t][lane];
-        const int es = wave_exp(S), e = es + ef;
+        const int es = col_exp(S), e = es + ef;
         Op<2> so[KS];
 #pragma unroll
         for (int s = 0; s < KS; ++s) so[s] = split8<2>(S[2 * s], S[2 * s + 1], pow2(-es));

@@ -75,7 +75,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
             dd[t] = lds_column4<DT>(vs, Lds::vrow, 16 * t, 16 * w, lane);
             if (MAPS && at_.unit) dd[t] = dl_f4{0.f, 0.f, 0.f, 0.f};
         }
-        const int e0 = wave_exp(S), em = max(e0, kLeast), eS = em + E;   // of the registers, of dS'
+        const int e0 = col_exp(S), em = max(e0, kLeast), eS = em + E;   // of the registers, of dS'
         const float sc = pow2(-em);
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
 #pragma unroll
                 for (int r = 0; r < 4; ++r) dd[t][r] = 16 * t + 4 * g4 + r < nt ? dd[t][r] : 0.f;
         }
-        const int ed = max(wave_exp(dd), kLeast);
+        const int ed = max(col_exp(dd), kLeast);
 #pragma unroll
         for (int f = 0; f < 6; ++f) xf[f] = ld_frag<NM>(xs, f, lane);
         in_order<NW == 4>();
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
                 for (int r = 0; r < 4; ++r) u[t][r] = te[t][r] * u[t][r] + py * x[t][r];
         }
         // z = du - (diag(beta) X)^T du; then y for the state
-        const int eu = max(wave_exp(u), kLeast);
+        const int eu = max(col_exp(u), kLeast);
         const float px = pow2_sum(eu + ex), su = pow2(-eu);
         Op<NT> kc[2][2][2], qc[2][2][2];   // two state tiles at a time
         dl_f4 f0[4];
@@ -168,9 +168,11 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
                 for (int r = 0; r < 4; ++r) y[t][r] = be[t][r] * z[r];
             }
         }
-        const int ez = max(wave_exp(y), kLeast), esc = scale_exp(mag(a.scale)) + 13;   // 2^esc: at most the scale
-        if (!MAPS && lane == 0)
-            d.exps[ch * kDeltaTiles + c0 / 16] = make_int4(ez, kept_exp(e0, E), ed, 0);
+        const int ez = max(col_exp(y), kLeast), esc = scale_exp(mag(a.scale)) + 13;   // 2^esc: at most the scale
+        if constexpr (!MAPS) {
+            const int4 e = make_int4(tile_exp(ez), tile_exp(kept_exp(e0, E)), tile_exp(ed), 0);
+            if (lane == 0) d.exps[ch * kDeltaTiles + c0 / 16] = e;
+        }
         // dS <- exp(G_63) dS' + Q^T (f do) - K^T (f y), both in units of the larger one's scale; of
         // 2^-60 of dS' where both are smaller than that
         const int En = max(max(ek + ez + ef, eq + ed + ef + esc + 1), max(eS - 60, E - 100));

@@ -127,16 +127,23 @@ __device__ __forceinline__ float max3_abs(float m, float x, float y) {
     asm("v_max3_f32 %0, %0, |%1|, |%2|" : "+v"(m) : "v"(x), "v"(y));
     return m;
 }
-// the exponent for x of the whole wave
-template <int N> __device__ __forceinline__ int wave_exp(const dl_f4 (&x)[N]) {
+// The exponent for x of this lane's column, whose rows four lanes share.  Columns of a state are
+// independent: each has its own scales, so that none loses bits, or all of them, by another's size.
+template <int N> __device__ __forceinline__ int col_exp(const dl_f4 (&x)[N]) {
     float m = 0.f;
 #pragma unroll
     for (int t = 0; t < N; ++t) {
         m = max3_abs(m, x[t][0], x[t][1]);
         m = max3_abs(m, x[t][2], x[t][3]);
     }
-    return scale_exp(__builtin_amdgcn_readfirstlane(group_max<64>(__float_as_uint(m))));
+    uint32_t b = __float_as_uint(m);
+    const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    b = umax(r[0], r[1]);
+    const auto s = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return scale_exp(umax(s[0], s[1]));
 }
+// the largest of the 16 columns' exponents
+__device__ __forceinline__ int tile_exp(int e) { return (int)group_max<16>((uint32_t)(e + 1024)) - 1024; }
 
 // Eight consecutive inputs as floats; zeros where !on.
 template <int DT> __device__ __forceinline__ void ld8(const typename IO<DT>::T *p, bool on, float (&x)[8]) {
@@ -424,7 +431,7 @@ template <int NW, bool MAPS, bool BACK = false> struct ScanPlace {
 // second part with the exponent of its scale for every 16 columns.
 template <int KS, typename P>
 __device__ __forceinline__ void store_map(const DeltaArgs &a, const DeltaSegments &sg, const P &at, const dl_f4 (&S)[2 * KS], int lane) {
-    const int dvp = (a.Dv + 15) & ~15, row = dvp + 32 * KS, e = wave_exp(S);
+    const int dvp = (a.Dv + 15) & ~15, row = dvp + 32 * KS, e = tile_exp(col_exp(S));
     float *p = sg.maps + ((at.bh * sg.G + at.seg) * 32 * KS + 8 * (lane >> 4)) * row + (at.unit ? dvp : 0) + at.c0 + (lane & 15);
 #pragma unroll
     for (int t = 0; t < 2 * KS; ++t)

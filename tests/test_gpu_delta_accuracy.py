@@ -84,3 +84,29 @@ def test_columns_of_zeros(B, L, H, Hk, Dk, Dv, dtype):
         t *= size if dtype == "f16" else size * size
         t[..., 16:32] = 0.0
     check_gradients((q, k, v, g, beta, S0), do, dS)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,L,H,Hk,Dk,Dv", [(2, 150, 2, 2, 128, 128), (1, 130, 4, 2, 40, 24), (1, 2700, 1, 1, 64, 72), (16, 65, 16, 16, 128, 128)])
+def test_columns_do_not_meet(B, L, H, Hk, Dk, Dv, dtype):
+    """A column of the values and states that is much larger, much smaller, or not finite leaves every bit of the
+    others as it was, and scales by itself."""
+    q, k, v, g, beta, S0, do, dS = full_inputs(B, L, H, Hk, Dk, Dv, dtype, 24)
+    rest = torch.arange(Dv, device="cuda") != 3
+    o, S = h3.delta_rule(q, k, v, g, beta, S0=S0)
+    gr = grads_of(q, k, v, g, beta, S0, do, dS)
+    for size in ((2.0 ** 5,) if dtype == "f16" else (2.0 ** 24, 2.0 ** -24, 2.0 ** 60, 2.0 ** -60)):
+        f = torch.where(rest, 1.0, size)
+        o2, S2 = h3.delta_rule(q, k, v * f.to(v.dtype), g, beta, S0=S0 * f)
+        assert torch.equal(o2[..., rest], o[..., rest]) and torch.equal(S2, S * f)
+        assert dtype == "f16" or torch.equal(o2, o * f.to(o.dtype))
+        gr2 = grads_of(q, k, v, g, beta, S0, do * f.to(do.dtype), dS * f)
+        assert torch.equal(gr2[2][..., rest], gr[2][..., rest]) and torch.equal(gr2[5], gr[5] * f)
+    for bad in (float("inf"), float("nan")):
+        v2, do2 = v.clone(), do.clone()
+        v2[:, L // 2, :, 3] = do2[:, L // 2, :, 3] = bad
+        o2, S2 = h3.delta_rule(q, k, v2, g, beta, S0=S0)
+        assert torch.equal(o2[..., rest], o[..., rest]) and torch.equal(S2[..., rest], S[..., rest])
+        assert not S2[..., 3].isfinite().any()
+        gr2 = grads_of(q, k, v, g, beta, S0, do2, dS)
+        assert torch.equal(gr2[2][..., rest], gr[2][..., rest]) and torch.equal(gr2[5][..., rest], gr[5][..., rest])
