@@ -311,7 +311,7 @@ int h3_layernorm_bwd(const void *dy, const void *x, const float *w, const float 
  *   S           (B, H, Dk, Dv) float32, 16-byte aligned, read and overwritten.
  *   Dk a multiple of 8 up to H3_DELTA_MAX_DK, Dv one up to H3_DELTA_MAX_DV;
  *   Hk divides H.  Outputs overlap nothing.  Arithmetic in float32.
- * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, B H ceil(Dv / 32) >= 2^26), EDEVICE.
+ * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, B H ceil(Dv / 32) > 2^26 - 4), EDEVICE.
  */
 int h3_delta_step(const void *q, const void *k, const void *v, const float *g, const float *beta, float scale, int B,
                   int T, int H, int Hk, int Dk, int Dv, int dtype, float *S, void *o, void *stream);
@@ -337,7 +337,8 @@ int h3_delta_step(const void *q, const void *k, const void *v, const float *g, c
  * float64; a NaN or Inf may reach every token of its chunk of 64.  Where no token
  * stretches the state (g <= 0, 0 <= beta |k|^2 <= 2) a chunk is off by a few 2^-22 of the state's size;
  * where tokens do, a chunk's solved matrix grows with what its 64 tokens stretch, and its errors with it.
- * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, 2^31 chunks, H Dv > 2^22), EWORKSPACE, EDEVICE.
+ * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, H Dv > 2^22, 2^32 threads a launch: from B H ceil(L / 64) of
+ * 2^23 (2^24 where Dk <= 64), or B H ceil(Dv / 64) of 2^24, on), EWORKSPACE, EDEVICE.
  */
 int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, const float *beta, const float *S0,
                   const int *lengths, float scale, int B, int L, int H, int Hk, int Dk, int Dv, int dtype, void *o,
@@ -357,7 +358,7 @@ int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, c
  *               Gradients of tokens from lengths[b] on are 0.
  *   workspace   >= h3_workspace_size(H3_OP_DELTA_BWD, B, H, L, Dk, Dv, dtype).
  * Nothing else that is written overlaps anything.  Results do not depend on timing.
- * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, 2^31 chunks, H Dv > 2^22), EWORKSPACE, EDEVICE.
+ * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, H Dv > 2^22, 2^32 threads: see h3_delta_rule), EWORKSPACE, EDEVICE.
  */
 int h3_delta_rule_bwd(const void *q, const void *k, const void *v, const float *g, const float *beta, const void *dout,
                       const float *dS, const void *saved, size_t saved_bytes, const int *lengths, float scale, int B, int L,

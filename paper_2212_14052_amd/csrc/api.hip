@@ -37,8 +37,7 @@ bool delta_sizes_ok(int Dk, int Dv) {
     return Dk >= 8 && Dk % 8 == 0 && Dk <= H3_DELTA_MAX_DK && Dv >= 8 && Dv % 8 == 0 && Dv <= H3_DELTA_MAX_DV;
 }
 int delta_chunks(int L) { return (L - 1) / kDeltaChunk + 1; }
-// its launches hold one workgroup a chunk: at most 2^31 - 1; offsets inside a
-// chunk are 32 bits
+// numbers of workgroups are 32 bits, offsets inside a chunk too
 bool delta_chunks_ok(int B, int L, int H, int Dv) {
     return (double)H * Dv <= 4194304.0 && (double)B * H * delta_chunks(L) < 2147483647.0 && (double)B * H * ((Dv + 15) / 16) < 2147483647.0;
 }
@@ -64,6 +63,7 @@ struct DeltaBytes {
 struct DeltaWs {
     size_t kq, seg, es, states, exps, kept_kq, dends, bexps, bseg, fwd, saved, bwd, maps, ins;
     int G, Ns, NW;
+    bool launches;   // every launch of either pass has fewer than 2^32 threads
     DeltaWs(int B, int H, int L, int Dk, int Dv, int dtype) {
         const size_t ch = (size_t)B * H * delta_chunks(L);
         const size_t dkp = (Dk + 31) / 32 * 32, dvp = (Dv + 15) / 16 * 16;
@@ -75,6 +75,12 @@ struct DeltaWs {
         G = cut.G;
         NW = cut.NW;
         Ns = (N + G - 1) / G;
+        const double bh = (double)B * H, wave = 64.0 * NW;
+        const int v = delta_col_tiles(Dv, NW), kv = v + delta_col_tiles(Dk, NW), kv8 = delta_col_tiles(Dv, 8) + delta_col_tiles(Dk, 8);
+        launches = bh * N * (Dk > 64 ? 512 : 256) < 4294967296.0 &&          // chunks, their gradients
+                   bh * G * v * wave < 4294967296.0 &&                       // scans
+                   (G == 1 || (bh * (G - 1) * kv8 * 512 < 4294967296.0 &&    // maps, forward and backward, and their joining
+                               bh * (G - 1) * kv * wave < 4294967296.0 && bh * delta_col_tiles(Dv, 1) * 256 < 4294967296.0));
         const size_t sgs = G > 1 ? (size_t)B * H * G : 0;
         maps = align_up(sgs * dkp * (dvp + dkp) * 4);
         ins = align_up(sgs * Dk * Dv * 4);
@@ -301,11 +307,12 @@ size_t h3_workspace_size(int op, int B, int H, int L, int m, int chunk, int dtyp
             if (chunk != 2 && chunk != 4 && chunk != 8) return 0;
             return heads_ws(B, H, L, chunk).total;
         case H3_OP_DELTA:   // m = Dk, chunk = Dv
-            return delta_ok(B, L, H, m, chunk) ? DeltaWs(B, H, L, m, chunk, dtype).fwd : 0;
         case H3_OP_DELTA_SAVED:
-            return delta_ok(B, L, H, m, chunk) ? DeltaWs(B, H, L, m, chunk, dtype).saved : 0;
-        case H3_OP_DELTA_BWD:
-            return delta_ok(B, L, H, m, chunk) ? DeltaWs(B, H, L, m, chunk, dtype).bwd : 0;
+        case H3_OP_DELTA_BWD: {
+            if (!delta_ok(B, L, H, m, chunk)) return 0;
+            const DeltaWs w(B, H, L, m, chunk, dtype);
+            return !w.launches ? 0 : op == H3_OP_DELTA ? w.fwd : op == H3_OP_DELTA_SAVED ? w.saved : w.bwd;
+        }
         case H3_OP_LAYERNORM_BWD:   // B = rows, H = d
             return norm_width_ok(H) ? align_up(layernorm_bwd_workspace(B, H)) : 0;
         case H3_OP_FFTCONV_BWD: {
@@ -658,7 +665,7 @@ int h3_delta_step(const void *q, const void *k, const void *v, const float *g, c
                   int T, int H, int Hk, int Dk, int Dv, int dtype, float *S, void *o, void *stream) {
     if (!q || !k || !v || !g || !beta || !S || !o || B < 1 || T < 1 || H < 1 || Hk < 1 || Dk < 1 || Dv < 1 || H % Hk)
         return H3_EINVAL;
-    if (!dtype_ok(dtype) || !delta_sizes_ok(Dk, Dv) || (double)B * H * ((Dv + 31) / 32) >= 67108864.0)   // 2^26 waves
+    if (!dtype_ok(dtype) || !delta_sizes_ok(Dk, Dv) || (double)B * H * ((Dv + 31) / 32) > 67108860.0)   // in workgroups of four waves under 2^32 threads
         return H3_EUNSUPPORTED;
     const DeltaBytes n(B, T, H, Hk, Dk, Dv, dtype);
     const uintptr_t ea = esize(dtype) - 1;
@@ -681,6 +688,7 @@ int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, c
     if (!dtype_ok(dtype) || !delta_ok(B, L, H, Dk, Dv)) return H3_EUNSUPPORTED;
     const DeltaWs w(B, H, L, Dk, Dv, dtype);
     if (!workspace || ws_bytes < w.fwd || (saved && saved_bytes < w.saved)) return H3_EWORKSPACE;
+    if (!w.launches) return H3_EUNSUPPORTED;
     const DeltaBytes n(B, L, H, Hk, Dk, Dv, dtype);
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || ((uintptr_t)g & 3) || ((uintptr_t)beta & 3) ||
         ((uintptr_t)S0 & 3) || ((uintptr_t)S_final & 3) || ((uintptr_t)lengths & 3) || !aligned16(saved) ||
@@ -721,6 +729,7 @@ int h3_delta_rule_bwd(const void *q, const void *k, const void *v, const float *
     if (!dtype_ok(dtype) || !delta_ok(B, L, H, Dk, Dv)) return H3_EUNSUPPORTED;
     const DeltaWs w(B, H, L, Dk, Dv, dtype);
     if (!workspace || ws_bytes < w.bwd || saved_bytes < w.saved) return H3_EWORKSPACE;
+    if (!w.launches) return H3_EUNSUPPORTED;
     const DeltaBytes n(B, L, H, Hk, Dk, Dv, dtype);
     for (const void *p : {q, k, v, dout, saved, (const void *)dq, (const void *)dk, (const void *)dv, (const void *)workspace})
         if (!aligned16(p)) return H3_EINVAL;

@@ -350,7 +350,7 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
         const uint4 *ks = at + Lds::k, *qs = at + Lds::q, *xs = at + Lds::rec, *ps = xs + NX * MAT;
         const T *vs = (const T *)(at + Lds::v);
         const ChunkGates *gt = (const ChunkGates *)(at + Lds::gates);
-        dl_f4 *kept = (dl_f4 *)states + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;   // where this state is left
+        dl_f4 *kept = (dl_f4 *)states + (ch * delta_col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;   // where this state is left
         const int ek = __builtin_amdgcn_readfirstlane(gt->ek), eq = __builtin_amdgcn_readfirstlane(gt->eq),
                   ex = __builtin_amdgcn_readfirstlane(gt->ex), ep = __builtin_amdgcn_readfirstlane(gt->ep),
                   et = __builtin_amdgcn_readfirstlane(gt->et);
@@ -431,7 +431,7 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
         }
         const int eu = max(col_exp(u), kLeast);
         if constexpr (SAVE) {
-            dl_f4 *p = (dl_f4 *)es + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 4 * 64 + lane;
+            dl_f4 *p = (dl_f4 *)es + (ch * delta_col_tiles(a.Dv, 1) + c0 / 16) * 4 * 64 + lane;
 #pragma unroll
             for (int t = 0; t < 4; ++t) store_stream(p + t * 64, __builtin_bit_cast(uint4, R[t]));
             const int2 e = make_int2(tile_exp(eu), tile_exp(kept_exp(e0, E)));
@@ -669,8 +669,8 @@ DeltaCut delta_cut(int B, int H, int N, int Dk, int Dv, int dtype) {
     for (int NW = 4; NW <= (dtype == F32 ? 4 : 8); NW += 4)
         for (int G = 1; G <= 64 && (G == 1 || 4 * G <= N); ++G) {
             const double Ns = (N + G - 1) / G;
-            double t = (NW == 4 ? 1.0 : 1.5) * ceil(bh * col_tiles(Dv, NW) * G / 256) * Ns;
-            if (G > 1) t += kMaps * ceil(bh * (col_tiles(Dv, 8) + col_tiles(Dk, 8)) * (G - 1) / 512) * Ns + 1.3 * G + 5;
+            double t = (NW == 4 ? 1.0 : 1.5) * ceil(bh * delta_col_tiles(Dv, NW) * G / 256) * Ns;
+            if (G > 1) t += kMaps * ceil(bh * (delta_col_tiles(Dv, 8) + delta_col_tiles(Dk, 8)) * (G - 1) / 512) * Ns + 1.3 * G + 5;
             if ((NW == 4 && G == 1) || t < 0.95 * least) {
                 best = DeltaCut{G, NW};
                 least = t;
@@ -687,7 +687,7 @@ hipError_t scan_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_
     constexpr int lds = ScanLds<DT, KS, NW>::total;
     const hipError_t e = lds_room(delta_scan_kernel<DT, KS, NW, MODE>, lds);
     if (e != hipSuccess) return e;
-    delta_scan_kernel<DT, KS, NW, MODE><<<(unsigned)((long)a.B * a.H * w.seg.G * col_tiles(a.Dv, NW)), 64 * NW, lds, st>>>(
+    delta_scan_kernel<DT, KS, NW, MODE><<<(unsigned)((long)a.B * a.H * w.seg.G * delta_col_tiles(a.Dv, NW)), 64 * NW, lds, st>>>(
         a, w.seg, w.rec, w.kq, (T *)o, S_final, w.es, w.states, w.exps);
     return hipGetLastError();
 }
@@ -702,7 +702,7 @@ hipError_t fwd_of(const DeltaArgs &a, const DeltaBuffers &w, void *o, float *S_f
     if (sg.G > 1) {
         constexpr int NW = 8, lds = ScanLds<DT, KS, NW, true>::total;
         if ((e = lds_room(delta_scan_kernel<DT, KS, NW, MAP>, lds)) != hipSuccess) return e;
-        delta_scan_kernel<DT, KS, NW, MAP><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW) + col_tiles(a.Dk, NW))), 64 * NW, lds, st>>>(
+        delta_scan_kernel<DT, KS, NW, MAP><<<(unsigned)(bh * (sg.G - 1) * (delta_col_tiles(a.Dv, NW) + delta_col_tiles(a.Dk, NW))), 64 * NW, lds, st>>>(
             a, sg, w.rec, w.kq, nullptr, nullptr, nullptr, nullptr, nullptr);
         if ((e = launch_delta_join(a, sg, a.S0, false, st)) != hipSuccess) return e;
     }

@@ -59,7 +59,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
         const T *vs = (const T *)(at + Lds::v);
         const ChunkGates *gt = (const ChunkGates *)(at + Lds::gates);
         const int nt = min(DC, len - n * DC);
-        dl_f4 *kept = (dl_f4 *)d.dends + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;   // where this state is left
+        dl_f4 *kept = (dl_f4 *)d.dends + (ch * delta_col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;   // where this state is left
         const int ek = __builtin_amdgcn_readfirstlane(gt->ek), eq = __builtin_amdgcn_readfirstlane(gt->eq),
                   ex = __builtin_amdgcn_readfirstlane(gt->ex), ep = __builtin_amdgcn_readfirstlane(gt->ep),
                   ef = __builtin_amdgcn_readfirstlane(gt->ef);
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
                                     [&](int m) -> dl_f4 & { return x[m]; });
             mm_each<NM, NM, 2>([&](int m) -> const Op<NM> & { return xf[upper_frag(m, 0)]; }, [&](int) -> const Op<NM> & { return bu[0]; },
                                     [&](int m) -> dl_f4 & { return x[m]; });
-            dl_f4 *p = (dl_f4 *)d.zs + (ch * col_tiles(a.Dv, 1) + c0 / 16) * 4 * 64 + lane;
+            dl_f4 *p = (dl_f4 *)d.zs + (ch * delta_col_tiles(a.Dv, 1) + c0 / 16) * 4 * 64 + lane;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 dl_f4 z;
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(64 * grad_waves<KS>, (KS > 2 || ONE ? 2 : 1)) void 
     const int wt = w & 3, half = w >> 2;   // token tile; which columns of 32, which of D and E
     // chunks from the front first: the scan wrote theirs last
     const int hk = (int)(blockIdx.x % a.Hk), b = (int)(blockIdx.x / a.Hk % a.B), n = (int)(blockIdx.x / a.Hk / a.B);
-    const int per = ONE ? 1 : a.H / a.Hk, ct16 = col_tiles(a.Dv, 1);
+    const int per = ONE ? 1 : a.H / a.Hk, ct16 = delta_col_tiles(a.Dv, 1);
     const int nt = min(DC, tokens_of(a, b) - n * DC), room = min(DC, a.L - n * DC);   // tokens, and places, of this chunk
     const long tok0 = (long)b * a.L + n * DC;
     const T *op = (const T *)d.dout;
@@ -658,12 +658,12 @@ hipError_t scans_of(const DeltaArgs &a, const DeltaBuffers &w, const DeltaGrads 
     hipError_t e;
     if (sg.G > 1) {
         if ((e = lds_room(delta_bwd_scan_kernel<DT, KS, NW, true>, lds)) != hipSuccess) return e;
-        delta_bwd_scan_kernel<DT, KS, NW, true><<<(unsigned)(bh * (sg.G - 1) * (col_tiles(a.Dv, NW) + col_tiles(a.Dk, NW))), 64 * NW, lds, st>>>(
+        delta_bwd_scan_kernel<DT, KS, NW, true><<<(unsigned)(bh * (sg.G - 1) * (delta_col_tiles(a.Dv, NW) + delta_col_tiles(a.Dk, NW))), 64 * NW, lds, st>>>(
             a, sg, w.back, w.kq, d);
         if ((e = launch_delta_join(a, sg, d.dS, true, st)) != hipSuccess) return e;
     }
     if ((e = lds_room(delta_bwd_scan_kernel<DT, KS, NW, false>, lds)) != hipSuccess) return e;
-    delta_bwd_scan_kernel<DT, KS, NW, false><<<(unsigned)(bh * sg.G * col_tiles(a.Dv, NW)), 64 * NW, lds, st>>>(a, sg, w.back, w.kq, d);
+    delta_bwd_scan_kernel<DT, KS, NW, false><<<(unsigned)(bh * sg.G * delta_col_tiles(a.Dv, NW)), 64 * NW, lds, st>>>(a, sg, w.back, w.kq, d);
     return hipGetLastError();
 }
 

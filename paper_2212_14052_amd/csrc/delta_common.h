@@ -403,9 +403,6 @@ template <int DT, int KS, int NW, bool LEAN = false> struct ChunkCopy {
 };
 
 // ---------------------------------------------------------------- segments ---
-// workgroups of n times 16 columns
-constexpr int col_tiles(int cols, int n) { return (cols + 16 * n - 1) / (16 * n); }
-
 // What a workgroup of a scan works on: a (b, h), a segment, its columns.  With MAPS
 // there are the columns of V from a zero state, and then the unit matrix's
 // from no values; no map is needed of the last segment (BACK: of the first).
@@ -414,7 +411,7 @@ template <int NW, bool MAPS, bool BACK = false> struct ScanPlace {
     int b, h, seg, cb, c0, width;   // width: columns there are
     bool unit;
     __device__ __forceinline__ ScanPlace(const DeltaArgs &a, const DeltaSegments &sg, unsigned block, int w) {
-        const int v = col_tiles(a.Dv, NW), tiles = v + (MAPS ? col_tiles(a.Dk, NW) : 0), segs = sg.G - (MAPS ? 1 : 0);
+        const int v = delta_col_tiles(a.Dv, NW), tiles = v + (MAPS ? delta_col_tiles(a.Dk, NW) : 0), segs = sg.G - (MAPS ? 1 : 0);
         const int tile = (int)(block % tiles);
         seg = (int)(block / tiles % segs) + (MAPS && BACK ? 1 : 0);
         bh = block / tiles / segs;

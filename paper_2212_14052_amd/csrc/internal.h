@@ -215,6 +215,8 @@ struct DeltaSegments {
 struct DeltaCut {
     int G, NW;
 };
+// workgroups of n times 16 columns
+constexpr int delta_col_tiles(int cols, int n) { return (cols + 16 * n - 1) / (16 * n); }
 DeltaCut delta_cut(int B, int H, int N, int Dk, int Dv, int dtype);
 constexpr int kDeltaTiles = 16;   // 16 columns each, at most
 struct DeltaBuffers {

@@ -1,0 +1,17 @@
+"""The largest calls that the layer norm and the delta rule take, and what is refused beyond (no GPU needed)."""
+import paper_2212_14052_amd as h3
+from tests.test_abi_mixers import EINVAL, EUNSUP, O, V, bwd, rule, size, step
+
+
+def test_launches_of_less_than_2_to_32_threads():
+    """Scans of four workgroups of 256 threads a head (two of 512), in one launch: 2^22 heads are too many."""
+    many = dict(L=1, Dk=8, Dv=256)
+    for op in (h3.OP_DELTA, h3.OP_DELTA_SAVED, h3.OP_DELTA_BWD):
+        assert size(op, B=1 << 19, H=8, **many) == 0
+        assert size(op, B=(1 << 22) - 1, H=1, **many) > 0
+        assert size(op, B=1 << 21, L=256, H=1, Dk=128, Dv=8) == 0       # 2^23 chunks, their gradients by 512 threads each
+    assert rule(B=1 << 19, H=8, Hk=8, wsb=1 << 62, **many) == EUNSUP
+    assert bwd(B=1 << 19, H=8, Hk=8, savedb=1 << 62, wsb=1 << 62, **many) == EUNSUP
+    for waves in range((1 << 26) - 3, (1 << 26) + 1):                   # 2^24 workgroups of 256 threads
+        assert step(B=waves, H=1, Hk=1, Dk=8, Dv=8, o=O << 8) == EUNSUP
+    assert step(B=(1 << 26) - 4, H=1, Hk=1, Dk=8, Dv=8, o=V) == EINVAL  # not too many: refused for its output
