@@ -390,13 +390,13 @@ Shape shape_of(int d, int dtype, bool aligned) {
 // and 256 (of 2048 and 512): 37.7, with 8192 and 1024: 40.6, so 34.0; of 4999 x 1031 float32
 // 42.3, 35.2 and 31.5.
 int fwd_groups(int rows, int tpr) {
-    const int rpb = threads_of(tpr) / tpr, most = tpr == 1024 ? 512 : 2048, want = (rows + rpb - 1) / rpb;
+    const int rpb = threads_of(tpr) / tpr, most = tpr == 1024 ? 512 : 2048, want = (rows - 1) / rpb + 1;
     return want < most ? want : most;
 }
 int bwd_groups(int rows, int tpr) {
     const int rpb = tpr == 0 ? 1 : threads_of(tpr) / tpr;
     const int most = tpr == 64 ? 512 : tpr == 256 ? 512 : 256;
-    const int want = (rows + rpb - 1) / rpb;
+    const int want = (rows - 1) / rpb + 1;
     return want < most ? want : most;
 }
 

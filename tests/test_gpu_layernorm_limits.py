@@ -1,0 +1,29 @@
+"""The layer norm at the largest number of rows."""
+import pytest
+import torch
+
+import paper_2212_14052_amd as h3
+
+pytestmark = pytest.mark.gpu
+ROWS = 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("rows", [ROWS, ROWS - 2])
+def test_most_rows(rows):
+    """Two fp16 values a row.  y is off by its rounding (half a step) and a few of float32; dx cancels down to
+    eps's part of it, so only its float32 roundings of terms of size r |dy| count: 16 x 2^-24, and its half step.
+    db sums ones: whole numbers up to 2^20 a thread, exact until the last additions of 512 partial sums."""
+    x = torch.empty(rows, 2, dtype=torch.float16, device="cuda").uniform_(-2, 2)
+    at = torch.cat([torch.arange(1000), torch.randint(0, rows, (5000,)), torch.arange(rows - 1000, rows)]).cuda()
+    y, mean, rstd = h3.layernorm(x)
+    xs = x[at].double()
+    m, r = xs.mean(1), (xs.var(1, unbiased=False) + 1e-5).rsqrt()
+    want = (xs - m[:, None]) * r[:, None]
+    assert ((mean[at] - m).abs() <= 2 ** -22 * xs.abs().amax(1)).all() and ((rstd[at] - r).abs() <= 2 ** -20 * r).all()
+    assert ((y[at].double() - want).abs() <= 2.0 ** -11 + 2.0 ** -20).all()
+    y.fill_(1.0)
+    dx, dw, db = h3.layernorm_bwd(y, x, None, mean, rstd)
+    assert (dx[at].abs() <= 16 * 2.0 ** -24 * r[:, None]).all()      # equal gradients: nothing is left
+    assert ((db.double() - rows).abs() <= 512 * 2.0 ** -24 * rows).all()
+    # h = (x - m) r is odd in the two columns, whose sums of 2^31 such terms are each other's negative
+    assert (dw.double().sum().abs() <= 2.0 ** -10 * rows)
