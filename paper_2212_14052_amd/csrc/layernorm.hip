@@ -163,11 +163,11 @@ __global__ __launch_bounds__(threads_of(TPR)) void layernorm_kernel(
 }
 
 // Rows wider than the registers of a workgroup: x is read for each sum and for
-// the output.
+// the output, which may lie over it (as in the other kernels: no __restrict__).
 template <int DT>
 __global__ __launch_bounds__(1024) void layernorm_wide_kernel(
-    const typename IO<DT>::T *__restrict__ x, const float *__restrict__ w, const float *__restrict__ b, int rows, int d,
-    float eps, typename IO<DT>::T *__restrict__ y, float *__restrict__ mean, float *__restrict__ rstd) {
+    const typename IO<DT>::T *x, const float *__restrict__ w, const float *__restrict__ b, int rows, int d,
+    float eps, typename IO<DT>::T *y, float *__restrict__ mean, float *__restrict__ rstd) {
     __shared__ float lds[16];
     const long row = blockIdx.x;
     const typename IO<DT>::T *xr = x + row * d;
@@ -302,8 +302,8 @@ __global__ __launch_bounds__(threads_of(TPR)) void layernorm_bwd_kernel(
 // The two halves of the backward pass for rows wider than the registers.
 template <int DT>
 __global__ __launch_bounds__(1024) void layernorm_bwd_wide_dx_kernel(
-    const typename IO<DT>::T *__restrict__ dy, const typename IO<DT>::T *__restrict__ x, const float *__restrict__ w,
-    const float *__restrict__ mean, const float *__restrict__ rstd, int rows, int d, typename IO<DT>::T *__restrict__ dx) {
+    const typename IO<DT>::T *dy, const typename IO<DT>::T *x, const float *__restrict__ w,
+    const float *__restrict__ mean, const float *__restrict__ rstd, int rows, int d, typename IO<DT>::T *dx) {
     __shared__ float lds[32];
     const long row = blockIdx.x;
     const float mu = mean[row], r = rstd[row];
