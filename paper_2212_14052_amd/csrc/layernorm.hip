@@ -501,8 +501,8 @@ hipError_t launch_layernorm(const void *x, const float *w, const float *b, int r
     return fwd_of<BF16>(x, w, b, rows, d, eps, y, mean, rstd, s);
 }
 
-// the most groups that any layout of these rows takes
-size_t layernorm_bwd_workspace(int rows, int d) { return (size_t)(rows < 1024 ? rows : 1024) * 2 * d * sizeof(float); }
+// for the most groups that any layout of these rows takes (see bwd_groups)
+size_t layernorm_bwd_workspace(int rows, int d) { return (size_t)(rows < 512 ? rows : 512) * 2 * d * sizeof(float); }
 
 hipError_t launch_layernorm_bwd(const void *dy, const void *x, const float *w, const float *mean, const float *rstd,
                                 int rows, int d, int dtype, void *dx, float *dw, float *db, float *ws, hipStream_t s) {

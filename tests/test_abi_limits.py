@@ -15,3 +15,9 @@ def test_launches_of_less_than_2_to_32_threads():
     for waves in range((1 << 26) - 3, (1 << 26) + 1):                   # 2^24 workgroups of 256 threads
         assert step(B=waves, H=1, Hk=1, Dk=8, Dv=8, o=O << 8) == EUNSUP
     assert step(B=(1 << 26) - 4, H=1, Hk=1, Dk=8, Dv=8, o=V) == EINVAL  # not too many: refused for its output
+
+
+def test_workspace_of_the_norm():
+    """A partial row of dw and one of db for each of at most 512 workgroups."""
+    for rows in (1, 511, 512, 513, 1 << 20):
+        assert size(h3.OP_LAYERNORM_BWD, B=rows, H=768) == min(rows, 512) * 2 * 768 * 4
