@@ -172,7 +172,14 @@ def _gpu(name: str, t: torch.Tensor) -> torch.device:
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor (got {t.device})")
+    _sizes(name, t)
     return t.device
+
+
+def _sizes(name: str, t: torch.Tensor):
+    """The C entries take sizes as ints, and ctypes passes a larger one on without its upper bits."""
+    if t.numel() > 2 ** 31 - 1 and max(t.shape) > 2 ** 31 - 1:
+        raise ValueError(f"{name}: sizes are at most 2^31 - 1 (got {tuple(t.shape)})")
 
 
 def _on(dev: torch.device, **ts):
@@ -560,6 +567,7 @@ def _delta_args(q, k, v, g, beta):
     dev = _gpu("q", q)
     if not _all_on(dev.index, k, v, g, beta):
         _on(dev, k=k, v=v, g=g, beta=beta)
+    _sizes("v", v)
     qs, vs = q.shape, v.shape
     if len(qs) != 4 or len(vs) != 4:
         raise ValueError("q must be (B, L, Hk, Dk) and v (B, L, H, Dv)")

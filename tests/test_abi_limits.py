@@ -1,4 +1,7 @@
 """The largest calls that the layer norm and the delta rule take, and what is refused beyond (no GPU needed)."""
+import pytest
+import torch
+
 import paper_2212_14052_amd as h3
 from tests.test_abi_mixers import EINVAL, EUNSUP, O, V, bwd, rule, size, step
 
@@ -21,3 +24,13 @@ def test_workspace_of_the_norm():
     """A partial row of dw and one of db for each of at most 512 workgroups."""
     for rows in (1, 511, 512, 513, 1 << 20):
         assert size(h3.OP_LAYERNORM_BWD, B=rows, H=768) == min(rows, 512) * 2 * 768 * 4
+
+
+def test_sizes_beyond_an_int():
+    """A size of 2^32 + 8 would reach the C entry as 8."""
+    one = torch.empty(1, dtype=torch.float16)
+    for shape in ((1, 2 ** 32 + 8), (2 ** 31, 1), (1, 2 ** 32 + 64, 1, 8), (1, 1, 2 ** 32 + 1, 8)):
+        with pytest.raises(ValueError):
+            h3._sizes("x", one.expand(shape))
+    for shape in ((), (0,), (0, 2 ** 31 - 1), (2 ** 31 - 1, 2 ** 20)):
+        h3._sizes("x", one.reshape(()) if shape == () else one.expand(shape))

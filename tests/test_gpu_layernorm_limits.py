@@ -27,3 +27,14 @@ def test_most_rows(rows):
     assert ((db.double() - rows).abs() <= 512 * 2.0 ** -24 * rows).all()
     # h = (x - m) r is odd in the two columns, whose sums of 2^31 such terms are each other's negative
     assert (dw.double().sum().abs() <= 2.0 ** -10 * rows)
+
+
+def test_row_beyond_an_int():
+    x = torch.empty(1, 2 ** 32 + 8, dtype=torch.float16, device="cuda")
+    with pytest.raises(ValueError):
+        h3.layernorm(x)
+    with pytest.raises(ValueError):
+        h3.layernorm_bwd(x, x, None, x[:, 0].float(), x[:, 0].float())
+    q = x.view(-1)[:2 ** 32].view(1, 2 ** 32, 1, 1)   # the sizes are looked at first
+    with pytest.raises(ValueError):
+        h3.delta_step(q, q, q, q[..., 0], q[..., 0], q)
