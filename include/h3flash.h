@@ -334,9 +334,11 @@ int h3_delta_step(const void *q, const void *k, const void *v, const float *g, c
  *   Dk, Dv, Hk as for h3_delta_step; any L >= 1.  Other than S_final and S0
  *   nothing that is written overlaps anything.
  * States, gates and sums are float32, differences of summed log decays
- * float64; a NaN or Inf may reach every token of its chunk of 64.  Where no token
- * stretches the state (g <= 0, 0 <= beta |k|^2 <= 2) a chunk is off by a few 2^-22 of the state's size;
+ * float64; a NaN or Inf may reach every token of its chunk of 64, in v or S0 of its own column.  Where no token
+ * stretches the state (g <= 0, 0 <= beta |k|^2 <= 2) a chunk is off by a few 2^-22 of the size of a state's column;
  * where tokens do, a chunk's solved matrix grows with what its 64 tokens stretch, and its errors with it.
+ * float32 keys and queries less than 2^-16 of their chunk's largest count with fewer bits than 22, below 2^-38 with none;
+ * bf16 ones are exact down to 2^-31 of it, fp16 ones always.
  * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, H Dv > 2^22, 2^32 threads a launch: from B H ceil(L / 64) of
  * 2^23 (2^24 where Dk <= 64), or B H ceil(Dv / 64) of 2^24, on), EWORKSPACE, EDEVICE.
  */

@@ -17,10 +17,10 @@
 // in the registers, the right operand of the next.  The waves of a workgroup share
 // the chunk's keys and queries in LDS, fetched one chunk ahead.
 //
-// At 8 sequences of 2048 tokens, 6 heads of 128 x 128, fp16: chunks 34 us (150 MB through
-// memory, 4.4 TB/s), scan 119: 32 chunks after one another at 3.7 us, whose 140 matrix instructions of a
-// wave would take 1.1.  What is left is the chain inside a chunk: K S, then R, its largest value,
-// X R, the errors' largest value, P u and the new state, each waiting for the one before, and
+// At 8 sequences of 2048 tokens, 6 heads of 128 x 128, fp16: chunks 33 us (141 MB through
+// memory, 4.2 TB/s), scan 112: 32 chunks after one another at 3.5 us, whose 132 matrix instructions of a
+// wave would take 0.9.  What is left is the chain inside a chunk: K S, then R, its largest values,
+// X R, the errors' largest values, P u and the new state, each waiting for the one before, and
 // the vector instructions between them.
 #include <math.h>
 
@@ -300,7 +300,8 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
 // What the backward pass reads is stored between the last products, and past the caches: a CU takes
 // 1 KB of stores or copies every 16 cycles, and a wave waits where it asks for many at once, as for
 // the state at a chunk's start, behind the next chunk's copies (both kernels for 4 x 2048
-// tokens of 20 heads of 128 bf16: 244 us so, 234 past the caches, 204 as it is; 166 with nothing kept).
+// tokens of 20 heads of 128 bf16: 213 us as it is, 165 with nothing kept; with P and u in one piece 204, then 234 at a
+// chunk's start past the caches, and 244 through them).
 //
 // Sequences may be cut into segments (see DeltaSegments).  In mode MAP a workgroup
 // does not produce outputs but its segment's map from state to state.
@@ -572,8 +573,8 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
 // The state in front of every segment from the segments' maps, in order (or the
 // gradient of the state behind each, in reverse): S <- F S + D.  A workgroup takes 16
 // columns, its four waves share the rows: each holds its part of the next map while
-// the states go round through LDS.  Bound by latency: 11 steps of 20 heads of 128 x 128 take 55 us,
-// a load, a product and two barriers each, against 250 for the scan that they let run at once.
+// the states go round through LDS.  Bound by latency: 11 steps of 20 heads of 128 x 128 take 51 us,
+// a load, a product and two barriers each, against 274 for the scan that they let run at once.
 template <int KS>
 __global__ __launch_bounds__(256, 1) void delta_join_kernel(DeltaArgs a, DeltaSegments sg, const float *__restrict__ S0, bool back) {
     constexpr int TW = (KS + 1) / 2;   // row tiles a wave
@@ -655,9 +656,12 @@ __global__ __launch_bounds__(256, 1) void delta_join_kernel(DeltaArgs a, DeltaSe
 
 }  // namespace
 
-// How a launch's scans are cut.  32768 tokens of 20 heads of 128 bf16 take 671 us in the 12
-// segments of eight waves that this gives, 1820 uncut, 765 with four waves, 1285 in four segments; 8 x 2048
-// tokens of 6 heads fp16 take 152 uncut with four waves, 192 with eight, 185 in four segments.
+// How a launch's scans are cut.  32768 tokens of 20 heads of 128 bf16 take 743 us in the 12
+// segments of eight waves that this gives, 1920 uncut, 800 with four waves, 1355 in four segments, 817 in 24; 8 x 2048
+// tokens of 6 heads fp16 take 139 uncut with four waves, 182 with eight, 176 in four segments.  Heads of
+// 8 x 8 to 128 x 256, fp16 and float32, 1536 to 32768 tokens of 2 to 512 heads (52 shapes), against the best of 1, 2, 4, 8, 16 and 32 segments
+// of four and of eight waves: at worst 1.17 times it, where a chunk of narrow heads takes less than the units
+// assumed and more segments would do (4096 tokens of 4 heads of 8 x 8 float32: 62 us, 53 in 16 segments, 151 uncut).
 // A workgroup of four waves takes about one time
 // unit (4 us) a chunk on a CU of its own, one of eight 1.5; two workgroups of eight that form
 // maps share a CU and take kMaps; joining takes about 1.3 units a segment.

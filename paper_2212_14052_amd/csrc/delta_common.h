@@ -7,11 +7,12 @@
 // pieces, the rounding and the rounding of what it leaves: 22 bits; of the four products
 // of pieces the smallest (2^-22 at most) is left out.  fp16 inputs are one piece
 // as they are.  Everything else is scaled by a power of two that takes the
-// largest value of its tile to 2^13 .. 2^14, so that nothing overflows and what
+// largest value that shares it to 2^13 .. 2^14, so that nothing overflows and what
 // fp16 cannot hold is below 2^-38 of that largest value; bf16 inputs are then one
 // exact piece (down to 2^-31 of the largest).  Exponents are kept as integers
-// and undone in float32.  (Three bf16 pieces, which need no scales, cost 182
-// matrix instructions a chunk of 16 columns where these cost 104 to 132.)
+// and undone in float32.  Each column of a state has its own; keys and queries have one for a
+// chunk, triangular matrices one each.  (Three bf16 pieces, which need no scales, cost 182
+// matrix instructions a chunk of 16 columns where these cost 132.)
 #pragma once
 #include "common.h"
 #include "internal.h"

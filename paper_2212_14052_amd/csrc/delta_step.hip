@@ -10,7 +10,8 @@
 // the T tokens, the next token's inputs are fetched while one is worked on: each call
 // reads and writes the state once and is bound by HBM, or by latency where there are few heads.
 // 64 sequences of 20 heads of 128 x 128 bf16, one token: 30.0 us, 5.6 TB/s.  One sequence of 6 heads:
-// 7.9 us of the kernel, less than the call on the host.
+// 7 to 8 us of the kernel, less than the call on the host (10).  19 sequences of 5 tokens, 12 heads of 64 x 96: 10 us
+// of the kernel, which asks for a token's inputs only one token ahead, as long as the call.
 #include "common.h"
 #include "internal.h"
 

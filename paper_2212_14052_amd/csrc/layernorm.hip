@@ -21,7 +21,8 @@
 //
 // Forward at 8192 x 2560 bf16: 16.9 us, 4.97 TB/s, what a large copy reaches (4.99).
 // At 16384 x 768 fp16: forward 8.4 us (6.0 TB/s: part of it stays in the last cache),
-// backward 19.8, the second kernel 6.2.
+// backward 19.8, the second kernel 6.2 (3 MB by 48 workgroups, which is few).  At 4999 x 1031 float32: forward 11,
+// backward 16.3, the second kernel 6.4; rows that do not start on 16 bytes are read 4 bytes at a time.
 #include <type_traits>
 
 #include "common.h"
