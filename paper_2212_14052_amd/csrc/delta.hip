@@ -78,17 +78,7 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
         gf->from0[lane] = f;
         gf->toend[lane] = e;
         gf->beta[lane] = bt;
-        // 2^et and 2^ef take every exp(G_63 - G_i) and exp(G_i) to at most 2
-        const int et = scale_exp(group_max<64>(__float_as_uint(e))) + 13, ef = scale_exp(group_max<64>(__float_as_uint(f))) + 13;
-        if (lane == 0) {
-            gf->et = et;
-            gf->ef = ef;
-        }
         if (back) {
-            if (lane == 0) {
-                gb->et = et;
-                gb->ef = ef;
-            }
             gb->from0[lane] = f;
             gb->toend[lane] = e;
             gb->beta[lane] = bt;
@@ -353,8 +343,7 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
         const ChunkGates *gt = (const ChunkGates *)(at + Lds::gates);
         dl_f4 *kept = (dl_f4 *)states + (ch * delta_col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;   // where this state is left
         const int ek = __builtin_amdgcn_readfirstlane(gt->ek), eq = __builtin_amdgcn_readfirstlane(gt->eq),
-                  ex = __builtin_amdgcn_readfirstlane(gt->ex), ep = __builtin_amdgcn_readfirstlane(gt->ep),
-                  et = __builtin_amdgcn_readfirstlane(gt->et);
+                  ex = __builtin_amdgcn_readfirstlane(gt->ex), ep = __builtin_amdgcn_readfirstlane(gt->ep);
         // K S and, transposed (rows are columns of S, so that a lane will hold four
         // consecutive values of one token), Q S
         dl_f4 R[4], u[4], x[4];
@@ -493,17 +482,17 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
                     else *(uint2 *)op = make_uint2(pack_16x2<DT>(x[t][0], x[t][1]), pack_16x2<DT>(x[t][2], x[t][3]));
                 }
         }
-        // S <- exp(G_63) S + K^T (exp(G_63 - G) u), in units of the keys' times the errors' scale;
-        // of 2^-60 of S where the errors are smaller than that
-        const int En = max(ek + eu + et, max(eS - 60, E - 100)), ew = En - ek;
-        const float fs = fl * pow2(max(E - En, -126)), sw = pow2(max(min(-ew, 127), -126));
+        // S <- exp(G_63) S + K^T w, w = exp(G_63 - G) u, in units of the keys' times w's scale (w's own: where the
+        // chunk decays, its largest value is far below that of u); of 2^-60 of exp(G_63) S where w is smaller than that
+#pragma unroll
+        for (int t = 0; t < 4; ++t) te[t] *= u[t];
+        const int En = max(ek + col_exp(te), max(eS - 60, E - 100) + floor_exp(fl));
+        const float fs = __builtin_amdgcn_ldexpf(fl, E - En), sw = pow2(max(min(ek - En, 127), -126));
         const int Eo = E;
         E = En;
         Op<2> wo[2];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) te[t] *= sw;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) wo[s] = split8<2>(u[2 * s], u[2 * s + 1], te[2 * s], te[2 * s + 1]);
+        for (int s = 0; s < 2; ++s) wo[s] = split8<2>(te[2 * s], te[2 * s + 1], sw);
         dl_f4 y[2][TG];   // summed from zero: added to S step by step, each step would round it
         auto add = [&](int q) {
 #pragma unroll

@@ -61,8 +61,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
         const int nt = min(DC, len - n * DC);
         dl_f4 *kept = (dl_f4 *)d.dends + (ch * delta_col_tiles(a.Dv, 1) + c0 / 16) * 2 * KS * 64 + lane;   // where this state is left
         const int ek = __builtin_amdgcn_readfirstlane(gt->ek), eq = __builtin_amdgcn_readfirstlane(gt->eq),
-                  ex = __builtin_amdgcn_readfirstlane(gt->ex), ep = __builtin_amdgcn_readfirstlane(gt->ep),
-                  ef = __builtin_amdgcn_readfirstlane(gt->ef);
+                  ex = __builtin_amdgcn_readfirstlane(gt->ex), ep = __builtin_amdgcn_readfirstlane(gt->ep);
         // du = t (K dS') + P^T do
         dl_f4 u[4], dd[4], te[4], be[4];
         Op<NM> pf[6], xf[6];
@@ -168,28 +167,27 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void delta_bwd_scan_kernel(DeltaAr
                 for (int r = 0; r < 4; ++r) y[t][r] = be[t][r] * z[r];
             }
         }
-        const int ez = max(col_exp(y), kLeast), esc = scale_exp(mag(a.scale)) + 13;   // 2^esc: at most the scale
+        const int ez = max(col_exp(y), kLeast);
         if constexpr (!MAPS) {
             const int4 e = make_int4(tile_exp(ez), tile_exp(kept_exp(e0, E)), tile_exp(ed), 0);
             if (lane == 0) d.exps[ch * kDeltaTiles + c0 / 16] = e;
         }
-        // dS <- exp(G_63) dS' + Q^T (f do) - K^T (f y), both in units of the larger one's scale; of
-        // 2^-60 of dS' where both are smaller than that
-        const int En = max(max(ek + ez + ef, eq + ed + ef + esc + 1), max(eS - 60, E - 100));
-        const float fs = fl * pow2(max(E - En, -126)), sy = pow2(max(min(ek - En, 127), -126)), so_ = pow2(max(min(eq - En, 127), -126));
+        // dS <- exp(G_63) dS' + Q^T (f do) - K^T (f y), both in units of the larger product's scale; of
+        // 2^-60 of exp(G_63) dS' where both are smaller than that
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            y[t] *= f0[t];
+            dd[t] *= f0[t] * a.scale;
+        }
+        const int En = max(max(ek + col_exp(y), eq + col_exp(dd)), max(eS - 60, E - 100) + floor_exp(fl));
+        const float fs = __builtin_amdgcn_ldexpf(fl, E - En), sy = -pow2(max(min(ek - En, 127), -126)), so_ = pow2(max(min(eq - En, 127), -126));
         const int Eo = E;
         E = En;
         Op<2> yo[2], qo[2];
-        dl_f4 fy[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            fy[t] = f0[t] * -sy;
-            f0[t] *= a.scale * so_;
-        }
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            yo[s] = split8<2>(y[2 * s], y[2 * s + 1], fy[2 * s], fy[2 * s + 1]);
-            qo[s] = split8<2>(dd[2 * s], dd[2 * s + 1], f0[2 * s], f0[2 * s + 1]);
+            yo[s] = split8<2>(y[2 * s], y[2 * s + 1], sy);
+            qo[s] = split8<2>(dd[2 * s], dd[2 * s + 1], so_);
         }
         dl_f4 x[2][2];
         auto add = [&](int q) {

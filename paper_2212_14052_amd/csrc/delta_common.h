@@ -91,19 +91,6 @@ template <int N> __device__ __forceinline__ Op<N> split8(dl_f4 a, dl_f4 b, float
     return split8<N>(x, s);
 }
 
-// each row times its own factor
-template <int N> __device__ __forceinline__ Op<N> split8(dl_f4 a, dl_f4 b, dl_f4 s, dl_f4 t) {
-    Op<N> o;
-    uint32_t w[4][N];
-    split2<N>(a[0], s[0], a[1], s[1], w[0]);
-    split2<N>(a[2], s[2], a[3], s[3], w[1]);
-    split2<N>(b[0], t[0], b[1], t[1], w[2]);
-    split2<N>(b[2], t[2], b[3], t[3], w[3]);
-#pragma unroll
-    for (int n = 0; n < N; ++n) o.p[n] = make_uint4(w[0][n], w[1][n], w[2][n], w[3][n]);
-    return o;
-}
-
 // -------------------------------------------------------------- scales -----
 // The exponent e with largest 2^-e in 2^13 .. 2^14, from the largest magnitude's
 // bits; 0 for Inf and NaN, -126 where 2^-e would leave float32 and for zero: a tile of
@@ -119,6 +106,8 @@ __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)
 // (of a value of 2^-67 or less fewer bits go in).
 constexpr int kLeast = -80;
 __device__ __forceinline__ float pow2_sum(int e) { return e < -126 ? 0.f : pow2(e > 127 ? 127 : e); }
+// e with 2^e <= x < 2^(e + 1); -127 for zero
+__device__ __forceinline__ int floor_exp(float x) { return (int)((__float_as_uint(x) >> 23) & 255u) - 127; }
 // what the backward pass is told of a state: its exponent e in the registers and E of the registers
 __device__ __forceinline__ int kept_exp(int e, int E) { return e <= -126 ? -126 : max(min(max(e, kLeast) + E, 114), -126); }
 __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }

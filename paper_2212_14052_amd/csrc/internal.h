@@ -184,11 +184,10 @@ struct DeltaArgs {
 };
 // What a chunk keeps beside its matrices: exp(G_i) from the chunk's start,
 // exp(G_63 - G_i) to its end, beta_i (0 behind the sequence's end); the exponents
-// of the scales of keys, queries, X and P; 2^et and 2^ef: at least half the largest
-// exp(G_63 - G_i) and exp(G_i).
+// of the scales of keys, queries, X and P.
 struct ChunkGates {
     float from0[kDeltaChunk], toend[kDeltaChunk], beta[kDeltaChunk];
-    int ek, eq, ex, ep, et, ef, unused[2];
+    int ek, eq, ex, ep, unused[4];
 };
 // Buffers of the chunks of every (b, h).  rec: what a scan of the chunks reads
 // of each, kDeltaRecBytes: operand fragments of X and P (64 x 64, two fp16 pieces each),

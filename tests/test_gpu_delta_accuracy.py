@@ -110,3 +110,19 @@ def test_columns_do_not_meet(B, L, H, Hk, Dk, Dv, dtype):
         assert not S2[..., 3].isfinite().any()
         gr2 = grads_of(q, k, v, g, beta, S0, do2, dS)
         assert torch.equal(gr2[2][..., rest], gr[2][..., rest]) and torch.equal(gr2[5][..., rest], gr[5][..., rest])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,L,H,Hk,Dk,Dv", [(2, 120, 2, 2, 128, 128), (1, 190, 4, 2, 64, 40), (16, 128, 16, 16, 128, 128)])
+def test_writes_that_fade(B, L, H, Hk, Dk, Dv, dtype):
+    """The last chunk is written to by its first token alone and then decays by up to 2^-45: what is left of that keeps its bits.
+    A chunk's roundings of operands and sums, 2^-21, and of its decay: float32 holds the logarithm's sum G by |G| 2^-24, or
+    twice that with the change to base 2."""
+    q, k, v, g, beta, S0, do, dS = full_inputs(B, L, H, Hk, Dk, Dv, dtype, 25)
+    last = (L - 1) // 64 * 64
+    g.fill_(-0.5)
+    beta[:, last + 1:] = 0.0
+    beta[:, :last] = 0.0
+    rS = reference(q, k, v, g, beta, None, 1.0)[1]
+    S = h3.delta_rule(q, k, v, g, beta)[1]
+    assert (S.double() - rS).norm() <= (2.0 ** -21 + 2 * 32 * 2.0 ** -24) * rS.norm()
