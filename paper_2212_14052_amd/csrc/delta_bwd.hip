@@ -11,9 +11,13 @@
 // (delta_bwd_chunk_kernel), with
 //     D = lower part of (do u^T) exp(G_i - G_j),  E = -(strictly lower part of (y u^T) exp(G_i - G_j)):
 //     dq = f (do S^T) + D K,   dk = reads + writes,  reads = E K - f (y S^T),
-//     writes = D^T Q + E^T K + t (u dS'^T),   dbeta_i = z_i . e_i,
-//     dG_i = q_i . dq_i + k_i . (reads_i - writes_i),   dg_t = sum_{i >= t} dG_i + <S', dS'>,
-// where <S', dS'> = exp(G_63) <S, dS'> + sum_i k_i . t_i (u dS'^T)_i.
+//     writes = D^T Q + E^T K + t (u dS'^T),   dbeta_i = z_i . e_i.
+// The decay of token t lies in what passes from a token j < t to a token i >= t, M_ij = D_ij q_i . k_j + E_ij k_i . k_j, in
+// what tokens i >= t read of S, in what tokens j < t leave to S', and in what S leaves to it:
+//     dg_t = sum_{i >= t > j} M_ij + sum_{i >= t} (q_i . f_i (do S^T)_i - k_i . f_i (y S^T)_i)
+//          + sum_{j < t} k_j . t_j (u dS'^T)_j + exp(G_63) <S, dS'>.
+// Every term has token t's decay in it (the difference of the sums of q . dq and k . dk does not, and is rounding alone
+// where gates are nearly closed: off by 1e-3 of dg at decays of exp(-5) to exp(-60), all of it where the last tokens only have gradients).
 #include "delta_common.h"
 
 namespace h3 {
@@ -261,8 +265,8 @@ template <int DT, int KS> struct GradLds {
     static constexpr int S = 0, dS = S + 4 * KS * 64, y = dS + 4 * KS * 64, u = y + 8 * 64, o = u + 8 * 64, stage = o + NT * 4 * 64;
     static constexpr int kq = kq_words<KS>(NT), k = 0, q = kq, D = 2 * kq, E = D + kq_words<2>(2), after = E + kq_words<2>(2);
     static constexpr int rest = stage > after ? stage : after;
-    static constexpr int gd = rest, gates = gd + DC / 2, red = gates + GATES, dot = red + NW * DC / 4, rin = dot + DC / 4, big = rin + NW / 2,
-                         total = (big + 2) * 16;
+    static constexpr int gd = rest, gates = gd + DC / 2, red = gates + GATES, dot = red + 2 * NW * DC / 4, rin = dot + DC / 4, big = rin + NW / 2,
+                         below = big + 2, across = below + 2 * DC / 4, total = (across + 2 * 4 * DC / 4) * 16;
     static_assert(total <= 160 * 1024, "LDS of a CU");
 };
 
@@ -289,9 +293,11 @@ __global__ __launch_bounds__(64 * grad_waves<KS>, (KS > 2 || ONE ? 2 : 1)) void 
     extern __shared__ uint4 lds[];
     double *gd = (double *)(lds + Lds::gd);
     ChunkGates *gt = (ChunkGates *)(lds + Lds::gates);
-    float *red = (float *)(lds + Lds::red);        // the waves' sums of dG
+    float *red = (float *)(lds + Lds::red);        // the waves' sums of what tokens read of S; of what they leave to S'
     float *dots = (float *)(lds + Lds::dot);       // z . e over the later columns
-    double *rin = (double *)(lds + Lds::rin);      // and of <S', dS'>
+    double *rin = (double *)(lds + Lds::rin);      // the waves' sums of <S, dS'>
+    float *below = (float *)(lds + Lds::below);    // of D and of E: sums of M over j < t and i >= t in t's row tile
+    float *across = (float *)(lds + Lds::across);  // of D and of E, a row tile: its rows' sums for every column left of it
     uint32_t *big = (uint32_t *)(lds + Lds::big);  // the waves' largest magnitudes of D and of E
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4, c16 = lane & 15;
     const int wt = w & 3, half = w >> 2;   // token tile; which columns of 32, which of D and E
@@ -535,8 +541,44 @@ __global__ __launch_bounds__(64 * grad_waves<KS>, (KS > 2 || ONE ? 2 : 1)) void 
                 for (int i = 0; i < 2; ++i) to[kq_block<2>(i, j, 0) * 128] = make_uint2(x[0][i], x[1][i]);
             }
         }
-        float kx = 0.f;   // sum of k . t (u dS'^T)
         __syncthreads();  // D and E are there
+        // M's row tile wt, from D and E as they are in the registers
+        {
+            float T[4] = {0.f, 0.f, 0.f, 0.f}, A[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int m = 0; m < NI; ++m) {
+                const bool of_d = NW == 4 ? m == 0 : half == 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (j > wt) continue;
+                    dl_f4 p = {0.f, 0.f, 0.f, 0.f}, y = p;
+#pragma unroll
+                    for (int s = 0; s < KS; ++s)
+                        p = mm(lds_rows<NT, KS>(of_d ? qs : ks, wt, s, lane), lds_rows<NT, KS>(ks, j, s, lane), p);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        p[r] = ad[m][j][r] * __builtin_amdgcn_ldexpf(p[r], ek + (of_d ? eq : ek));
+                        if (j == wt) p[r] = 4 * g4 + r > c16 ? p[r] : 0.f;
+                    }
+                    // rows t: the sums over rows i >= t of the tile
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) y = __builtin_amdgcn_mfma_f32_16x16x4f32(4 * g4 + s >= c16 ? 1.f : 0.f, p[s], y, 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) T[r] += j < wt || c16 < 4 * g4 + r ? y[r] : 0.f;
+                    A[j] += y[0];
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int m = 1; m < 16; m *= 2) T[r] += __shfl_xor(T[r], m);
+            float *b = below + (NW == 4 ? 0 : half) * DC, *a = across + (NW == 4 ? 0 : half) * 4 * DC + wt * DC;
+            if (c16 == 0) *(dl_f4 *)(b + 16 * wt + 4 * g4) = dl_f4{T[0], T[1], T[2], T[3]};
+            if (g4 == 0)
+#pragma unroll
+                for (int j = 0; j < 3; ++j)
+                    if (j < wt) a[16 * j + c16] = A[j];
+        }
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             __builtin_amdgcn_sched_barrier(0);   // a token tile's operands at a time: the registers
@@ -564,7 +606,7 @@ __global__ __launch_bounds__(64 * grad_waves<KS>, (KS > 2 || ONE ? 2 : 1)) void 
                     ec[s] = column(Es, s);
                 }
             }
-            float dG = 0.f;
+            float rs = 0.f, ws = 0.f;
             const int ct = w;   // this wave's channel tile
             if (ct < 2 * KS) {
                 float kv[4] = {0.f, 0.f, 0.f, 0.f}, qv[4] = {0.f, 0.f, 0.f, 0.f};
@@ -583,7 +625,8 @@ __global__ __launch_bounds__(64 * grad_waves<KS>, (KS > 2 || ONE ? 2 : 1)) void 
                     dq[t][r] = __builtin_amdgcn_ldexpf(dq[t][r], eS + eo) * (f * a.scale);
                     kr[t][r] = __builtin_amdgcn_ldexpf(kr[t][r], eS + ey) * -f;
                     kw[t][r] = __builtin_amdgcn_ldexpf(kw[t][r], eE + eu) * e;
-                    kx += kv[r] * kw[t][r];
+                    rs += qv[r] * dq[t][r] + kv[r] * kr[t][r];
+                    ws += kv[r] * kw[t][r];
                 }
                 dl_f4 p = {0.f, 0.f, 0.f, 0.f}, q = p, x = p, y = p;
 #pragma unroll
@@ -605,10 +648,7 @@ __global__ __launch_bounds__(64 * grad_waves<KS>, (KS > 2 || ONE ? 2 : 1)) void 
                     kw[t][r] += __builtin_amdgcn_ldexpf(x[r], eq + eD) + __builtin_amdgcn_ldexpf(y[r], ek + eF);
                 }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    dG += qv[r] * dq[t][r] + kv[r] * (kr[t][r] - kw[t][r]);
-                    kr[t][r] += kw[t][r];
-                }
+                for (int r = 0; r < 4; ++r) kr[t][r] += kw[t][r];
                 if constexpr (ONE) {
                     store(t, dq[t], kr[t]);
                 } else {
@@ -616,30 +656,44 @@ __global__ __launch_bounds__(64 * grad_waves<KS>, (KS > 2 || ONE ? 2 : 1)) void 
                     tk[t] += kr[t];
                 }
             }
-            dG += __shfl_xor(dG, 16);
-            dG += __shfl_xor(dG, 32);
-            if (g4 == 0) red[w * DC + row] = dG;
+            rs += __shfl_xor(rs, 16);
+            ws += __shfl_xor(ws, 16);
+            rs += __shfl_xor(rs, 32);
+            ws += __shfl_xor(ws, 32);
+            if (g4 == 0) {
+                red[w * DC + row] = rs;
+                red[(NW + w) * DC + row] = ws;
+            }
         }
-        in64 += kx;
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) in64 += __shfl_xor(in64, m);
         if (lane == 0) rin[w] = in64;
         __syncthreads();
         if (w == 0) {
-            // suffix sums in float64: many terms, of both signs
-            double x = 0.0, y = 0.0;
+            // Sums over the lanes up to this one, token t = lane: of reads from the last token on, of what the tokens
+            // before t leave, and of the rows below each row tile over the columns before t.
+            const int tile = lane >> 4, j = max(lane - 1, 0);   // column: the token before
+            float x = 0.f, y = 0.f, left[3] = {0.f, 0.f, 0.f};
+            double c = 0.0;
 #pragma unroll
             for (int i = 0; i < NW; ++i) {
-                x += (double)red[i * DC + lane];
-                y += rin[i];
+                x += red[i * DC + 63 - lane];
+                y += red[(NW + i) * DC + j];
+                c += rin[i];
             }
 #pragma unroll
-            for (int m = 1; m < 64; m *= 2) {
-                const double z = __shfl_down(x, m);
-                if (lane + m < 64) x += z;
+            for (int i = 0; i < NW / 4; ++i) {
+                c += (double)below[i * DC + lane];
+#pragma unroll
+                for (int t = 0; t < 3; ++t)
+#pragma unroll
+                    for (int q = t + 1; q < 4; ++q) left[t] += j >> 4 <= t ? across[(4 * i + q) * DC + j] : 0.f;
             }
-            x += y;
-            if (lane < room) d.dg[(tok0 + lane) * a.H + h] = lane < nt ? (float)x : 0.f;
+#pragma unroll
+            for (int t = 0; t < 3; ++t) left[t] = lane_sums(lane > 0 ? left[t] : 0.f);
+            c += __shfl(lane_sums(x), 63 - lane) + lane_sums(lane > 0 ? y : 0.f);
+            c += tile == 0 ? left[0] : tile == 1 ? left[1] : tile == 2 ? left[2] : 0.f;
+            if (lane < room) d.dg[(tok0 + lane) * a.H + h] = lane < nt ? (float)c : 0.f;
         }
     }
     if (ONE && nt > 0) return;

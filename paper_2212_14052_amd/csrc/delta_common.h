@@ -290,6 +290,20 @@ __device__ __forceinline__ dl_f4 lds_column4(const typename IO<DT>::T *m, int ro
     return v;
 }
 
+// the sum of x over the lanes up to and with this one, on the vector unit
+template <int CTRL, int ROWS> __device__ __forceinline__ float from_lane(float x) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float lane_sums(float x) {
+    x += from_lane<0x111, 0xf>(x);   // row_shr:1, 2, 4, 8
+    x += from_lane<0x112, 0xf>(x);
+    x += from_lane<0x114, 0xf>(x);
+    x += from_lane<0x118, 0xf>(x);
+    x += from_lane<0x142, 0xa>(x);   // lane 15 of rows 0 and 2 to the rows behind them
+    x += from_lane<0x143, 0xc>(x);   // lane 31 to rows 2 and 3
+    return x;
+}
+
 // ------------------------------------------------------- a chunk's decays ---
 constexpr double kLog2e = 1.4426950408889634073599246810018921;
 // a log decay below this is an exact zero in float32 whatever it is (also -inf,

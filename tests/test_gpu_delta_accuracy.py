@@ -126,3 +126,40 @@ def test_writes_that_fade(B, L, H, Hk, Dk, Dv, dtype):
     rS = reference(q, k, v, g, beta, None, 1.0)[1]
     S = h3.delta_rule(q, k, v, g, beta)[1]
     assert (S.double() - rS).norm() <= (2.0 ** -21 + 2 * 32 * 2.0 ** -24) * rS.norm()
+
+
+@pytest.mark.parametrize("late", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,L,H,Hk,Dk,Dv", [(6, 150, 4, 4, 128, 128), (12, 130, 4, 2, 64, 40), (8, 100, 6, 2, 96, 72), (12, 70, 4, 4, 24, 16),
+                                            (8, 64, 6, 3, 128, 24)])
+def test_gradient_of_strong_decays(B, L, H, Hk, Dk, Dv, dtype, late):
+    """Decays of exp(-5) to exp(-60) a token, whose gradients have that factor; all outputs have gradients, or (late) the last
+    five only.  Every term of dg is a product of up to five operands of 2^-22 of the largest, at most eight times
+    the usual size (5 x 2^-19), times a decay with an error of 87 x 2^-24: under 2^-16 of a token's gradients over all heads."""
+    q, k, v, g, beta, S0, do, dS = full_inputs(B, L, H, Hk, Dk, Dv, dtype, 27)
+    gen = torch.Generator().manual_seed(28)
+    g = -torch.empty(B, L, H).uniform_(5, 60, generator=gen).cuda()
+    if late:
+        do[:, :L - 5] = 0.0
+        dS = None
+    ref = reverse(q, k, v, g, beta, S0, do, dS, Dk ** -0.5)[0][3]
+    dg = grads_of(q, k, v, g, beta, S0, do, dS)[3]
+    far, size = (dg.double() - ref).norm(dim=(0, 2)), ref.norm(dim=(0, 2))
+    # Pieces hold 22 bits of what is at least 2^-16 of the largest that shares their scale (2^13 .. 2^14 of fp16, whose
+    # second piece ends at 2^-24: 2^-3 is the least value with 22 bits), which the z of a token that only faded gradients reach is
+    # not: nothing is promised of tokens whose gradients are smaller than that.
+    seen = size >= 2.0 ** -16 * size.max()
+    assert (far <= 2.0 ** -16 * size)[seen].all(), (far / size)[seen].max().item()
+    assert (dg.double() - ref).norm() <= 2.0 ** -18 * ref.norm()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_gradient_of_a_dropped_state(dtype):
+    """Nothing passes a decay of -inf: its gradient is 0, and those around it are what they are for -1e30."""
+    q, k, v, g, beta, S0, do, dS = full_inputs(2, 150, 4, 2, 64, 64, dtype, 29)
+    at = [0, 10, 63, 64, 100, 149]
+    g[:, at] = -float("inf")
+    got = grads_of(q, k, v, g, beta, S0, do, dS)
+    assert (got[3][:, at] == 0).all()
+    g[:, at] = -1e30
+    assert all(torch.equal(a, b) for a, b in zip(got, grads_of(q, k, v, g, beta, S0, do, dS)))
