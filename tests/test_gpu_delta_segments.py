@@ -50,3 +50,21 @@ def test_decays_that_empty_segments():
     g[:, 256], g[:, 700], g[:, 1024:1280] = -float("inf"), -1e30, -200.0
     fwd.run_and_check("f32", q, k, v, g, beta, S0)
     bwd.run_and_check("f32", q, k, v, g, beta, S0, do, dS)
+
+
+def test_segments_repeat_in_a_graph_on_another_stream():
+    args = bwd.full_inputs(2, 1500, 2, 1, 128, 128, "bf16", 33)
+    want = [t.clone() for t in bwd.grads_of(*args)]
+    o, S = (t.clone() for t in h3.delta_rule(*args[:5], S0=args[5]))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got, fwd2 = bwd.grads_of(*args), h3.delta_rule(*args[:5], S0=args[5])
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            graph.replay()
+            eager = bwd.grads_of(*args)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and all(torch.equal(a, b) for a, b in zip(eager, want))
+        assert torch.equal(fwd2[0], o) and torch.equal(fwd2[1], S)
