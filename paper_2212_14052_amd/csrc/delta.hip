@@ -18,9 +18,9 @@
 // the chunk's keys and queries in LDS, fetched one chunk ahead.
 //
 // At 8 sequences of 2048 tokens, 6 heads of 128 x 128, fp16: chunks 33 us (141 MB through
-// memory, 4.2 TB/s), scan 112: 32 chunks after one another at 3.5 us, whose 132 matrix instructions of a
+// memory, 4.2 TB/s), scan 115: 32 chunks after one another at 3.6 us, whose 132 matrix instructions of a
 // wave would take 0.9.  What is left is the chain inside a chunk: K S, then R, its largest values,
-// X R, the errors' largest values, P u and the new state, each waiting for the one before, and
+// X R, the errors' and their decayed ones' largest values, P u and the new state, each waiting for the one before, and
 // the vector instructions between them.
 #include <math.h>
 
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a, uint4 *__
 // What the backward pass reads is stored between the last products, and past the caches: a CU takes
 // 1 KB of stores or copies every 16 cycles, and a wave waits where it asks for many at once, as for
 // the state at a chunk's start, behind the next chunk's copies (both kernels for 4 x 2048
-// tokens of 20 heads of 128 bf16: 213 us as it is, 165 with nothing kept; with P and u in one piece 204, then 234 at a
+// tokens of 20 heads of 128 bf16: 212 us as it is, 169 with nothing kept; with P and u in one piece 204, then 234 at a
 // chunk's start past the caches, and 244 through them).
 //
 // Sequences may be cut into segments (see DeltaSegments).  In mode MAP a workgroup
@@ -563,7 +563,7 @@ __global__ __launch_bounds__(64 * NW, MODE == MAP ? NW / 2 : NW / 4) void delta_
 // gradient of the state behind each, in reverse): S <- F S + D.  A workgroup takes 16
 // columns, its four waves share the rows: each holds its part of the next map while
 // the states go round through LDS.  Bound by latency: 11 steps of 20 heads of 128 x 128 take 51 us,
-// a load, a product and two barriers each, against 274 for the scan that they let run at once.
+// a load, a product and two barriers each, against 276 for the scan that they let run at once.
 template <int KS>
 __global__ __launch_bounds__(256, 1) void delta_join_kernel(DeltaArgs a, DeltaSegments sg, const float *__restrict__ S0, bool back) {
     constexpr int TW = (KS + 1) / 2;   // row tiles a wave

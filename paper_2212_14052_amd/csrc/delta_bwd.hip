@@ -6,7 +6,7 @@
 //     du = P^T do + t (K dS'),   z = du - (diag(beta) X)^T du,   y = beta z = dv,
 //     dS = exp(G_63) dS' + Q^T (f do) - K^T (f y)
 // is again a scan whose columns do not meet, in the order from the end
-// (delta_bwd_scan_kernel, bound by the same chain inside a chunk as the forward pass's: 138 us for 4 x 2048
+// (delta_bwd_scan_kernel, bound by the same chain inside a chunk as the forward pass's: 141 us for 4 x 2048
 // tokens of 20 heads of 128 bf16; with dS' stored at a chunk's start it took 186 where it took 142); it leaves z and dS' of every chunk.  Then every chunk for itself
 // (delta_bwd_chunk_kernel), with
 //     D = lower part of (do u^T) exp(G_i - G_j),  E = -(strictly lower part of (y u^T) exp(G_i - G_j)):
@@ -278,7 +278,7 @@ template <int DT, int KS> struct GradLds {
 // (rows are channels), so that a lane holds four consecutive channels of one token; and a row tile
 // of D and E, of eight waves the first four of D, the others of E.
 //
-// 4 x 2048 tokens of 20 heads of 128 bf16: 255 us for 783 MB, 3.1 TB/s.  The states alone are as many
+// 4 x 2048 tokens of 20 heads of 128 bf16: 272 us for 783 MB, 2.9 TB/s; 17 of them for the sums of dg.  The states alone are as many
 // bytes as the chunk's inputs and gradients together, and a CU holds one workgroup, whose
 // loads run beside its products but not beside its splits.  With four waves, D and E split by every
 // wave for itself and keys and queries asked for only then it took 293; in the 128 registers a
