@@ -335,7 +335,8 @@ int h3_delta_step(const void *q, const void *k, const void *v, const float *g, c
  *   nothing that is written overlaps anything.
  * States, gates and sums are float32, differences of summed log decays
  * float64; a NaN or Inf may reach every token of its chunk of 64, in v or S0 of its own column.  Where no token
- * stretches the state (g <= 0, 0 <= beta |k|^2 <= 2) a chunk is off by a few 2^-22 of the size of a state's column;
+ * stretches the state (g <= 0, 0 <= beta |k|^2 <= 2) a chunk is off by a few 2^-22 of the largest size
+ * that a state's column has in it (what is 2^-16 of that and less, or under 2^-67, keeps fewer bits than 22);
  * where tokens do, a chunk's solved matrix grows with what its 64 tokens stretch, and its errors with it.
  * float32 keys and queries less than 2^-16 of their chunk's largest count with fewer bits than 22, below 2^-38 with none;
  * bf16 ones are exact down to 2^-31 of it, fp16 ones always.
@@ -359,7 +360,9 @@ int h3_delta_rule(const void *q, const void *k, const void *v, const float *g, c
  *   dS0         (B, H, Dk, Dv) float32, the gradient of the first state, or NULL; may be dS's buffer.
  *               Gradients of tokens from lengths[b] on are 0.
  *   workspace   >= h3_workspace_size(H3_OP_DELTA_BWD, B, H, L, Dk, Dv, dtype).
- * Nothing else that is written overlaps anything.  Results do not depend on timing.
+ * Nothing else that is written overlaps anything.  Results do not depend on timing.  Precision as in h3_delta_rule; sums
+ * over columns (dq, dk, dg, dbeta's products) count a column's part with fewer bits than 22 where it is 2^-16 of the largest
+ * column's and less, in the state or in its gradient.  dg_t has token t's decay as a factor (0 at -inf).
  * Errors: EINVAL, EUNSUPPORTED (Dk, Dv, dtype, H Dv > 2^22, 2^32 threads: see h3_delta_rule), EWORKSPACE, EDEVICE.
  */
 int h3_delta_rule_bwd(const void *q, const void *k, const void *v, const float *g, const float *beta, const void *dout,

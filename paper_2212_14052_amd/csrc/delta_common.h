@@ -11,7 +11,7 @@
 // fp16 cannot hold is below 2^-38 of that largest value; bf16 inputs are then one
 // exact piece (down to 2^-31 of the largest).  Exponents are kept as integers
 // and undone in float32.  Each column of a state has its own; keys and queries have one for a
-// chunk, triangular matrices one each.  (Three bf16 pieces, which need no scales, cost 182
+// chunk, triangular matrices one each: what lies 2^-16 and more below the largest that shares its scale has fewer bits.  (Three bf16 pieces, which need no scales, cost 182
 // matrix instructions a chunk of 16 columns where these cost 132.)
 #pragma once
 #include "common.h"
